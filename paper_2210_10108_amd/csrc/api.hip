@@ -773,6 +773,13 @@ pnerf_status run(pnerf_field* F, Mode mode, int32_t K, const float* poses, int32
 }  // namespace
 
 // =================================================================== C ABI
+void pnerf::set_last_error(const char* msg) {
+  try {
+    g_err = msg;
+  } catch (...) {  // no memory for the message: the status alone tells
+  }
+}
+
 extern "C" {
 
 const char* pnerf_last_error(void) { return g_err.c_str(); }

@@ -254,6 +254,9 @@ hipError_t launch_resample(int K, float* poses, float* state, int state_dim, con
 // be current): 2 * max_k int32 words, looked up once per device.
 hipError_t resample_scratch(int device, int32_t** ptr, int* max_k);
 
+// The message that pnerf_last_error returns on this thread.
+void set_last_error(const char* msg);
+
 int reduce_parts(int K);
 int mlp_fwd_blocks_per_cu(int lpg, int f16);
 int mlp_bwd_blocks_per_cu(int lpg, int sh_dir_grad, int f16);

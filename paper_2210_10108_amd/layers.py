@@ -1,0 +1,386 @@
+"""Python binding of the layer operators (C ABI in include/pnerf_layers.h).
+
+Argument marshalling only, as in `pnerf`: every operator runs in libpnerf.so,
+torch provides device memory and the stream.  Tensors may have any strides as
+long as their last dimension is contiguous; outputs that are not passed in are
+allocated contiguous.  A call enqueues its kernels on `stream` (default: the
+device's current stream) and returns.  Outputs and workspaces that it allocates
+are torch's memory of that stream, and inputs used on another stream than the
+current one are recorded on it, so tensors may be dropped while the work is
+queued; what the streams wait for is the caller's, as everywhere in torch.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+from . import pnerf
+
+F32, F16, BF16 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+class AttentionParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("q_rows", C.c_int32),
+                ("kv_rows", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("scale", C.c_float),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+                ("v_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3),
+                ("do_stride", C.c_int64 * 3), ("dq_stride", C.c_int64 * 3),
+                ("dk_stride", C.c_int64 * 3), ("dv_stride", C.c_int64 * 3),
+                ("q_len", C.c_void_p), ("kv_len", C.c_void_p), ("kv_mask", C.c_void_p),
+                ("kv_mask_stride", C.c_int64)]
+
+
+class NormRotateParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("q_rows", C.c_int32), ("k_rows", C.c_int32),
+                ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("n_positions", C.c_int32),
+                ("eps", C.c_float),
+                ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2),
+                ("q_out_stride", C.c_int64 * 2), ("k_out_stride", C.c_int64 * 2),
+                ("dq_out_stride", C.c_int64 * 2), ("dk_out_stride", C.c_int64 * 2),
+                ("dq_stride", C.c_int64 * 2), ("dk_stride", C.c_int64 * 2),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("table", C.c_void_p),
+                ("q_pos", C.c_void_p), ("k_pos", C.c_void_p)]
+
+
+class LinearParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("m", C.c_int32),
+                ("n", C.c_int32), ("k", C.c_int32),
+                ("x_stride", C.c_int64), ("w_stride", C.c_int64), ("residual_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("z_stride", C.c_int64), ("dy_stride", C.c_int64),
+                ("dx_stride", C.c_int64), ("dw_stride", C.c_int64)]
+
+
+_P, _I64, _I32 = C.c_void_p, C.c_int64, C.c_int32
+# name -> argtypes; every function declared in include/pnerf_layers.h (each returns a status)
+_SIGS = {
+    "pnerf_cross_attention_workspace": [_P, _I32, _P],
+    "pnerf_cross_attention": [_P] * 7 + [_I64, _P],
+    "pnerf_cross_attention_backward": [_P] * 11 + [_I64, _P],
+    "pnerf_norm_rotate": [_P] * 6,
+    "pnerf_norm_rotate_workspace": [_P, _P],
+    "pnerf_norm_rotate_backward": [_P] * 10 + [_I64, _P],
+    "pnerf_linear_workspace": [_P, _I32, _P],
+    "pnerf_linear": [_P] * 8 + [_I64, _P],
+    "pnerf_linear_backward": [_P] * 9 + [_I64, _P],
+}
+
+_lib = None
+
+
+def lib() -> C.CDLL:
+    """libpnerf.so with the signatures of the layer operators."""
+    global _lib
+    if _lib is None:
+        L = pnerf.lib()
+        for name, args in _SIGS.items():
+            fn = getattr(L, name)
+            fn.restype = C.c_int
+            fn.argtypes = args
+        _lib = L
+    return _lib
+
+
+def _check(status: int):
+    if status != pnerf.OK:
+        raise pnerf.PnerfError(status, lib().pnerf_last_error().decode())
+
+
+class _Call:
+    """One call: its device and stream, what it allocates, what it keeps alive."""
+
+    def __init__(self, first, stream):
+        import torch
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            raise TypeError("operands must be device tensors")
+        self.device, self.dtype = first.device, first.dtype
+        if self.dtype not in _dtypes():
+            raise TypeError(f"unsupported data type {self.dtype}")
+        self.code = _dtypes()[self.dtype]
+        current = torch.cuda.current_stream(self.device)
+        self.stream = current if stream is None else stream
+        if self.stream.device != self.device:
+            raise ValueError(f"stream on {self.stream.device}, tensors on {self.device}")
+        self.foreign = self.stream != current
+
+    def tensor(self, t, name, shape, dtype=None, contiguous=False):
+        """Checks a tensor and returns its address (None for None)."""
+        if t is None:
+            return None
+        if not t.is_cuda or t.device != self.device:
+            raise TypeError(f"{name} must be on {self.device}")
+        if t.dtype != (dtype or self.dtype):
+            raise TypeError(f"{name} must be {dtype or self.dtype}, got {t.dtype}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+        if contiguous:
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        elif t.stride(-1) != 1 and shape[-1] > 1:
+            raise ValueError(f"the last dimension of {name} must be contiguous")
+        if self.foreign:
+            t.record_stream(self.stream)
+        return t.data_ptr()
+
+    def new(self, shape, dtype=None):
+        """An output or workspace: memory of the call's stream, which the current
+        one may read as well."""
+        import torch
+        if not self.foreign:
+            return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            t = torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
+
+    def workspace(self, nbytes):
+        """(address, bytes, the tensor) of a workspace."""
+        if not nbytes:
+            return None, 0, None
+        import torch
+        t = self.new((nbytes,), torch.uint8)
+        return t.data_ptr(), nbytes, t
+
+    def run(self, fn, *args):
+        import torch
+        s = C.c_void_p(self.stream.cuda_stream)
+        if torch.cuda.current_device() == self.device.index:
+            _check(fn(*args, s))
+        else:
+            with torch.cuda.device(self.device):
+                _check(fn(*args, s))
+
+
+_DTYPES = None
+
+
+def _dtypes():
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+    return _DTYPES
+
+
+# ---------------------------------------------------------------- attention
+def _attention(call, q, k, v, q_len, kv_len, kv_mask, scale):
+    import torch
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must have 4 dimensions: batch, rows, heads, head width")
+    B, Sq, Hq, D = q.shape
+    Sk, Hkv = k.shape[1:3]
+    p = AttentionParams()
+    p.dtype, p.batch, p.q_rows, p.kv_rows = call.code, B, Sq, Sk
+    p.q_heads, p.kv_heads, p.head_dim = Hq, Hkv, D
+    p.scale = (1.0 / math.sqrt(D) if D else 1.0) if scale is None else scale
+    p.q_stride[:] = q.stride()[:3]
+    p.k_stride[:] = k.stride()[:3]
+    p.v_stride[:] = v.stride()[:3]
+    p.q_len = call.tensor(q_len, "q_len", (B,), torch.int32, True)
+    p.kv_len = call.tensor(kv_len, "kv_len", (B,), torch.int32, True)
+    if kv_mask is not None:
+        if kv_mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"kv_mask must be torch.bool or torch.uint8, got {kv_mask.dtype}")
+        p.kv_mask = call.tensor(kv_mask, "kv_mask", (B, Sk), kv_mask.dtype)
+        p.kv_mask_stride = kv_mask.stride(0)
+    qp, kp, vp = (call.tensor(q, "q", (B, Sq, Hq, D)), call.tensor(k, "k", (B, Sk, Hkv, D)),
+                  call.tensor(v, "v", (B, Sk, Hkv, D)))
+    return p, qp, kp, vp
+
+
+def cross_attention(q, k, v, q_len=None, kv_len=None, kv_mask=None, scale=None, o=None,
+                    return_lse: bool = False, stream=None):
+    """pnerf_cross_attention.  q [B, Sq, Hq, D], k and v [B, Sk, Hkv, D] (float16
+    or bfloat16, Hq a multiple of Hkv, D at most 128); q_len and kv_len int32 [B];
+    kv_mask bool or uint8 [B, Sk], nonzero where a key may be read; scale defaults
+    to 1 / sqrt(D).  Returns o [B, Sq, Hq, D], or (o, lse) with lse float32
+    [B, Hq, Sq], which the backward pass needs."""
+    import torch
+    call = _Call(q, stream)
+    p, qp, kp, vp = _attention(call, q, k, v, q_len, kv_len, kv_mask, scale)
+    if o is None:
+        o = call.new(q.shape)
+    op = call.tensor(o, "o", tuple(q.shape))
+    p.o_stride[:] = o.stride()[:3]
+    lse = call.new((q.shape[0], q.shape[2], q.shape[1]), torch.float32) if return_lse else None
+    lp = call.tensor(lse, "lse", tuple(lse.shape), torch.float32) if return_lse else None
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_cross_attention_workspace(ref, 0, C.byref(n)))
+    ws, nb, _keep = call.workspace(n.value)
+    call.run(_lib.pnerf_cross_attention, ref, qp, kp, vp, op, lp, ws, nb)
+    return (o, lse) if return_lse else o
+
+
+def cross_attention_backward(do, q, k, v, o, lse, q_len=None, kv_len=None, kv_mask=None, scale=None,
+                             dq=None, dk=None, dv=None, stream=None):
+    """pnerf_cross_attention_backward: (dq, dk, dv) for do = dL/do, with o and lse
+    as cross_attention(..., return_lse=True) gave them and its other arguments."""
+    import torch
+    call = _Call(q, stream)
+    p, qp, kp, vp = _attention(call, q, k, v, q_len, kv_len, kv_mask, scale)
+    B, Sq, Hq, _ = shape = tuple(q.shape)
+    dq = call.new(shape) if dq is None else dq
+    dk = call.new(k.shape) if dk is None else dk
+    dv = call.new(k.shape) if dv is None else dv
+    op, dop = call.tensor(o, "o", shape), call.tensor(do, "do", shape)
+    lp = call.tensor(lse, "lse", (B, Hq, Sq), torch.float32, True)
+    dqp, dkp, dvp = (call.tensor(dq, "dq", shape), call.tensor(dk, "dk", tuple(k.shape)),
+                     call.tensor(dv, "dv", tuple(k.shape)))
+    p.o_stride[:], p.do_stride[:] = o.stride()[:3], do.stride()[:3]
+    p.dq_stride[:], p.dk_stride[:], p.dv_stride[:] = dq.stride()[:3], dk.stride()[:3], dv.stride()[:3]
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_cross_attention_workspace(ref, 1, C.byref(n)))
+    ws, nb, _keep = call.workspace(n.value)
+    call.run(_lib.pnerf_cross_attention_backward, ref, qp, kp, vp, op, lp, dop, dqp, dkp, dvp, ws, nb)
+    return dq, dk, dv
+
+
+# ---------------------------------------------------------------- norm and rotation
+def _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved):
+    import torch
+    p = NormRotateParams()
+    p.dtype, p.eps, p.interleaved = call.code, eps, int(interleaved)
+    p.head_dim = D = q.shape[-1]
+    if table is not None:
+        if table.dim() != 3 or table.shape[1] != 2:
+            raise ValueError(f"table has shape {tuple(table.shape)}, expected (positions, 2, pairs)")
+        p.n_positions, p.rotary_dim = table.shape[0], 2 * table.shape[2]
+        p.table = call.tensor(table, "table", tuple(table.shape), torch.float32, True)
+    ptrs = []
+    for side, x, w, pos in (("q", q, q_weight, q_pos), ("k", k, k_weight, k_pos)):
+        if x is None:
+            ptrs.append(None)
+            continue
+        if x.dim() != 3:
+            raise ValueError(f"{side} must have 3 dimensions: rows, heads, head width")
+        T, H, _ = x.shape
+        ptrs.append(call.tensor(x, side, (T, H, D)))
+        setattr(p, side + "_rows", T)
+        setattr(p, side + "_heads", H)
+        getattr(p, side + "_stride")[:] = x.stride()[:2]
+        setattr(p, side + "_weight", call.tensor(w, side + "_weight", (D,), None, True))
+        setattr(p, side + "_pos", call.tensor(pos, side + "_pos", (T,), torch.int32, True))
+    return p, ptrs
+
+
+def norm_rotate(q, k, q_weight, k_weight, table, q_pos, k_pos, eps: float = 1e-6,
+                interleaved: bool = False, q_out=None, k_out=None, stream=None):
+    """pnerf_norm_rotate.  q [Tq, Hq, D] and k [Tk, Hk, D] (or k None: queries
+    alone), weights [D] or None; table float32 [positions, 2, pairs] (cosines,
+    sines) or None (no rotation), positions int32 [Tq] and [Tk].  Returns
+    (q_out, k_out); an output may be its input."""
+    call = _Call(q, stream)
+    p, (qp, kp) = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
+    q_out = call.new(q.shape) if q_out is None else q_out
+    qo = call.tensor(q_out, "q_out", tuple(q.shape))
+    p.q_out_stride[:] = q_out.stride()[:2]
+    ko = None
+    if k is not None:
+        k_out = call.new(k.shape) if k_out is None else k_out
+        ko = call.tensor(k_out, "k_out", tuple(k.shape))
+        p.k_out_stride[:] = k_out.stride()[:2]
+    call.run(lib().pnerf_norm_rotate, C.byref(p), qp, kp, qo, ko)
+    return q_out, k_out if k is not None else None
+
+
+def norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, q_pos, k_pos,
+                         eps: float = 1e-6, interleaved: bool = False, dq=None, dk=None, stream=None):
+    """pnerf_norm_rotate_backward: (dq, dk, dq_weight, dk_weight) for the
+    gradients of the outputs; dk and dk_weight are None where k is, a weight's
+    gradient where the weight is.  dq may be dq_out, dk may be dk_out."""
+    call = _Call(q, stream)
+    p, (qp, kp) = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
+    out, ptrs = [], []
+    for side, x, dy, dx, w in (("q", q, dq_out, dq, q_weight), ("k", k, dk_out, dk, k_weight)):
+        if x is None:
+            out += [None, None]
+            ptrs.append((None, None, None))
+            continue
+        dx = call.new(x.shape) if dx is None else dx
+        dw = None if w is None else call.new(w.shape)
+        ptrs.append((call.tensor(dy, f"d{side}_out", tuple(x.shape)),
+                     call.tensor(dx, f"d{side}", tuple(x.shape)),
+                     call.tensor(dw, f"d{side}_weight", tuple(x.shape[-1:]))))
+        getattr(p, f"d{side}_out_stride")[:] = dy.stride()[:2]
+        getattr(p, f"d{side}_stride")[:] = dx.stride()[:2]
+        out += [dx, dw]
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_norm_rotate_workspace(ref, C.byref(n)))
+    ws, nb, _keep = call.workspace(n.value)
+    (gq, dqp, wq), (gk, dkp, wk) = ptrs
+    call.run(_lib.pnerf_norm_rotate_backward, ref, qp, kp, gq, gk, dqp, dkp, wq, wk, ws, nb)
+    return out[0], out[2], out[1], out[3]
+
+
+# ---------------------------------------------------------------- linear
+def _linear(call, x, w, activation):
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must have 2 dimensions")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
+    (M, K), N = x.shape, w.shape[1]
+    p = LinearParams()
+    p.dtype, p.activation, p.m, p.n, p.k = call.code, ACTIVATIONS[activation], M, N, K
+    p.x_stride, p.w_stride = x.stride(0), w.stride(0)
+    return p, call.tensor(x, "x", (M, K)), call.tensor(w, "w", (K, N))
+
+
+def linear(x, w, bias=None, residual=None, activation: str = "none", y=None,
+           return_preact: bool = False, stream=None):
+    """pnerf_linear: act(x @ w + bias) + residual for x [M, K], w [K, N] (float16
+    or bfloat16), bias [N], residual [M, N]; activation "none", "relu", "gelu"
+    or "silu".  y may be the residual.  Returns y, or (y, z) with
+    return_preact, z = x @ w + bias as linear_backward takes it."""
+    call = _Call(x, stream)
+    p, xp, wp = _linear(call, x, w, activation)
+    shape = (p.m, p.n)
+    bp = call.tensor(bias, "bias", (p.n,), None, True)
+    rp = call.tensor(residual, "residual", shape)
+    if residual is not None:
+        p.residual_stride = residual.stride(0)
+    y = call.new(shape) if y is None else y
+    yp = call.tensor(y, "y", shape)
+    p.y_stride = y.stride(0)
+    z = zp = None
+    if return_preact:
+        z = call.new(shape)
+        zp = call.tensor(z, "z", shape)
+        p.z_stride = z.stride(0)
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_linear_workspace(ref, 0, C.byref(n)))
+    ws, nb, _keep = call.workspace(n.value)
+    call.run(_lib.pnerf_linear, ref, xp, wp, bp, rp, yp, zp, ws, nb)
+    return (y, z) if return_preact else y
+
+
+def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = True, dx=None, dw=None,
+                    stream=None):
+    """pnerf_linear_backward: (dx, dw, db) for dy = dL/dy; db is None without
+    bias.  z as linear(..., return_preact=True) gave it (None will do when the
+    activation is "none").  The residual's gradient is dy itself."""
+    call = _Call(x, stream)
+    p, xp, wp = _linear(call, x, w, activation)
+    shape = (p.m, p.n)
+    gp = call.tensor(dy, "dy", shape)
+    p.dy_stride = dy.stride(0)
+    zp = call.tensor(z, "z", shape)
+    if z is not None:
+        p.z_stride = z.stride(0)
+    dx = call.new(x.shape) if dx is None else dx
+    dw = call.new(w.shape) if dw is None else dw
+    db = call.new((p.n,)) if bias else None
+    dxp, dwp = call.tensor(dx, "dx", tuple(x.shape)), call.tensor(dw, "dw", tuple(w.shape))
+    dbp = call.tensor(db, "db", (p.n,))
+    p.dx_stride, p.dw_stride = dx.stride(0), dw.stride(0)
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_linear_workspace(ref, 1, C.byref(n)))
+    ws, nb, _keep = call.workspace(n.value)
+    call.run(_lib.pnerf_linear_backward, ref, xp, wp, zp, gp, dxp, dwp, dbp, ws, nb)
+    return dx, dw, db
