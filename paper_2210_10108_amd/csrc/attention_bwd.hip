@@ -173,20 +173,42 @@ __global__ __launch_bounds__(NW * 64) void k_attn_dq(const AttnArgs a, int split
     }
     __syncthreads();
     if (t + 1 < t1) fetch(t + 1);
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      floatx16 s = {}, dp = {};
+    auto first = [&](int n, floatx16& s, floatx16& dp) {
+      s = dp = floatx16{};
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         const int p = swz<CH>(32 * n + r, 2 * i + h);
         s = T::mma(sk[p], qf[i], s);
         dp = T::mma(sv[p], gf[i], dp);
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -st[0]));
+    };
+    if (nk <= kBN) {
+      // few keys: o's rounding weighs on do . o, so delta is taken as sum_j p dp,
+      // which this one tile holds, for the dk, dv pass as well
+      float sum = 0.0f;
+#pragma unroll 1
+      for (int n = 0; n < 2; ++n) {
+        floatx16 s, dp;
+        first(n, s, dp);
+        const uint32_t w = (uint32_t)(vm >> (32 * n)) >> (4 * h);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += (w >> (8 * (i / 4) + i % 4)) & 1 ? s[i] * dp[i] : 0.0f;
+      }
+      float s0, s1;
+      halves(sum, s0, s1);
+      st[1] = ldexpf(s0 + s1, -a.shift);
+      if (h == 0 && ok) reinterpret_cast<floatx2*>(a.delta)[at] = st;
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      floatx16 s, dp;
+      first(n, s, dp);
       const uint32_t w = (uint32_t)(vm >> (32 * n)) >> (4 * h);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -st[0]));
-        s[i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? p * (dp[i] - st[1]) : 0.0f;
+        s[i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? s[i] * (dp[i] - st[1]) : 0.0f;
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {

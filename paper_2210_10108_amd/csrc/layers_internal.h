@@ -164,6 +164,13 @@ __device__ __forceinline__ void halves(float x, float& a, float& b) {
   b = __uint_as_float(r[1]);
 }
 
+// LDS written by lanes of this wavefront may be read by its others from here on
+// (a wavefront's LDS accesses complete in order: this holds the compiler).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Work item `id` of n such that consecutive items run on one XCD (workgroups
 // go to the XCDs in turn): items that share operands share an L2.
 __device__ __forceinline__ int xcd_order(int id, int n) {

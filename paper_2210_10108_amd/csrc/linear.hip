@@ -74,6 +74,26 @@ __device__ __forceinline__ void finish4(const Product& p, int m, int n, float c[
   store4<VEC>((uint16_t*)p.c + m * p.cs + n, make_uint2(T::pack(c[0], c[1]), T::pack(c[2], c[3])), cnt);
 }
 
+// c[0..7] of row m, columns n..n+7, aligned rows.
+template <class T, bool EPI>
+__device__ __forceinline__ void finish8(const Product& p, int m, int n, float c[8]) {
+  auto add = [&](const uint4 v) {
+    c[0] += T::lo(v.x), c[1] += T::hi(v.x), c[2] += T::lo(v.y), c[3] += T::hi(v.y);
+    c[4] += T::lo(v.z), c[5] += T::hi(v.z), c[6] += T::lo(v.w), c[7] += T::hi(v.w);
+  };
+  auto packed = [&] { return make_uint4(T::pack(c[0], c[1]), T::pack(c[2], c[3]), T::pack(c[4], c[5]), T::pack(c[6], c[7])); };
+  if (EPI) {
+    uint4 res = make_uint4(0, 0, 0, 0);
+    if (p.res) res = *reinterpret_cast<const uint4*>((const uint16_t*)p.res + m * p.rs + n);
+    if (p.bias) add(*reinterpret_cast<const uint4*>((const uint16_t*)p.bias + n));
+    if (p.z) *reinterpret_cast<uint4*>((uint16_t*)p.z + m * p.zs + n) = packed();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = act_value(p.act, c[i]);
+    if (p.res) add(res);
+  }
+  *reinterpret_cast<uint4*>((uint16_t*)p.c + m * p.cs + n) = packed();
+}
+
 // Any sizes, strides and alignment: 64 x 64 tiles, 32 deep, a 32 x 32 part a
 // wavefront; both operands go through LDS with their contracted axis contiguous.
 // The product is formed transposed (A operand: columns of B), so that a lane's
@@ -135,6 +155,326 @@ __global__ __launch_bounds__(256) void k_product_any(const Product p) {
   }
 }
 
+// ------------------------------------------------------------ aligned products
+// Rows of 16-byte chunks go from memory to LDS by loads that write LDS
+// themselves, 64 chunks of consecutive LDS a wavefront and instruction; a chunk's
+// place within its row is xored with bits of the row so that the fragment reads
+// cover all banks, which the lanes' addresses in memory follow.  The buffer
+// descriptor's bound gives zeros past the last row; lanes past the end of a row
+// take an offset beyond any bound.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr int kBK = 64;                      // depth of a tile in LDS
+constexpr uint32_t kOutside = 0x80000000u;   // an offset beyond every descriptor's bound
+constexpr int64_t kMaxFastStride = 1 << 21;  // elements: a tile's offsets stay below 2^31 bytes
+
+// (m0, the destination, is no register that the compiler keeps anything in here:
+// nothing else in these kernels uses it.)
+__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, u32x4 desc) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(lds), "v"(offset), "s"(desc) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+
+// One operand's tile of ROWS rows (of A, or columns of B) x 64: its loads and
+// its fragments.  KC: the contracted axis is contiguous, an LDS row is a row of
+// the operand, 8 chunks; else an LDS row is one k, ROWS / 8 chunks.
+template <int ROWS, int NW, bool KC>
+struct Tile {
+  static constexpr int kChunks = KC ? kBK / 8 : ROWS / 8;        // of an LDS row
+  static constexpr int kLoads = ROWS * kBK / 8 / 64 / NW;        // instructions a wavefront
+  static constexpr int kStep = NW * 64 / kChunks;                // LDS rows between them
+  static constexpr int kBytes = ROWS * kBK * 2;
+  const char* base;   // of the current tile in memory
+  int64_t row_bytes;  // between LDS rows
+  int rows, inner;    // LDS rows left, and elements of one
+  uint32_t off;       // this lane's first chunk
+  int chunk;          // ... and which of its row it is
+  uint32_t frag[KC ? 4 : 2];
+
+  __device__ __forceinline__ void init(const Operand& o, int i0, int most, int k0, int K, int wave, int lane,
+                                       int ifrag) {
+    base = (const char*)o.p + 2 * (i0 * o.si + k0 * o.sk);
+    row_bytes = 2 * (KC ? o.si : o.sk);
+    rows = KC ? most - i0 : K - k0;
+    inner = KC ? K - k0 : most - i0;
+    const int p = wave * 64 + lane, r = p / kChunks;
+    chunk = (p % kChunks) ^ (KC ? r & 7 : (r & 3) << 1);
+    off = (uint32_t)(r * row_bytes + 16 * chunk);
+    const int l32 = lane & 31, h = lane >> 5, l16 = lane & 15;
+    if (KC) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) frag[s] = (ifrag + l32) * (2 * kBK) + 16 * ((2 * s + h) ^ (l32 & 7));
+    } else {
+      const int k = 8 * h + l16 / 4, col = ifrag + 16 * ((lane >> 4) & 1) + 4 * (l16 % 4);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        frag[s] = k * (2 * ROWS) + 16 * (((col + 32 * s) / 8) ^ ((k & 3) << 1)) + 2 * (col % 8);
+    }
+  }
+  // Loads n0 .. n1 - 1 of the tile, into LDS at lds.
+  template <int N0, int N1>
+  __device__ __forceinline__ void load(uint32_t lds, int wave) {
+    const int64_t span = (rows - 1) * row_bytes + 2 * inner;
+    u32x4 desc;
+    desc[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
+    desc[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xFFFFu);
+    desc[2] = __builtin_amdgcn_readfirstlane((uint32_t)min(span, (int64_t)0x7FFFFFFF));
+    desc[3] = 0x00027000u;
+    const uint32_t first = 8 * chunk < inner ? off : kOutside;
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
+#pragma unroll
+    for (int n = N0; n < N1; ++n)
+      load_to_lds(to + n * NW * 1024, first + (uint32_t)(n * kStep) * (uint32_t)row_bytes, desc);
+  }
+  __device__ __forceinline__ void next() {
+    base += KC ? 2 * kBK : kBK * row_bytes;
+    if (KC)
+      inner -= kBK;
+    else
+      rows -= kBK;
+  }
+  // Fragment of 32 rows (number t of the wavefront's) at depth 16 s.
+  __device__ __forceinline__ uint4 fragment(const char* lds, int t, int s) const {
+    if (KC) return *reinterpret_cast<const uint4*>(lds + frag[s] + t * 32 * 2 * kBK);
+    const char* p = lds + frag[t & 1] + (t / 2) * 128 + s * 16 * (2 * ROWS);
+    const uint2 a = read_tr(p), b = read_tr(p + 4 * (2 * ROWS));
+    return make_uint4(a.x, a.y, b.x, b.y);
+  }
+};
+
+// BM x BN tiles, 64 deep, two of them in LDS: while the products of one run, the
+// loads of the one after the next fill the buffer just read.  Four wavefronts,
+// 2 x 2; fragments are read one 16-deep step ahead, across the tiles' border, so
+// that the one barrier a tile falls between the last reads of a tile and the
+// last of its products.
+template <class T, bool EPI, bool AK, bool BK, int BM, int BN>
+__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(const Product p, int splits, float* part) {
+  constexpr int TM = BM / 64, TN = BN / 64;  // 32 x 32 results a wavefront
+  using TA = Tile<BM, 4, AK>;
+  using TB = Tile<BN, 4, BK>;
+  constexpr int kBuf = TA::kBytes + TB::kBytes;
+  __shared__ alignas(128) char lds[2 * kBuf];
+
+  // tiles in the order of the XCDs, and within one XCD's run 8 rows of tiles at a
+  // time, so that the tiles in flight share operands in its L2
+  const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN;
+  int id = xcd_order(blockIdx.x, gridDim.x);
+  const int sp = id / (tiles_m * tiles_n);
+  id -= sp * tiles_m * tiles_n;
+  const int band = id / (8 * tiles_n), in_band = id - band * 8 * tiles_n;
+  const int height = min(8, tiles_m - band * 8);
+  const int m0 = (band * 8 + in_band % height) * BM, n0 = in_band / height * BN;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const int all = (p.K + kBK - 1) / kBK, per = (all + splits - 1) / splits;
+  const int t0 = min(sp * per, all), nt = min(t0 + per, all) - t0;
+
+  TA a;
+  TB b;
+  a.init(p.a, m0, p.M, t0 * kBK, p.K, wave, lane, wm * (BM / 2));
+  b.init(p.b, n0, p.N, t0 * kBK, p.K, wave, lane, wn * (BN / 2));
+  const uint32_t la = lds_address(lds), lb = la + TA::kBytes;
+
+  floatx16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = floatx16{};
+
+  uint4 fa[2][TM], fb[2][TN];
+  auto fragments = [&](int set, const char* buf, int s) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[set][i] = a.fragment(buf, i, s);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[set][j] = b.fragment(buf + TA::kBytes, j, s);
+  };
+  constexpr int HA = TA::kLoads / 2, HB = TB::kLoads / 2;
+  if (nt > 0) {
+    a.template load<0, TA::kLoads>(la, wave), b.template load<0, TB::kLoads>(lb, wave);
+    a.next(), b.next();
+    if (nt > 1) {
+      a.template load<0, TA::kLoads>(la + kBuf, wave), b.template load<0, TB::kLoads>(lb + kBuf, wave);
+      a.next(), b.next();
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    fragments(0, lds, 0);
+  }
+  for (int t = 0; t < nt; ++t) {
+    const int cur = (t & 1) * kBuf, oth = kBuf - cur;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s < 3) {
+        fragments((s + 1) & 1, lds + cur, s + 1);
+      } else if (t + 1 < nt) {
+        // the next tile is in LDS, and every wavefront has read this one
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        fragments(0, lds + oth, 0);
+      }
+      // the tile after the next, into the buffer that the last barrier freed
+      if (s == 3 && t + 2 < nt) {
+        a.template load<0, HA>(la + cur, wave), b.template load<0, HB>(lb + cur, wave);
+      }
+      if (s == 0 && t > 0 && t + 1 < nt) {
+        a.template load<HA, TA::kLoads>(la + oth, wave), b.template load<HB, TB::kLoads>(lb + oth, wave);
+        a.next(), b.next();
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = T::mma(fb[s & 1][j], fa[s & 1][i], acc[i][j]);
+    }
+  }
+
+  // Results by way of LDS, 32 rows of the wavefront at a time, so that a lane
+  // has 8 neighbours of a row and a row's lanes are neighbours.
+  constexpr int kRow = BN / 2 + 4, kLanes = BN / 16;
+  static_assert(4 * 32 * kRow * 4 <= 2 * kBuf, "results fit the tiles' LDS");
+  float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kRow;
+  const int r = lane & 31, h = lane >> 5, n = n0 + wn * (BN / 2) + 8 * (lane % kLanes);
+  __syncthreads();  // every wavefront has read its last fragments
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<floatx4*>(mine + r * kRow + 32 * j + 8 * q + 4 * h) =
+            floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    wave_fence();
+#pragma unroll 1
+    for (int row = lane / kLanes; row < 32; row += 64 / kLanes) {
+      const int m = m0 + wm * (BM / 2) + 32 * i + row;
+      if (m >= p.M || n >= p.N) continue;
+      const floatx4* from = reinterpret_cast<const floatx4*>(mine + row * kRow + 8 * (lane % kLanes));
+      const floatx4 x = from[0], y = from[1];
+      if (splits > 1) {
+        floatx4* to = reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.N + n);
+        to[0] = x, to[1] = y;
+      } else {
+        float c[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        finish8<T, EPI>(p, m, n, c);
+      }
+    }
+    wave_fence();
+  }
+}
+
+// The parts of the contracted axis added up in order, and the epilogue: 4
+// elements of a row a thread.
+template <class T, bool EPI>
+__global__ __launch_bounds__(256) void k_product_join(const Product p, int splits, const float* part) {
+  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (e >= (int64_t)p.M * p.N) return;
+  floatx4 x = *reinterpret_cast<const floatx4*>(part + e);
+  for (int s = 1; s < splits; ++s)
+    x += *reinterpret_cast<const floatx4*>(part + (int64_t)s * p.M * p.N + e);
+  float c[4] = {x[0], x[1], x[2], x[3]};
+  finish4<T, EPI, true>(p, (int)(e / p.N), (int)(e % p.N), c);
+}
+
+// Few rows (at most 32): the weights' bytes are the time.  They go from memory
+// to registers, each once: lane l of a wavefront holds 4 neighbouring columns of
+// W (4 (l % 16) ..) at depths 8 (l / 16) .. + 7, which two-register byte
+// permutes turn into operands of the 16 x 16 x 32 product -- column j of every
+// lane makes one.  A workgroup takes 64 columns, its 16 wavefronts the depths in
+// turn; their sums meet in LDS.
+template <class T>
+struct Mma16;
+template <>
+struct Mma16<F16> {
+  __device__ static __forceinline__ floatx4 mma(uint4 a, uint4 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma16<BF16> {
+  __device__ static __forceinline__ floatx4 mma(uint4 a, uint4 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+
+constexpr int kFewWaves = 16;
+template <class T, int MT>
+__global__ __launch_bounds__(kFewWaves * 64) void k_product_few(const Product p, int splits, float* part) {
+  __shared__ float red[kFewWaves][16 * MT][64 + 4];
+  const int tiles_n = (p.N + 63) / 64;
+  const int n0 = blockIdx.x % tiles_n * 64, sp = blockIdx.x / tiles_n;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
+  const int steps = (p.K + 31) / 32, n = n0 + 4 * c16;
+  const uint16_t* w = (const uint16_t*)p.b.p + n;
+  const uint16_t* x = (const uint16_t*)p.a.p;
+  floatx4 acc[MT][4];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{};
+  uint2 rw[2][8];
+  uint4 rx[2][MT];
+  auto fetch = [&](int set, int step) {
+    const int k0 = 32 * step + 8 * g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      rw[set][i] = n < p.N && k0 + i < p.K ? *reinterpret_cast<const uint2*>(w + (int64_t)(k0 + i) * p.b.sk)
+                                           : make_uint2(0, 0);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int m = 16 * i + c16;
+      rx[set][i] = load8<true>(x + m * p.a.si + k0, m < p.M ? p.K - k0 : 0);
+    }
+  };
+  auto multiply = [&](int set) {
+    const uint2* v = rw[set];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+      uint32_t f[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        f[i] = j < 2 ? __builtin_amdgcn_perm(v[2 * i + 1].x, v[2 * i].x, sel)
+                     : __builtin_amdgcn_perm(v[2 * i + 1].y, v[2 * i].y, sel);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        acc[i][j] = Mma16<T>::mma(make_uint4(f[0], f[1], f[2], f[3]), rx[set][i], acc[i][j]);
+    }
+  };
+  const int stride = kFewWaves * splits, first = sp * kFewWaves + wave;
+  if (first < steps) fetch(0, first);
+  for (int s = first; s < steps; s += 2 * stride) {
+    if (s + stride < steps) fetch(1, s + stride);
+    multiply(0);
+    if (s + stride < steps) {
+      if (s + 2 * stride < steps) fetch(0, s + 2 * stride);
+      multiply(1);
+    }
+  }
+  // result: column m = lane % 16, row 4 g + i of product j is column 4 (4 g + i) + j of the tile
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<floatx4*>(&red[wave][16 * i + c16][4 * (4 * g + q)]) =
+          floatx4{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
+  __syncthreads();
+  for (int e = threadIdx.x; e < 16 * MT * 16; e += kFewWaves * 64) {
+    const int m = e / 16, c = 4 * (e % 16);
+    if (m >= p.M || n0 + c >= p.N) continue;
+    floatx4 t = {};
+#pragma unroll
+    for (int i = 0; i < kFewWaves; ++i) t += *reinterpret_cast<const floatx4*>(&red[i][m][c]);
+    if (splits > 1) {
+      *reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.N + n0 + c) = t;
+    } else {
+      float v[4] = {t[0], t[1], t[2], t[3]};
+      finish4<T, true, true>(p, m, n0 + c, v);
+    }
+  }
+}
+
 // dz = dy act'(z) (left out where act is none: dz is dy) and the column sums of
 // 64 rows each: 256 columns a workgroup, 8 a thread.
 template <class T, bool VEC>
@@ -188,27 +528,100 @@ __global__ __launch_bounds__(256) void k_linear_db(const float* part, int blocks
                                                red[2][threadIdx.x] + red[3][threadIdx.x]);
 }
 
-template <class T, bool EPI, bool AK, bool BK>
-void product(const Product& p, hipStream_t s) {
-  if (p.M == 0) return;
-  const int64_t n = (int64_t)((p.M + 63) / 64) * ((p.N + 63) / 64);
-  k_product_any<T, EPI, AK, BK><<<(unsigned)n, 256, 0, s>>>(p);
+// How a product is run: which kernel, and into how many parts its contracted
+// axis is cut.
+enum Kind { kAny, kFew, kTile128, kTile256 };
+struct Plan {
+  Kind kind;
+  int splits;
+};
+
+// Tiles of 256 x 256 read the least from LDS and memory, but there must be
+// enough of them to go round the compute units; smaller products take 128 x 128
+// tiles, two workgroups a compute unit, and where those are still too few, parts
+// of the depth of at least 4 tiles each.
+Plan plan_of(int M, int N, int K, bool fast, bool few) {
+  if (!fast) return {kAny, 1};
+  auto over = [](int a, int b) { return ((int64_t)a + b - 1) / b; };
+  if (few && M <= 32) {
+    const int64_t wgs = over(N, 64), most = over(K, 32) / (2 * kFewWaves);
+    return {kFew, (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / wgs, most))};
+  }
+  const int64_t big = over(M, 256) * over(N, 256);
+  if (big >= 3 * kCUs / 4) return {kTile256, 1};
+  const int64_t small = std::max<int64_t>(1, over(M, 128) * over(N, 128));  // M may be 0
+  return {kTile128, (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCUs / small, over(K, kBK) / 4))};
+}
+int64_t plan_bytes(const Plan& pl, int64_t M, int64_t N) { return pl.splits > 1 ? pl.splits * M * N * 4 : 0; }
+
+bool fast_strides(const Product& p, bool AK, bool BK) {
+  return (AK ? p.a.si : p.a.sk) <= kMaxFastStride && (BK ? p.b.si : p.b.sk) <= kMaxFastStride;
 }
 
-template <class T>
-void forward(const LinearArgs& a, void* ws, hipStream_t s) {
+template <class T, bool EPI, bool AK, bool BK>
+void product(const Product& p, const Plan& pl, float* part, hipStream_t s) {
+  if (p.M == 0) return;
+  auto tiles = [&](int a, int b) { return (unsigned)(((int64_t)p.M + a - 1) / a * (((int64_t)p.N + b - 1) / b)); };
+  switch (pl.kind) {
+    case kAny:
+      k_product_any<T, EPI, AK, BK><<<tiles(64, 64), 256, 0, s>>>(p);
+      break;
+    case kFew:
+      if constexpr (EPI) {
+        const unsigned n = (p.N + 63) / 64 * pl.splits;
+        if (p.M <= 16)
+          k_product_few<T, 1><<<n, kFewWaves * 64, 0, s>>>(p, pl.splits, part);
+        else
+          k_product_few<T, 2><<<n, kFewWaves * 64, 0, s>>>(p, pl.splits, part);
+      }
+      break;
+    case kTile128:
+      k_product<T, EPI, AK, BK, 128, 128><<<tiles(128, 128) * pl.splits, 256, 0, s>>>(p, pl.splits, part);
+      break;
+    case kTile256:
+      k_product<T, EPI, AK, BK, 256, 256><<<tiles(256, 256), 256, 0, s>>>(p, 1, part);
+      break;
+  }
+  if (pl.splits > 1)
+    k_product_join<T, EPI><<<(unsigned)(((int64_t)p.M * p.N / 4 + 255) / 256), 256, 0, s>>>(p, pl.splits, part);
+}
+
+Product forward_product(const LinearArgs& a) {
   Product p = {};
   p.M = a.M, p.N = a.N, p.K = a.K;
   p.a = {a.x, a.xs, 1};
   p.b = {a.w, 1, a.ws};
   p.c = a.y, p.cs = a.ys;
   p.act = a.act, p.bias = a.bias, p.res = a.res, p.rs = a.rs, p.z = a.z, p.zs = a.zs;
-  product<T, true, true, false>(p, s);
+  return p;
 }
-
 int64_t dz_row(const LinearArgs& a) { return ((int64_t)a.N + 7) / 8 * 8; }
 int64_t dz_bytes(const LinearArgs& a) {  // dz, where it is not dy itself
   return a.act == kNone ? 0 : ((int64_t)a.M * dz_row(a) * 2 + 15) / 16 * 16;
+}
+int64_t db_bytes(const LinearArgs& a) { return ((int64_t)((a.M + 63) / 64) * a.N * 4 + 15) / 16 * 16; }
+Product dx_product(const LinearArgs& a, const void* dz, int64_t dzs) {  // [M][K], over N
+  Product p = {};
+  p.M = a.M, p.N = a.K, p.K = a.N;
+  p.a = {dz, dzs, 1};
+  p.b = {a.w, a.ws, 1};
+  p.c = a.dx, p.cs = a.dxs;
+  return p;
+}
+Product dw_product(const LinearArgs& a, const void* dz, int64_t dzs) {  // [K][N], over M
+  Product p = {};
+  p.M = a.K, p.N = a.N, p.K = a.M;
+  p.a = {a.x, 1, a.xs};
+  p.b = {dz, 1, dzs};
+  p.c = a.dw, p.cs = a.dws;
+  return p;
+}
+
+template <class T>
+void forward(const LinearArgs& a, void* ws, hipStream_t s) {
+  const Product p = forward_product(a);
+  product<T, true, true, false>(p, plan_of(p.M, p.N, p.K, a.vec && fast_strides(p, true, false), true),
+                                (float*)ws, s);
 }
 
 template <class T>
@@ -217,6 +630,7 @@ void backward(const LinearArgs& a, void* ws, hipStream_t s) {
   const void* dz = a.act == kNone ? a.dy : ws;
   const int64_t dzs = a.act == kNone ? a.dys : dz_row(a);
   float* part = a.db ? (float*)((char*)ws + dz_bytes(a)) : nullptr;
+  float* sums = (float*)((char*)ws + dz_bytes(a) + db_bytes(a));
   if (blocks && (a.act != kNone || a.db)) {
     const int64_t n = (int64_t)blocks * ((a.N + 255) / 256);
     if (a.vec)
@@ -225,27 +639,22 @@ void backward(const LinearArgs& a, void* ws, hipStream_t s) {
       k_linear_dz<T, false><<<(unsigned)n, 256, 0, s>>>(a, (uint16_t*)ws, dzs, part);
   }
   if (a.db) k_linear_db<T><<<(a.N + 63) / 64, 256, 0, s>>>(part, blocks, a.N, (typename T::E*)a.db);
-  if (a.dx) {  // [M][K], over N
-    Product p = {};
-    p.M = a.M, p.N = a.K, p.K = a.N;
-    p.a = {dz, dzs, 1};
-    p.b = {a.w, a.ws, 1};
-    p.c = a.dx, p.cs = a.dxs;
-    product<T, false, true, true>(p, s);
+  if (a.dx) {
+    const Product p = dx_product(a, dz, dzs);
+    product<T, false, true, true>(p, plan_of(p.M, p.N, p.K, a.vec && fast_strides(p, true, true), false), sums, s);
   }
-  if (a.dw) {  // [K][N], over M
-    Product p = {};
-    p.M = a.K, p.N = a.N, p.K = a.M;
-    p.a = {a.x, 1, a.xs};
-    p.b = {dz, 1, dzs};
-    p.c = a.dw, p.cs = a.dws;
-    product<T, false, false, false>(p, s);
+  if (a.dw) {
+    const Product p = dw_product(a, dz, dzs);
+    product<T, false, false, false>(p, plan_of(p.M, p.N, p.K, a.vec && fast_strides(p, false, false), false), sums, s);
   }
 }
 
 }  // namespace
 
-int64_t linear_fwd_bytes(const LinearArgs& a) { return 0; }
+// The workspace is the same whatever the tensors' alignment.
+int64_t linear_fwd_bytes(const LinearArgs& a) {
+  return plan_bytes(plan_of(a.M, a.N, a.K, true, true), a.M, a.N);
+}
 
 hipError_t launch_linear_fwd(const LinearArgs& a, void* ws, hipStream_t s) {
   a.dtype == kF16 ? forward<F16>(a, ws, s) : forward<BF16>(a, ws, s);
@@ -253,7 +662,8 @@ hipError_t launch_linear_fwd(const LinearArgs& a, void* ws, hipStream_t s) {
 }
 
 int64_t linear_bwd_bytes(const LinearArgs& a) {
-  return dz_bytes(a) + (int64_t)((a.M + 63) / 64) * a.N * 4;
+  return dz_bytes(a) + db_bytes(a) + std::max(plan_bytes(plan_of(a.M, a.K, a.N, true, false), a.M, a.K),
+                                              plan_bytes(plan_of(a.K, a.N, a.M, true, false), a.K, a.N));
 }
 
 hipError_t launch_linear_bwd(const LinearArgs& a, void* ws, hipStream_t s) {
