@@ -2,9 +2,9 @@
 // keys j, a_ij = scale q_i . k_j, for queries and keys of different lengths.
 //
 // The query heads that share a kv head are rows of one product: row r of kv head
-// g is query row r / G, head g G + r % G.  A wavefront owns 32 rows, a workgroup
-// NW wavefronts' rows and one pass over tiles of 64 keys with the running
-// maximum m and sum l of each row's softmax:
+// g is query row r / G, head g G + r % G.  A wavefront holds 32 rows and passes
+// over tiles of 64 keys with the running maximum m and sum l of each row's
+// softmax:
 //   S^T = K Q^T     (A = keys from LDS, B = the rows' queries, in registers)
 //   P = exp2(c S - m), l += sum P
 //   O^T += V^T P^T  (A = values by transposed LDS reads, B = P)
@@ -12,107 +12,50 @@
 // in two lanes (l and l + 32): the softmax needs one exchange a tile, and P is
 // the second product's B operand as it stands -- lane half h holds keys
 // 8 i + 4 h + 0..3, an order of the contraction that the value reads follow.
+//
+// Keys and values go from memory to LDS by loads that write LDS themselves.  A
+// key that may not be read (past its length, masked) and the elements past the
+// head's width are zeros there: its lanes take an offset beyond the descriptor's
+// bound, so that what such a place holds never enters a product.
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
 
-#include "layers_internal.h"
+#include "attention_common.h"
 
 namespace pnerf {
 namespace {
 
-constexpr int kBN = 64;  // keys of a tile
+// The softmax state and sums of a lane's row.
+template <class T, int DP>
+struct Rows {
+  uint4 qf[DP / 16];
+  floatx16 o[DP / 32];
+  float m, l;
 
-// Position of 16-byte chunk c of row r in a tile row of CH chunks: a rotation
-// of the row's low bits is xored in, so that 8 rows at one chunk (the 16-byte
-// reads) and 4 rows at two adjacent chunks (the transposed reads) each cover
-// all the banks.
-template <int CH>
-__device__ __forceinline__ int swz(int r, int c) {
-  return r * CH + (c ^ (((r & 3) << 1) | ((r >> 2) & 1)));
-}
-
-template <class T, int DP, int NW, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(NW * 64) void k_attn_fwd(const AttnArgs a) {
-  constexpr int CH = DP / 8, NT = NW * 64, NS = DP / 16, ND = DP / 32;
-  constexpr int NL = kBN * CH / NT;  // 16-byte chunks per thread of a K or V tile
-  __shared__ uint4 sk[kBN * CH], sv[kBN * CH];
-
-  const int tiles_m = (a.M + NW * 32 - 1) / (NW * 32);
-  int id = xcd_order(blockIdx.x, gridDim.x);
-  const int mt = id % tiles_m;
-  id /= tiles_m;
-  const int sp = SPLIT ? id % a.splits : 0;
-  if (SPLIT) id /= a.splits;
-  const int g = id % a.Hkv, b = id / a.Hkv;
-
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int r = lane & 31, h = lane >> 5;
-  const int row = mt * NW * 32 + wave * 32 + r;
-  const int qi = row / a.G, head = g * a.G + row % a.G;
-  const int nq = a.q_len ? min(max(a.q_len[b], 0), a.Sq) : a.Sq;
-  const int nk = a.kv_len ? min(max(a.kv_len[b], 0), a.Sk) : a.Sk;
-  const bool ok = row < a.M && qi < nq;
-
-  // this part's tiles
-  int t0 = 0, t1 = (nk + kBN - 1) / kBN;
-  if (SPLIT) {
-    const int per = (t1 + a.splits - 1) / a.splits;
-    t0 = min(sp * per, t1);
-    t1 = min(t0 + per, t1);
-  }
-  if ((mt * NW * 32) / a.G >= nq) t1 = t0;  // no row of this workgroup is valid
-
-  const uint16_t* qp = (const uint16_t*)a.q + b * a.qs[0] + (int64_t)qi * a.qs[1] + head * a.qs[2];
-  const uint16_t* kp = (const uint16_t*)a.k + b * a.ks[0] + g * a.ks[2];
-  const uint16_t* vp = (const uint16_t*)a.v + b * a.vs[0] + g * a.vs[2];
-  const uint8_t* mp = a.mask ? a.mask + b * a.mask_stride : nullptr;
-
-  uint4 qf[NS];
+  template <bool VEC>
+  __device__ __forceinline__ void init(const uint16_t* q, bool ok, int D, int h) {
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const int d = 16 * s + 8 * h;
-    qf[s] = load8<VEC>(qp + d, ok ? min(a.D - d, 8) : 0);
+    for (int s = 0; s < DP / 16; ++s) {
+      const int d = 16 * s + 8 * h;
+      qf[s] = load8<VEC>(q + d, ok ? min(D - d, 8) : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) o[i] = floatx16{};
+    m = -INFINITY, l = 0.0f;
   }
 
-  floatx16 o[ND];
-#pragma unroll
-  for (int i = 0; i < ND; ++i) o[i] = floatx16{};
-  float m = -INFINITY, l = 0.0f;
-
-  uint4 rk[NL], rv[NL];
-  bool allowed = false;  // key `lane` of the staged tile
-  auto fetch = [&](int t) {
-    const int j = t * kBN + lane;
-    allowed = j < nk && (!mp || mp[j]);
-#pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int e = tid + n * NT, jr = t * kBN + e / CH, d = 8 * (e % CH);
-      const int cnt = jr < nk ? min(a.D - d, 8) : 0;
-      rk[n] = load8<VEC>(kp + (int64_t)jr * a.ks[1] + d, cnt);
-      rv[n] = load8<VEC>(vp + (int64_t)jr * a.vs[1] + d, cnt);
-    }
-  };
-  if (t0 < t1) fetch(t0);
-
-  for (int t = t0; t < t1; ++t) {
-    const uint64_t vm = __ballot(allowed);
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int e = tid + n * NT, kr = e / CH, at = swz<CH>(kr, e % CH);
-      const bool on = (vm >> kr) & 1;  // what a masked key or value holds never enters a product
-      sk[at] = on ? rk[n] : make_uint4(0, 0, 0, 0);
-      sv[at] = on ? rv[n] : make_uint4(0, 0, 0, 0);
-    }
-    __syncthreads();
-    if (t + 1 < t1) fetch(t + 1);
-
+  // One tile; vm: its keys that may be read; before_values runs between the two products.
+  template <class F>
+  __device__ __forceinline__ void tile(const uint4* sk, const uint4* sv, uint64_t vm, float c, int lane,
+                                       F before_values) {
+    constexpr int CH = DP / 8;
+    const int r = lane & 31, h = lane >> 5;
     floatx16 s[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       s[n] = floatx16{};
 #pragma unroll
-      for (int i = 0; i < NS; ++i) s[n] = T::mma(sk[swz<CH>(32 * n + r, 2 * i + h)], qf[i], s[n]);
+      for (int i = 0; i < DP / 16; ++i) s[n] = T::mma(sk[swz<CH>(32 * n + r, 2 * i + h)], qf[i], s[n]);
     }
     if (vm != ~0ull) {
 #pragma unroll
@@ -123,6 +66,7 @@ __global__ __launch_bounds__(NW * 64) void k_attn_fwd(const AttnArgs a) {
           if (!((w >> (8 * (i / 4) + i % 4)) & 1)) s[n][i] = -INFINITY;
       }
     }
+    before_values();
     float mx = -INFINITY;
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -130,80 +74,230 @@ __global__ __launch_bounds__(NW * 64) void k_attn_fwd(const AttnArgs a) {
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
     float m0, m1;
     halves(mx, m0, m1);
-    const float mn = fmaxf(m, a.c * fmaxf(m0, m1));
-    const float base = mn == -INFINITY ? 0.0f : mn;  // no allowed key yet
-    const float alpha = __builtin_amdgcn_exp2f(m - base);
-    m = mn;
-    l *= alpha;
+    const float mn = fmaxf(m, c * fmaxf(m0, m1));
+    if (__any(mn > m)) {  // some row's maximum has grown
+      const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+      m = mn;
+      l *= alpha;
 #pragma unroll
-    for (int i = 0; i < ND; ++i) o[i] *= alpha;
+      for (int i = 0; i < DP / 32; ++i) o[i] *= alpha;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;  // no allowed key yet
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], a.c, -base));
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
         l += s[n][i];
       }
 #pragma unroll
     for (int n = 0; n < 4; ++n) {  // 16 keys each
-      const floatx16& p = s[n / 2];
-      const int i0 = 8 * (n % 2);
-      const uint4 pf = make_uint4(T::pack(p[i0], p[i0 + 1]), T::pack(p[i0 + 2], p[i0 + 3]),
-                                  T::pack(p[i0 + 4], p[i0 + 5]), T::pack(p[i0 + 6], p[i0 + 7]));
+      const uint4 pf = pack8<T>(s[n / 2], 8 * (n % 2));
 #pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const int l16 = lane & 15, kr = 16 * n + 4 * h + l16 / 4;
-        const int col = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (l16 % 4);
-        const char* lo = (const char*)(sv + swz<CH>(kr, col / 8)) + 2 * (col % 8);
-        const char* hi = (const char*)(sv + swz<CH>(kr + 8, col / 8)) + 2 * (col % 8);
-        const uint2 v0 = read_tr(lo), v1 = read_tr(hi);
-        o[d] = T::mma(make_uint4(v0.x, v0.y, v1.x, v1.y), pf, o[d]);
-      }
+      for (int d = 0; d < DP / 32; ++d) o[d] = T::mma(tr_frag<CH>(sv, 16 * n, 32 * d, lane), pf, o[d]);
     }
   }
 
-  float l0, l1;
-  halves(l, l0, l1);
-  l = l0 + l1;
-  if (!ok) {  // past q_len, beside rows that are not
-    m = -INFINITY, l = 0.0f;
+  // The row's sum of both halves; nothing where the row is not to be computed.
+  __device__ __forceinline__ void close(bool ok) {
+    float l0, l1;
+    halves(l, l0, l1);
+    l = l0 + l1;
+    if (!ok) {  // past q_len, beside rows that are not
+      m = -INFINITY, l = 0.0f;
 #pragma unroll
-    for (int i = 0; i < ND; ++i) o[i] = floatx16{};
+      for (int i = 0; i < DP / 32; ++i) o[i] = floatx16{};
+    }
   }
-  if (SPLIT) {
-    if (row >= a.M) return;
+
+  __device__ __forceinline__ void store_partial(const AttnArgs& a, int sp, int64_t at, int h, bool some) const {
     const int64_t rows = (int64_t)a.B * a.Hkv * a.M;
-    const int64_t at = ((int64_t)b * a.Hkv + g) * a.M + row;
-    if (h == 0) {
-      floatx2* ml = reinterpret_cast<floatx2*>(a.part + (int64_t)a.splits * rows * DP);
-      ml[sp * rows + at] = floatx2{m, l};
-    }
-    if (t0 == t1) return;  // the join does not read an empty part's sums
-    float* po = a.part + (sp * rows + at) * DP;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<floatx4*>(po + 32 * d + 8 * i + 4 * h) =
-            floatx4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-    return;
+    if (h == 0)
+      reinterpret_cast<floatx2*>(a.part + (int64_t)a.splits * rows * DP)[sp * rows + at] = floatx2{m, l};
+    if (some) store_part<DP>(o, a.part + (sp * rows + at) * DP, h);  // the join reads no empty part's sums
   }
-  if (row >= a.M) return;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  uint16_t* op = (uint16_t*)a.o + b * a.os[0] + (int64_t)qi * a.os[1] + head * a.os[2];
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int col = 32 * d + 8 * i + 4 * h;
-      const floatx16& x = o[d];
-      store4<VEC>(op + col, make_uint2(T::pack(x[4 * i] * inv, x[4 * i + 1] * inv),
-                                       T::pack(x[4 * i + 2] * inv, x[4 * i + 3] * inv)),
-                  min(a.D - col, 4));
+  template <bool VEC>
+  __device__ __forceinline__ void store(const AttnArgs& a, int b, int qi, int head, int h) const {
+    uint16_t* op = (uint16_t*)a.o + b * a.os[0] + (int64_t)qi * a.os[1] + head * a.os[2];
+    store_cols<T, DP, VEC>(o, op, l == 0.0f ? 0.0f : 1.0f / l, a.D, h);
+    if (a.lse && h == 0) a.lse[((int64_t)b * a.Hq + head) * a.Sq + qi] = log_sum(m, l);
+  }
+};
+
+// Which part of the keys, rows and heads a workgroup takes, and a lane's row.
+struct Place {
+  int b, g, sp, t0, t1, row, qi, head, nk;
+  bool ok;
+  const uint16_t* q;
+  const uint8_t* mask;
+  __device__ __forceinline__ Place(const AttnArgs& a, int rows_wg, int row_in) {
+    const int tiles_m = (a.M + rows_wg - 1) / rows_wg;
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int mt = id % tiles_m;
+    id /= tiles_m;
+    sp = id % a.splits;
+    id /= a.splits;
+    g = id % a.Hkv, b = id / a.Hkv;
+    row = mt * rows_wg + row_in;
+    qi = row / a.G, head = g * a.G + row % a.G;
+    const int nq = clamp_len(a.q_len, b, a.Sq);
+    nk = clamp_len(a.kv_len, b, a.Sk);
+    ok = row < a.M && qi < nq;
+    const int all = (nk + kBN - 1) / kBN, per = (all + a.splits - 1) / a.splits;
+    t0 = min(sp * per, all);
+    t1 = min(t0 + per, all);
+    if ((mt * rows_wg) / a.G >= nq) t1 = t0;  // no row of this workgroup is valid
+    q = (const uint16_t*)a.q + b * a.qs[0] + (int64_t)qi * a.qs[1] + head * a.qs[2];
+    mask = a.mask ? a.mask + b * a.mask_stride : nullptr;
+  }
+  __device__ __forceinline__ bool allowed(int j) const { return j < nk && (!mask || mask[j]); }
+};
+
+// Many rows: four wavefronts of 32 rows share the tiles, two of them in LDS: the
+// loads of the next run while the products of one do.  One barrier a tile.
+template <class T, int DP>
+__global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
+  using Tile = KVTile<DP, 4>;
+  __shared__ uint4 lds[2][2 * Tile::kPieces];  // keys, then values
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const Place at(a, 128, wave * 32 + (lane & 31));
+  Tile kt(a.k, a.ks, at.b, at.g, a.D, wave, lane), vt(a.v, a.vs, at.b, at.g, a.D, wave, lane);
+  Rows<T, DP> x;
+  x.template init<true>(at.q, at.ok, a.D, h);
+  const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[1])};
+  auto load = [&](int t, uint64_t vm) {
+    kt.load(to[t & 1], t, at.nk, vm, lane);
+    vt.load(to[t & 1] + 16 * Tile::kPieces, t, at.nk, vm, lane);
+  };
+  uint64_t vm = 0, vm_next = 0;
+  bool allowed = false;  // key `lane` of the tile after the next
+  if (at.t0 < at.t1) {
+    vm_next = __ballot(at.allowed(at.t0 * kBN + lane));
+    load(at.t0, vm_next);
+    allowed = at.allowed((at.t0 + 1) * kBN + lane);
+  }
+  for (int t = at.t0; t < at.t1; ++t) {
+    wait_loads();
+    __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
+    vm = vm_next;
+    vm_next = __ballot(allowed);
+    if (t + 1 < at.t1) {
+      load(t + 1, vm_next);
+      allowed = at.allowed((t + 2) * kBN + lane);
     }
-  if (a.lse && h == 0)
-    a.lse[((int64_t)b * a.Hq + head) * a.Sq + qi] =
-        l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    x.tile(lds[t & 1], lds[t & 1] + Tile::kPieces, vm, a.c, lane, [] {});
+  }
+  x.close(at.ok);
+  if (at.row >= a.M) return;
+  if (a.splits > 1)
+    x.store_partial(a, at.sp, ((int64_t)at.b * a.Hkv + at.g) * a.M + at.row, h, at.t0 < at.t1);
+  else
+    x.template store<true>(a, at.b, at.qi, at.head, h);
+}
+
+// At most 32 rows of a kv head (single tokens): the bytes of the states are the
+// time.  Four wavefronts with the same rows take the tiles in turn, each with its
+// own keys and values in LDS and no barrier; keys are loaded again as soon as the
+// scores are there, values as soon as they have been used.  At the end the
+// wavefronts' sums meet in LDS.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_attn_few(const AttnArgs a) {
+  using Tile = KVTile<DP, 1>;
+  __shared__ uint4 lds[4][2 * Tile::kPieces];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const Place at(a, 32, lane & 31);
+  Tile kt(a.k, a.ks, at.b, at.g, a.D, 0, lane), vt(a.v, a.vs, at.b, at.g, a.D, 0, lane);
+  Rows<T, DP> x;
+  x.template init<true>(at.q, at.ok, a.D, h);
+  uint4 *sk = lds[wave], *sv = sk + Tile::kPieces;
+  const uint32_t to_k = lds_address(sk), to_v = lds_address(sv);
+  int t = at.t0 + wave;
+  uint64_t vm = 0;
+  bool allowed = false;
+  if (t < at.t1) {
+    vm = __ballot(at.allowed(t * kBN + lane));
+    kt.load(to_k, t, at.nk, vm, lane);
+    vt.load(to_v, t, at.nk, vm, lane);
+    allowed = at.allowed((t + 4) * kBN + lane);
+  }
+  for (; t < at.t1; t += 4) {
+    wait_loads();
+    const uint64_t vm_next = __ballot(allowed);
+    const bool more = t + 4 < at.t1;
+    x.tile(sk, sv, vm, a.c, lane, [&] {
+      wait_reads();
+      if (more) {
+        kt.load(to_k, t + 4, at.nk, vm_next, lane);
+        allowed = at.allowed((t + 8) * kBN + lane);
+      }
+    });
+    wait_reads();
+    if (more) vt.load(to_v, t + 4, at.nk, vm_next, lane);
+    vm = vm_next;
+  }
+
+  // the wavefronts' sums at the largest of their maxima
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(lds);
+  static_assert(4 * 32 * (DP + 4) * 4 + 4 * 64 * 4 <= sizeof(lds), "the sums fit the tiles' LDS");
+  floatx2* red_ml = reinterpret_cast<floatx2*>(red + 4 * 32 * (DP + 4));
+  x.close(at.ok);
+  if (h == 0) red_ml[wave * 32 + lane] = floatx2{x.m, x.l};
+  store_part<DP>(x.o, red + (wave * 32 + (lane & 31)) * (DP + 4), h);
+  __syncthreads();
+  constexpr int kLanes = DP / 4;  // of a row, 4 elements each
+  for (int r = threadIdx.x / kLanes; r < min(a.M, 32); r += 256 / kLanes) {
+    const int d = 4 * (threadIdx.x % kLanes);
+    float m = -INFINITY, l = 0.0f;
+    floatx4 o = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, red_ml[w * 32 + r][0]);
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const floatx2 v = red_ml[w * 32 + r];
+      const float f = __builtin_amdgcn_exp2f(v[0] - base);
+      l += f * v[1];
+      o += f * *reinterpret_cast<const floatx4*>(red + (w * 32 + r) * (DP + 4) + d);
+    }
+    const int64_t rows = (int64_t)a.B * a.Hkv * a.M, row = ((int64_t)at.b * a.Hkv + at.g) * a.M + r;
+    if (a.splits > 1) {
+      if (d == 0)
+        reinterpret_cast<floatx2*>(a.part + (int64_t)a.splits * rows * DP)[at.sp * rows + row] = floatx2{m, l};
+      *reinterpret_cast<floatx4*>(a.part + (at.sp * rows + row) * DP + d) = o;
+    } else {
+      const int qi = r / a.G, head = at.g * a.G + r % a.G;
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      store4<true>((uint16_t*)a.o + at.b * a.os[0] + (int64_t)qi * a.os[1] + head * a.os[2] + d,
+                   make_uint2(T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)), a.D - d);
+      if (a.lse && d == 0) a.lse[((int64_t)at.b * a.Hq + head) * a.Sq + qi] = log_sum(m, l);
+    }
+  }
+}
+
+// Any strides, alignment and head width: as k_attn_fwd, the tiles by way of
+// registers, element by element.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_attn_any(const AttnArgs a) {
+  __shared__ uint4 sk[kBN * DP / 8], sv[kBN * DP / 8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const Place at(a, 128, wave * 32 + (lane & 31));
+  Rows<T, DP> x;
+  x.template init<false>(at.q, at.ok, a.D, h);
+  for (int t = at.t0; t < at.t1; ++t) {
+    const uint64_t vm = __ballot(at.allowed(t * kBN + lane));
+    __syncthreads();
+    copy_tile<DP>(sk, a.k, a.ks, at.b, at.g, a.D, t, vm);
+    copy_tile<DP>(sv, a.v, a.vs, at.b, at.g, a.D, t, vm);
+    __syncthreads();
+    x.tile(sk, sv, vm, a.c, lane, [] {});
+  }
+  x.close(at.ok);
+  if (at.row >= a.M) return;
+  if (a.splits > 1)
+    x.store_partial(a, at.sp, ((int64_t)at.b * a.Hkv + at.g) * a.M + at.row, h, at.t0 < at.t1);
+  else
+    x.template store<false>(a, at.b, at.qi, at.head, h);
 }
 
 // Joins the parts of the key axis, a workgroup per row: the parts' sums meet at
@@ -246,45 +340,35 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
     for (int i = 0; i < NG; ++i) x += red[i][d];
     op[d] = (typename T::E)(x * inv);
   }
-  if (a.lse && threadIdx.x == 0)
-    a.lse[((int64_t)b * a.Hq + head) * a.Sq + qi] =
-        l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  if (a.lse && threadIdx.x == 0) a.lse[((int64_t)b * a.Hq + head) * a.Sq + qi] = log_sum(m, l);
 }
 
-int padded(int D) { return D <= 64 ? 64 : 128; }
-int waves(const AttnArgs& a) { return a.M <= 32 ? 1 : 4; }
-
-template <class T, int DP, int NW, bool VEC>
+template <class T, int DP>
 void launch(const AttnArgs& a, hipStream_t s) {
-  const int tiles = (a.M + NW * 32 - 1) / (NW * 32);
-  const int64_t n = (int64_t)tiles * a.splits * a.Hkv * a.B;
-  if (a.splits > 1)
-    k_attn_fwd<T, DP, NW, VEC, true><<<(unsigned)n, NW * 64, 0, s>>>(a);
+  const bool few = a.M <= 32;
+  const int rows = few ? 32 : 128;
+  const unsigned n = (unsigned)((int64_t)((a.M + rows - 1) / rows) * a.splits * a.Hkv * a.B);
+  if (!fast_loads(a))
+    k_attn_any<T, DP><<<n, 256, 0, s>>>(a);
+  else if (few)
+    k_attn_few<T, DP><<<n, 256, 0, s>>>(a);
   else
-    k_attn_fwd<T, DP, NW, VEC, false><<<(unsigned)n, NW * 64, 0, s>>>(a);
+    k_attn_fwd<T, DP><<<n, 256, 0, s>>>(a);
   if (a.splits > 1) k_attn_join<T, DP><<<(unsigned)(a.B * a.Hkv * a.M), 256, 0, s>>>(a);
-}
-
-template <class T>
-void launch_t(const AttnArgs& a, hipStream_t s) {
-  const bool wide = padded(a.D) == 128, many = waves(a) > 1;
-  if (wide && many) a.vec ? launch<T, 128, 4, true>(a, s) : launch<T, 128, 4, false>(a, s);
-  if (wide && !many) a.vec ? launch<T, 128, 1, true>(a, s) : launch<T, 128, 1, false>(a, s);
-  if (!wide && many) a.vec ? launch<T, 64, 4, true>(a, s) : launch<T, 64, 4, false>(a, s);
-  if (!wide && !many) a.vec ? launch<T, 64, 1, true>(a, s) : launch<T, 64, 1, false>(a, s);
 }
 
 }  // namespace
 
-// Few rows leave compute units idle: the keys are then cut into parts, so that
-// the chip's resident workgroups are all busy, of at least 4 tiles each.
+// Few workgroups leave compute units idle: where there are not enough for half of
+// them, the keys are cut into parts, of at least 4 tiles (16 for few rows, where
+// 4 wavefronts share a part) each.
 int attn_fwd_splits(const AttnArgs& a) {
-  const int nw = waves(a);
-  const int64_t wgs = (int64_t)((a.M + nw * 32 - 1) / (nw * 32)) * a.Hkv * a.B;
-  const int64_t target = nw == 1 ? 4 * kCUs : 2 * kCUs;
+  const bool few = a.M <= 32;
+  const int rows = few ? 32 : 128;
+  const int64_t wgs = (int64_t)((a.M + rows - 1) / rows) * a.Hkv * a.B;
   const int64_t tiles = (a.Sk + kBN - 1) / kBN;
   if (wgs == 0) return 1;
-  return (int)std::max<int64_t>(1, std::min(target / wgs, tiles / 4));
+  return (int)std::max<int64_t>(1, std::min(kCUs / wgs, tiles / (few ? 16 : 4)));
 }
 
 int64_t attn_fwd_bytes(const AttnArgs& a) {
@@ -296,7 +380,11 @@ hipError_t launch_attn_fwd(const AttnArgs& a0, void* ws, hipStream_t s) {
   AttnArgs a = a0;
   a.part = (float*)ws;
   if (a.B == 0 || a.M == 0) return hipSuccess;
-  a.dtype == kF16 ? launch_t<F16>(a, s) : launch_t<BF16>(a, s);
+  const bool wide = padded(a.D) == 128;
+  if (a.dtype == kF16)
+    wide ? launch<F16, 128>(a, s) : launch<F16, 64>(a, s);
+  else
+    wide ? launch<BF16, 128>(a, s) : launch<BF16, 64>(a, s);
   return hipGetLastError();
 }
 

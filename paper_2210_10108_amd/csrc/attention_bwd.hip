@@ -12,39 +12,12 @@
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
 
-#include "layers_internal.h"
+#include "attention_common.h"
 
 namespace pnerf {
 namespace {
 
-constexpr int kBN = 64;      // keys of a tile of the dq pass, rows of one of the dk, dv pass
 constexpr int kKeys = 128;   // keys of a workgroup of the dk, dv pass: 32 a wavefront
-
-template <int CH>
-__device__ __forceinline__ int swz(int r, int c) {  // see attention.hip
-  return r * CH + (c ^ (((r & 3) << 1) | ((r >> 2) & 1)));
-}
-
-__device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
-  return len ? min(max(len[b], 0), most) : most;
-}
-
-// A operand of 32 columns x 16 rows, transposed from a tile in LDS: rows row0 +
-// 4 h + 0..3 and + 8, columns col0 + lane % 32 (the order of a result's registers).
-template <int CH>
-__device__ __forceinline__ uint4 tr_frag(const uint4* tile, int row0, int col0, int lane) {
-  const int l16 = lane & 15, r = row0 + 4 * (lane >> 5) + l16 / 4;
-  const int col = col0 + 16 * ((lane >> 4) & 1) + 4 * (l16 % 4);
-  const uint2 a = read_tr((const char*)(tile + swz<CH>(r, col / 8)) + 2 * (col % 8));
-  const uint2 b = read_tr((const char*)(tile + swz<CH>(r + 8, col / 8)) + 2 * (col % 8));
-  return make_uint4(a.x, a.y, b.x, b.y);
-}
-
-template <class T>
-__device__ __forceinline__ uint4 pack8(const floatx16& p, int i) {
-  return make_uint4(T::pack(p[i], p[i + 1]), T::pack(p[i + 2], p[i + 3]),
-                    T::pack(p[i + 4], p[i + 5]), T::pack(p[i + 6], p[i + 7]));
-}
 
 // (lse / ln 2 - shift, delta) of every row; (+inf, 0) where the row has no
 // allowed key or is past q_len, which makes all of its p zero.
@@ -74,31 +47,6 @@ __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
       reinterpret_cast<floatx2*>(a.delta)[at] =
           ok ? floatx2{lse * 1.4426950408889634f - (float)a.shift, sum} : floatx2{INFINITY, 0.0f};
   }
-}
-
-// Results of a wavefront, transposed (column = row or key of the lane), to
-// memory: 16-bit elements times f, or 32-bit partial sums.
-template <class T, int DP, bool VEC>
-__device__ __forceinline__ void store_cols(const floatx16* acc, uint16_t* p, float f, int D, int h) {
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int col = 32 * d + 8 * i + 4 * h;
-      const floatx16& x = acc[d];
-      store4<VEC>(p + col, make_uint2(T::pack(x[4 * i] * f, x[4 * i + 1] * f),
-                                      T::pack(x[4 * i + 2] * f, x[4 * i + 3] * f)),
-                  min(D - col, 4));
-    }
-}
-template <int DP>
-__device__ __forceinline__ void store_part(const floatx16* acc, float* p, int h) {
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<floatx4*>(p + 32 * d + 8 * i + 4 * h) =
-          floatx4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
 }
 
 template <class T, int DP, int NW, bool VEC>
@@ -366,8 +314,6 @@ __global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a, int splits, 
     out = (typename T::E*)a.dk + b * a.dks[0] + at * a.dks[1] + g * a.dks[2];
   out[d] = (typename T::E)(x * f);
 }
-
-int padded(int D) { return D <= 64 ? 64 : 128; }
 
 // Parts of the contracted axis, so that the chip is busy also where one axis is
 // short: of at least 4 tiles each.

@@ -1,0 +1,121 @@
+// What the attention kernels share: tiles of keys and values in LDS, fragments,
+// results.
+#pragma once
+#include "layers_internal.h"
+
+namespace pnerf {
+
+constexpr int kBN = 64;                          // keys of a tile
+constexpr int64_t kMaxTileStride = 1 << 22;      // elements: a tile's offsets stay below 2^31 bytes
+
+inline int padded(int D) { return D <= 64 ? 64 : 128; }  // head width in the kernels
+// Whether tiles can go to LDS by 16-byte loads with 32-bit offsets.
+inline bool fast_loads(const AttnArgs& a) {
+  return a.vec && a.ks[1] <= kMaxTileStride && a.vs[1] <= kMaxTileStride;
+}
+
+#if defined(__HIP_DEVICE_COMPILE__) || defined(PNERF_LAYERS_DEVICE)
+// The bits of row r that are xored into the position of its 16-byte chunks: 8
+// rows at one chunk (the 16-byte reads) and 4 rows at two adjacent chunks (the
+// transposed reads) each cover all the banks.
+__device__ __forceinline__ int swz_bits(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+// Position of chunk c of row r in a tile of CH chunks a row.
+template <int CH>
+__device__ __forceinline__ int swz(int r, int c) {
+  return r * CH + (c ^ swz_bits(r));
+}
+
+__device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
+  return len ? min(max(len[b], 0), most) : most;
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// The loads of one kv head's tiles into LDS, by NW wavefronts.
+template <int DP, int NW>
+struct KVTile {
+  static constexpr int kPieces = kBN * DP / 8;         // 16-byte chunks of a tile
+  static constexpr int kLoads = kPieces / 64 / NW;     // of a wavefront
+  static constexpr int kRows = 64 / (DP / 8);          // rows of one
+  const char* base;
+  int64_t row_bytes;
+  int wave, D;
+  __device__ __forceinline__ KVTile(const void* p, const int64_t s[3], int b, int g, int D_, int wave_, int lane)
+      : base((const char*)p + 2 * (b * s[0] + g * s[2])), row_bytes(2 * s[1]), wave(wave_), D(D_) {}
+  // Tile t, whose keys that may be read are vm, to LDS at lds.
+  __device__ __forceinline__ void load(uint32_t lds, int t, int n_rows, uint64_t vm, int lane) const {
+    const u32x4 desc = descriptor(base + (int64_t)t * kBN * row_bytes,
+                                  (int64_t)(n_rows - t * kBN - 1) * row_bytes + 2 * D);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int r = (n * NW + wave) * kRows + lane / (DP / 8);
+      const int c = (lane % (DP / 8)) ^ swz_bits(r);
+      const bool on = 8 * c < D && ((vm >> r) & 1);
+      load_to_lds(to + n * NW * 1024, on ? (uint32_t)r * (uint32_t)row_bytes + 16 * c : kOutside, desc);
+    }
+  }
+};
+
+// A tile by way of registers, element by element, 256 threads.
+template <int DP>
+__device__ __forceinline__ void copy_tile(uint4* lds, const void* p, const int64_t s[3], int b, int g, int D,
+                                          int t, uint64_t vm) {
+  constexpr int CH = DP / 8;
+  const uint16_t* base = (const uint16_t*)p + b * s[0] + g * s[2];
+  for (int e = threadIdx.x; e < kBN * CH; e += 256) {
+    const int r = e / CH, d = 8 * (e % CH);
+    const bool on = (vm >> r) & 1;
+    lds[swz<CH>(r, e % CH)] = load8<false>(base + (int64_t)(t * kBN + r) * s[1] + d, on ? min(D - d, 8) : 0);
+  }
+}
+
+// A operand of 32 columns x 16 rows, transposed from a tile in LDS: rows row0 +
+// 4 h + 0..3 and + 8, columns col0 + lane % 32 (the order of a result's registers).
+template <int CH>
+__device__ __forceinline__ uint4 tr_frag(const uint4* tile, int row0, int col0, int lane) {
+  const int l16 = lane & 15, r = row0 + 4 * (lane >> 5) + l16 / 4;
+  const int col = col0 + 16 * ((lane >> 4) & 1) + 4 * (l16 % 4);
+  const uint2 a = read_tr((const char*)(tile + swz<CH>(r, col / 8)) + 2 * (col % 8));
+  const uint2 b = read_tr((const char*)(tile + swz<CH>(r + 8, col / 8)) + 2 * (col % 8));
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
+
+// Registers i .. i + 7 of a result as the B operand of 16 of its rows.
+template <class T>
+__device__ __forceinline__ uint4 pack8(const floatx16& p, int i) {
+  return make_uint4(T::pack(p[i], p[i + 1]), T::pack(p[i + 2], p[i + 3]),
+                    T::pack(p[i + 4], p[i + 5]), T::pack(p[i + 6], p[i + 7]));
+}
+
+// A lane's column of a transposed result to memory: 16-bit elements times f, or
+// 32-bit partial sums.
+template <class T, int DP, bool VEC>
+__device__ __forceinline__ void store_cols(const floatx16* acc, uint16_t* p, float f, int D, int h) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int col = 32 * d + 8 * i + 4 * h;
+      const floatx16& x = acc[d];
+      store4<VEC>(p + col, make_uint2(T::pack(x[4 * i] * f, x[4 * i + 1] * f),
+                                      T::pack(x[4 * i + 2] * f, x[4 * i + 3] * f)),
+                  min(D - col, 4));
+    }
+}
+template <int DP>
+__device__ __forceinline__ void store_part(const floatx16* acc, float* p, int h) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<floatx4*>(p + 32 * d + 8 * i + 4 * h) =
+          floatx4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) {  // m in units of ln 2
+  return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+#endif
+
+}  // namespace pnerf

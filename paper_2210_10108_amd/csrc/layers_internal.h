@@ -164,6 +164,31 @@ __device__ __forceinline__ void halves(float x, float& a, float& b) {
   b = __uint_as_float(r[1]);
 }
 
+// Loads that write LDS themselves: 16 bytes a lane, the lanes' 64 pieces one
+// after the other from `lds` (a byte address, the same in all lanes).  `offset`
+// is each lane's own, against a descriptor's base and bound: past the bound zeros
+// are written, and kOutside is past every bound.  (m0, which holds the address, is
+// no register that the compiler keeps anything in: nothing else here uses it.)
+// The compiler does not see the loads: s_waitcnt is the kernel's own.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr uint32_t kOutside = 0x80000000u;
+__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, u32x4 desc) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(lds), "v"(offset), "s"(desc) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+// Descriptor of `bytes` bytes from base (the same in all lanes), at most 2^31 - 1.
+__device__ __forceinline__ u32x4 descriptor(const void* base, int64_t bytes) {
+  u32x4 d;
+  d[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
+  d[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xFFFFu);
+  d[2] = __builtin_amdgcn_readfirstlane((uint32_t)min(bytes, (int64_t)0x7FFFFFFF));
+  d[3] = 0x00027000u;
+  return d;
+}
+
 // LDS written by lanes of this wavefront may be read by its others from here on
 // (a wavefront's LDS accesses complete in order: this holds the compiler).
 __device__ __forceinline__ void wave_fence() {

@@ -177,25 +177,12 @@ __global__ __launch_bounds__(256) void k_product_any(const Product p) {
 
 // ------------------------------------------------------------ aligned products
 // Rows of 16-byte chunks go from memory to LDS by loads that write LDS
-// themselves, 64 chunks of consecutive LDS a wavefront and instruction; a chunk's
-// place within its row is xored with bits of the row so that the fragment reads
-// cover all banks, which the lanes' addresses in memory follow.  The buffer
-// descriptor's bound gives zeros past the last row; lanes past the end of a row
-// take an offset beyond any bound.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// themselves (load_to_lds); a chunk's place within its row is xored with bits of
+// the row so that the fragment reads cover all banks, which the lanes' addresses
+// in memory follow.  The buffer descriptor's bound gives zeros past the last row;
+// lanes past the end of a row take an offset beyond any bound.
 constexpr int kBK = 64;                      // depth of a tile in LDS
-constexpr uint32_t kOutside = 0x80000000u;   // an offset beyond every descriptor's bound
 constexpr int64_t kMaxFastStride = 1 << 21;  // elements: a tile's offsets stay below 2^31 bytes
-
-// (m0, the destination, is no register that the compiler keeps anything in here:
-// nothing else in these kernels uses it.)
-__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, u32x4 desc) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(lds), "v"(offset), "s"(desc) : "memory");
-}
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
-}
 
 // One operand's tile of ROWS rows (of A, or columns of B) x 64: its loads and
 // its fragments.  KC: the contracted axis is contiguous, an LDS row is a row of
@@ -236,12 +223,7 @@ struct Tile {
   // Loads n0 .. n1 - 1 of the tile, into LDS at lds.
   template <int N0, int N1>
   __device__ __forceinline__ void load(uint32_t lds, int wave) {
-    const int64_t span = (rows - 1) * row_bytes + 2 * inner;
-    u32x4 desc;
-    desc[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
-    desc[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xFFFFu);
-    desc[2] = __builtin_amdgcn_readfirstlane((uint32_t)min(span, (int64_t)0x7FFFFFFF));
-    desc[3] = 0x00027000u;
+    const u32x4 desc = descriptor(base, (rows - 1) * row_bytes + 2 * inner);
     const uint32_t first = 8 * chunk < inner ? off : kOutside;
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
 #pragma unroll
