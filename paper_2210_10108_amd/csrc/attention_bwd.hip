@@ -17,7 +17,7 @@
 namespace pnerf {
 namespace {
 
-constexpr int kKeys = 128;   // keys of a workgroup of the dk, dv pass: 32 a wavefront
+constexpr int kKeys = 128;  // keys of a workgroup of the dk, dv pass: 32 a wavefront
 
 // (lse / ln 2 - shift, delta) of every row; (+inf, 0) where the row has no
 // allowed key or is past q_len, which makes all of its p zero.
@@ -49,28 +49,31 @@ __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
   }
 }
 
-template <class T, int DP, int NW, bool VEC>
-__global__ __launch_bounds__(NW * 64) void k_attn_dq(const AttnArgs a, int splits, float* part) {
-  constexpr int CH = DP / 8, NT = NW * 64, NS = DP / 16, ND = DP / 32;
-  constexpr int NL = kBN * CH / NT;
-  __shared__ uint4 sk[kBN * CH], sv[kBN * CH];
+// dq: four wavefronts of 32 rows share the tiles of keys and values, two of them
+// in LDS (FAST; else one, by way of registers).  As in the forward kernel the row
+// is the column of every product: its lse and delta are a lane's own.
+template <class T, int DP, bool FAST>
+__global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits, float* part) {
+  constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32;
+  using Tile = KVTile<DP, 4>;
+  __shared__ uint4 lds[FAST ? 2 : 1][2 * Tile::kPieces];  // keys, then values
 
-  const int tiles_m = (a.M + NW * 32 - 1) / (NW * 32);
+  const int tiles_m = (a.M + 127) / 128;
   int id = xcd_order(blockIdx.x, gridDim.x);
   const int mt = id % tiles_m;
   id /= tiles_m;
   const int sp = id % splits;
   id /= splits;
   const int g = id % a.Hkv, b = id / a.Hkv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, h = lane >> 5;
-  const int row = mt * NW * 32 + wave * 32 + r;
+  const int row = mt * 128 + wave * 32 + r;
   const int qi = row / a.G, head = g * a.G + row % a.G;
   const int nq = clamp_len(a.q_len, b, a.Sq), nk = clamp_len(a.kv_len, b, a.Sk);
   int t1 = (nk + kBN - 1) / kBN;
   const int per = (t1 + splits - 1) / splits, t0 = min(sp * per, t1);
   t1 = min(t0 + per, t1);
-  if ((mt * NW * 32) / a.G >= nq) t1 = t0;
+  if ((mt * 128) / a.G >= nq) t1 = t0;
 
   const int64_t rows = (int64_t)a.B * a.Hkv * a.M;
   const int64_t at = ((int64_t)b * a.Hkv + g) * a.M + row;
@@ -80,47 +83,51 @@ __global__ __launch_bounds__(NW * 64) void k_attn_dq(const AttnArgs a, int split
 
   const uint16_t* qp = (const uint16_t*)a.q + b * a.qs[0] + (int64_t)qi * a.qs[1] + head * a.qs[2];
   const uint16_t* gp = (const uint16_t*)a.dout + b * a.dos[0] + (int64_t)qi * a.dos[1] + head * a.dos[2];
-  const uint16_t* kp = (const uint16_t*)a.k + b * a.ks[0] + g * a.ks[2];
-  const uint16_t* vp = (const uint16_t*)a.v + b * a.vs[0] + g * a.vs[2];
   const uint8_t* mp = a.mask ? a.mask + b * a.mask_stride : nullptr;
-
+  auto may_read = [&](int j) { return j < nk && (!mp || mp[j]); };
   uint4 qf[NS], gf[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     const int d = 16 * s + 8 * h, n = ok ? min(a.D - d, 8) : 0;
-    qf[s] = load8<VEC>(qp + d, n);
-    gf[s] = load8<VEC>(gp + d, n);
+    qf[s] = load8<FAST>(qp + d, n);
+    gf[s] = load8<FAST>(gp + d, n);
   }
   floatx16 acc[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) acc[i] = floatx16{};
 
-  uint4 rk[NL], rv[NL];
-  bool allowed = false;
-  auto fetch = [&](int t) {
-    const int j = t * kBN + lane;
-    allowed = j < nk && (!mp || mp[j]);
-#pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int e = tid + n * NT, jr = t * kBN + e / CH, d = 8 * (e % CH);
-      const int cnt = jr < nk ? min(a.D - d, 8) : 0;
-      rk[n] = load8<VEC>(kp + (int64_t)jr * a.ks[1] + d, cnt);
-      rv[n] = load8<VEC>(vp + (int64_t)jr * a.vs[1] + d, cnt);
-    }
+  const Tile kt(a.k, a.ks, b, g, a.D, wave, lane), vt(a.v, a.vs, b, g, a.D, wave, lane);
+  const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[FAST])};
+  auto load = [&](int t, uint64_t vm) {
+    kt.load(to[t & 1], t, nk, vm, lane);
+    vt.load(to[t & 1] + 16 * Tile::kPieces, t, nk, vm, lane);
   };
-  if (t0 < t1) fetch(t0);
+  uint64_t vm_next = 0;
+  bool allowed = false;  // key `lane` of the tile after the next
+  if (FAST && t0 < t1) {
+    vm_next = __ballot(may_read(t0 * kBN + lane));
+    load(t0, vm_next);
+    allowed = may_read((t0 + 1) * kBN + lane);
+  }
   for (int t = t0; t < t1; ++t) {
-    const uint64_t vm = __ballot(allowed);
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int e = tid + n * NT, kr = e / CH, p = swz<CH>(kr, e % CH);
-      const bool on = (vm >> kr) & 1;
-      sk[p] = on ? rk[n] : make_uint4(0, 0, 0, 0);
-      sv[p] = on ? rv[n] : make_uint4(0, 0, 0, 0);
+    const uint4 *sk = lds[FAST ? t & 1 : 0], *sv = sk + Tile::kPieces;
+    uint64_t vm;
+    if (FAST) {
+      wait_loads();
+      __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
+      vm = vm_next;
+      vm_next = __ballot(allowed);
+      if (t + 1 < t1) {
+        load(t + 1, vm_next);
+        allowed = may_read((t + 2) * kBN + lane);
+      }
+    } else {
+      vm = __ballot(may_read(t * kBN + lane));
+      __syncthreads();
+      copy_tile<DP>(lds[0], a.k, a.ks, b, g, a.D, t, vm);
+      copy_tile<DP>(lds[0] + Tile::kPieces, a.v, a.vs, b, g, a.D, t, vm);
+      __syncthreads();
     }
-    __syncthreads();
-    if (t + 1 < t1) fetch(t + 1);
     auto first = [&](int n, floatx16& s, floatx16& dp) {
       s = dp = floatx16{};
 #pragma unroll
@@ -153,10 +160,14 @@ __global__ __launch_bounds__(NW * 64) void k_attn_dq(const AttnArgs a, int split
     for (int n = 0; n < 2; ++n) {
       floatx16 s, dp;
       first(n, s, dp);
-      const uint32_t w = (uint32_t)(vm >> (32 * n)) >> (4 * h);
+      const uint32_t valid = (uint32_t)(vm >> (32 * n));
+      if (valid == ~0u) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? s[i] * (dp[i] - st[1]) : 0.0f;
+        for (int i = 0; i < 16; ++i) s[i] *= dp[i] - st[1];
+      } else {
+        const uint32_t w = valid >> (4 * h);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (w >> (8 * (i / 4) + i % 4)) & 1 ? s[i] * (dp[i] - st[1]) : 0.0f;
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -172,16 +183,46 @@ __global__ __launch_bounds__(NW * 64) void k_attn_dq(const AttnArgs a, int split
     store_part<DP>(acc, part + (sp * rows + at) * DP, h);
   } else {
     uint16_t* out = (uint16_t*)a.dq + b * a.dqs[0] + (int64_t)qi * a.dqs[1] + head * a.dqs[2];
-    store_cols<T, DP, VEC>(acc, out, ldexpf(a.scale, -a.shift), a.D, h);
+    store_cols<T, DP, FAST>(acc, out, ldexpf(a.scale, -a.shift), a.D, h);
   }
 }
 
-template <class T, int DP, bool VEC>
-__global__ __launch_bounds__(256) void k_attn_dkv(const AttnArgs a, int splits, float* part) {
-  constexpr int CH = DP / 8, NT = 256, NS = DP / 16, ND = DP / 32;
-  constexpr int NL = kBN * CH / NT;
-  __shared__ uint4 sq[kBN * CH], sg[kBN * CH];
-  __shared__ floatx2 sst[kBN];
+// The loads of tiles of 64 rows of one kv head's queries (or their gradients)
+// into LDS, by NW wavefronts: row i is query row i / G, head i % G.
+template <int DP, int NW>
+struct RowTile {
+  static constexpr int kLoads = kBN * DP / 8 / 64 / NW, kRows = 64 / (DP / 8);
+  const char* base;
+  int64_t s1, s2;  // bytes
+  int wave, D, G;
+  float inv_g;
+  __device__ __forceinline__ RowTile(const void* p, const int64_t s[3], int b, int g, int G_, int D_, int wave_)
+      : base((const char*)p + 2 * (b * s[0] + (int64_t)g * G_ * s[2])), s1(2 * s[1]), s2(2 * s[2]), wave(wave_),
+        D(D_), G(G_), inv_g(1.0f / G_) {}
+  __device__ __forceinline__ void load(uint32_t lds, int t, int n_rows, int lane) const {
+    const int q0 = t * kBN / G, h0 = t * kBN - q0 * G;
+    // rows past the last take the offset that is beyond every bound: the bound itself is not needed
+    const u32x4 desc = descriptor(base + q0 * s1, 0x7FFFFFFF);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int r = (n * NW + wave) * kRows + lane / (DP / 8);
+      const int c = (lane % (DP / 8)) ^ swz_bits(r);
+      const int x = h0 + r, q = (int)(((float)x + 0.5f) * inv_g), hd = x - q * G;  // x / G: x < 64 + G
+      const bool on = 8 * c < D && t * kBN + r < n_rows;
+      load_to_lds(to + n * NW * 1024,
+                  on ? (uint32_t)q * (uint32_t)s1 + (uint32_t)hd * (uint32_t)s2 + 16 * c : kOutside, desc);
+    }
+  }
+};
+
+// dk and dv: a wavefront holds 32 keys and values, as columns, and passes over
+// the rows of every query head of its kv head, in tiles that the workgroup's
+// wavefronts share.
+template <class T, int DP, bool FAST>
+__global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a, int splits, float* part) {
+  constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32, kPieces = kBN * CH;
+  __shared__ uint4 lds[FAST ? 2 : 1][2 * kPieces + 64];  // queries, their gradients, (lse, delta) of each row
 
   const int tiles_k = (a.Sk + kKeys - 1) / kKeys;
   int id = xcd_order(blockIdx.x, gridDim.x);
@@ -190,7 +231,7 @@ __global__ __launch_bounds__(256) void k_attn_dkv(const AttnArgs a, int splits, 
   const int sp = id % splits;
   id /= splits;
   const int g = id % a.Hkv, b = id / a.Hkv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
   const int key = kt * kKeys + wave * 32 + r;
   const int nq = clamp_len(a.q_len, b, a.Sq), nk = clamp_len(a.kv_len, b, a.Sk);
@@ -207,43 +248,46 @@ __global__ __launch_bounds__(256) void k_attn_dkv(const AttnArgs a, int splits, 
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     const int d = 16 * s + 8 * h, n = ok ? min(a.D - d, 8) : 0;
-    kf[s] = load8<VEC>(kp + d, n);
-    vf[s] = load8<VEC>(vp + d, n);
+    kf[s] = load8<FAST>(kp + d, n);
+    vf[s] = load8<FAST>(vp + d, n);
   }
   floatx16 dk[ND], dv[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) dk[i] = dv[i] = floatx16{};
 
-  const uint16_t* qp = (const uint16_t*)a.q + b * a.qs[0] + (int64_t)g * a.G * a.qs[2];
-  const uint16_t* gp = (const uint16_t*)a.dout + b * a.dos[0] + (int64_t)g * a.G * a.dos[2];
-  const floatx2* stat = reinterpret_cast<const floatx2*>(a.delta) + ((int64_t)b * a.Hkv + g) * a.M;
-
-  uint4 rq[NL], rg[NL];
-  floatx2 rs[NL];  // the row's (lse, delta), beside each of its chunks
-  auto fetch = [&](int t) {
-#pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int e = tid + n * NT, row = t * kBN + e / CH, d = 8 * (e % CH);
-      const int qi = row / a.G, hd = row % a.G;
-      const int cnt = row < mrows ? min(a.D - d, 8) : 0;
-      rs[n] = row < mrows ? stat[row] : floatx2{INFINITY, 0.0f};
-      rq[n] = load8<VEC>(qp + (int64_t)qi * a.qs[1] + hd * a.qs[2] + d, cnt);
-      rg[n] = load8<VEC>(gp + (int64_t)qi * a.dos[1] + hd * a.dos[2] + d, cnt);
-    }
+  const float* stat = a.delta + 2 * ((int64_t)b * a.Hkv + g) * a.M;
+  const RowTile<DP, 4> qt(a.q, a.qs, b, g, a.G, a.D, wave), gt(a.dout, a.dos, b, g, a.G, a.D, wave);
+  const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[FAST])};
+  auto load = [&](int t) {
+    qt.load(to[t & 1], t, mrows, lane);
+    gt.load(to[t & 1] + 16 * kPieces, t, mrows, lane);
+    if (wave == 0)  // zeros past the last row, whose query and gradient are zeros as well
+      load_to_lds(to[t & 1] + 32 * kPieces, lane < 32 ? 16 * lane : kOutside,
+                  descriptor(stat + 2 * t * kBN, (int64_t)(mrows - t * kBN) * 8));
   };
-  if (t0 < t1) fetch(t0);
-  for (int t = t0; t < t1; ++t) {
+  auto copy = [&](int t) {
     __syncthreads();
-#pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int e = tid + n * NT, row = e / CH, p = swz<CH>(row, e % CH);
-      const bool on = rs[n][0] != INFINITY;  // what a row without a key holds never enters a product
-      sq[p] = on ? rq[n] : make_uint4(0, 0, 0, 0);
-      sg[p] = on ? rg[n] : make_uint4(0, 0, 0, 0);
-      if (e % CH == 0) sst[row] = rs[n];
+    for (int e = tid; e < kPieces; e += 256) {
+      const int row = t * kBN + e / CH, qi = row / a.G, hd = g * a.G + row % a.G, d = 8 * (e % CH);
+      const int n = row < mrows ? min(a.D - d, 8) : 0, p = swz<CH>(e / CH, e % CH);
+      lds[0][p] = load8<false>((const uint16_t*)a.q + b * a.qs[0] + qi * a.qs[1] + hd * a.qs[2] + d, n);
+      lds[0][kPieces + p] = load8<false>((const uint16_t*)a.dout + b * a.dos[0] + qi * a.dos[1] + hd * a.dos[2] + d, n);
     }
+    if (tid < 2 * kBN)
+      reinterpret_cast<float*>(lds[0] + 2 * kPieces)[tid] = t * kBN + tid / 2 < mrows ? stat[2 * t * kBN + tid] : 0.0f;
     __syncthreads();
-    if (t + 1 < t1) fetch(t + 1);
+  };
+  if (FAST && t0 < t1) load(t0);
+  for (int t = t0; t < t1; ++t) {
+    if (FAST) {
+      wait_loads();
+      __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
+      if (t + 1 < t1) load(t + 1);
+    } else {
+      copy(t);
+    }
+    const uint4 *sq = lds[FAST ? t & 1 : 0], *sg = sq + kPieces;
+    const floatx4* sst = reinterpret_cast<const floatx4*>(sg + kPieces);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       floatx16 s = {}, dp = {};
@@ -254,10 +298,12 @@ __global__ __launch_bounds__(256) void k_attn_dkv(const AttnArgs a, int splits, 
         dp = T::mma(sg[p], vf[i], dp);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const floatx2 st = sst[32 * n + 8 * (i / 4) + 4 * h + i % 4];
+      for (int i = 0; i < 16; i += 2) {
+        const floatx4 st = sst[16 * n + 4 * (i / 4) + 2 * h + i % 4 / 2];  // two rows
         s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -st[0]));
+        s[i + 1] = __builtin_amdgcn_exp2f(fmaf(s[i + 1], a.c, -st[2]));
         dp[i] = s[i] * (dp[i] - st[1]);
+        dp[i + 1] = s[i + 1] * (dp[i + 1] - st[3]);
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -282,10 +328,10 @@ __global__ __launch_bounds__(256) void k_attn_dkv(const AttnArgs a, int splits, 
     store_part<DP>(dv, p + DP, h);
   } else {
     const float back = ldexpf(1.0f, -a.shift);
-    store_cols<T, DP, VEC>(dk, (uint16_t*)a.dk + b * a.dks[0] + (int64_t)key * a.dks[1] + g * a.dks[2],
-                           a.scale * back, a.D, h);
-    store_cols<T, DP, VEC>(dv, (uint16_t*)a.dv + b * a.dvs[0] + (int64_t)key * a.dvs[1] + g * a.dvs[2],
-                           back, a.D, h);
+    store_cols<T, DP, FAST>(dk, (uint16_t*)a.dk + b * a.dks[0] + (int64_t)key * a.dks[1] + g * a.dks[2],
+                            a.scale * back, a.D, h);
+    store_cols<T, DP, FAST>(dv, (uint16_t*)a.dv + b * a.dvs[0] + (int64_t)key * a.dvs[1] + g * a.dvs[2],
+                            back, a.D, h);
   }
 }
 
@@ -315,18 +361,23 @@ __global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a, int splits, 
   out[d] = (typename T::E)(x * f);
 }
 
-// Parts of the contracted axis, so that the chip is busy also where one axis is
+// Parts of the contracted axis, so that the chip is busy also where the other is
 // short: of at least 4 tiles each.
 int dq_splits(const AttnArgs& a) {
-  const int nw = a.M <= 32 ? 1 : 4;
-  const int64_t wgs = (int64_t)((a.M + nw * 32 - 1) / (nw * 32)) * a.Hkv * a.B;
-  const int64_t target = nw == 1 ? 4 * kCUs : 2 * kCUs, tiles = (a.Sk + kBN - 1) / kBN;
-  return wgs ? (int)std::max<int64_t>(1, std::min(target / wgs, tiles / 4)) : 1;
+  const int64_t wgs = (((int64_t)a.M + 127) / 128) * a.Hkv * a.B, tiles = (a.Sk + kBN - 1) / kBN;
+  return wgs ? (int)std::max<int64_t>(1, std::min(kCUs / wgs, tiles / 4)) : 1;
 }
 int dkv_splits(const AttnArgs& a) {
   const int64_t wgs = (int64_t)((a.Sk + kKeys - 1) / kKeys) * a.Hkv * a.B;
   const int64_t tiles = ((int64_t)a.M + kBN - 1) / kBN;
-  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / wgs, tiles / 4)) : 1;
+  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCUs / wgs, tiles / 4)) : 1;
+}
+// Whether the tiles of rows can go to LDS by 16-byte loads with 32-bit offsets.
+bool fast_rows(const AttnArgs& a) {
+  auto fits = [&](const int64_t s[3]) {
+    return s[1] <= kMaxTileStride && s[2] <= kMaxTileStride && 2 * ((kBN / a.G + 2) * s[1] + a.G * s[2]) < (1ll << 31);
+  };
+  return fits(a.qs) && fits(a.dos);
 }
 int64_t stat_floats(const AttnArgs& a) { return ((int64_t)2 * a.B * a.Hkv * a.M + 3) / 4 * 4; }
 int64_t dq_floats(const AttnArgs& a) {
@@ -338,24 +389,21 @@ int64_t dkv_floats(const AttnArgs& a) {
   return s > 1 ? (int64_t)s * a.B * a.Hkv * a.Sk * 2 * padded(a.D) : 0;
 }
 
-template <class T, int DP, bool VEC>
+template <class T, int DP, bool FAST>
 void launch(const AttnArgs& a, float* part_q, float* part_kv, hipStream_t s) {
   const int64_t rows = (int64_t)a.B * a.Hkv * a.M, keys = (int64_t)a.B * a.Hkv * a.Sk;
   if (rows) {
     const int per = 256 / (DP / 8);
-    k_attn_stat<T, DP, VEC><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(a);
-    const int ns = dq_splits(a), nw = a.M <= 32 ? 1 : 4;
-    const int64_t n = (int64_t)((a.M + nw * 32 - 1) / (nw * 32)) * ns * a.Hkv * a.B;
-    if (nw == 1)
-      k_attn_dq<T, DP, 1, VEC><<<(unsigned)n, 64, 0, s>>>(a, ns, part_q);
-    else
-      k_attn_dq<T, DP, 4, VEC><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
+    k_attn_stat<T, DP, FAST><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(a);
+    const int ns = dq_splits(a);
+    const int64_t n = (((int64_t)a.M + 127) / 128) * ns * a.Hkv * a.B;
+    k_attn_dq<T, DP, FAST><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
     if (ns > 1) k_attn_sum<T, DP, false><<<(unsigned)((rows * DP + 255) / 256), 256, 0, s>>>(a, ns, part_q);
   }
   if (keys) {
     const int ns = dkv_splits(a);
     const int64_t n = (int64_t)((a.Sk + kKeys - 1) / kKeys) * ns * a.Hkv * a.B;
-    k_attn_dkv<T, DP, VEC><<<(unsigned)n, 256, 0, s>>>(a, ns, part_kv);
+    k_attn_dkv<T, DP, FAST><<<(unsigned)n, 256, 0, s>>>(a, ns, part_kv);
     if (ns > 1)
       k_attn_sum<T, DP, true><<<(unsigned)((keys * 2 * DP + 255) / 256), 256, 0, s>>>(a, ns, part_kv);
   }
@@ -363,10 +411,11 @@ void launch(const AttnArgs& a, float* part_q, float* part_kv, hipStream_t s) {
 
 template <class T>
 void launch_t(const AttnArgs& a, float* pq, float* pk, hipStream_t s) {
+  const bool fast = fast_loads(a) && fast_rows(a);
   if (padded(a.D) == 128)
-    a.vec ? launch<T, 128, true>(a, pq, pk, s) : launch<T, 128, false>(a, pq, pk, s);
+    fast ? launch<T, 128, true>(a, pq, pk, s) : launch<T, 128, false>(a, pq, pk, s);
   else
-    a.vec ? launch<T, 64, true>(a, pq, pk, s) : launch<T, 64, false>(a, pq, pk, s);
+    fast ? launch<T, 64, true>(a, pq, pk, s) : launch<T, 64, false>(a, pq, pk, s);
 }
 
 }  // namespace
