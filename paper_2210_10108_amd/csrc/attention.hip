@@ -157,11 +157,12 @@ struct Place {
 // loads of the next run while the products of one do.  One barrier a tile.
 template <class T, int DP>
 __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
-  using Tile = KVTile<DP, 4>;
+  using Tile = RowTile<DP, 4>;
   __shared__ uint4 lds[2][2 * Tile::kPieces];  // keys, then values
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const Place at(a, 128, wave * 32 + (lane & 31));
-  Tile kt(a.k, a.ks, at.b, at.g, a.D, wave, lane), vt(a.v, a.vs, at.b, at.g, a.D, wave, lane);
+  const Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, wave, lane);
+  const Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, wave, lane);
   Rows<T, DP> x;
   x.template init<true>(at.q, at.ok, a.D, h);
   const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[1])};
@@ -202,11 +203,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
 // wavefronts' sums meet in LDS.
 template <class T, int DP>
 __global__ __launch_bounds__(256) void k_attn_few(const AttnArgs a) {
-  using Tile = KVTile<DP, 1>;
+  using Tile = RowTile<DP, 1>;
   __shared__ uint4 lds[4][2 * Tile::kPieces];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const Place at(a, 32, lane & 31);
-  Tile kt(a.k, a.ks, at.b, at.g, a.D, 0, lane), vt(a.v, a.vs, at.b, at.g, a.D, 0, lane);
+  const Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, 0, lane);
+  const Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, 0, lane);
   Rows<T, DP> x;
   x.template init<true>(at.q, at.ok, a.D, h);
   uint4 *sk = lds[wave], *sv = sk + Tile::kPieces;

@@ -18,20 +18,23 @@ namespace pnerf {
 namespace {
 
 constexpr int kKeys = 128;  // keys of a workgroup of the dk, dv pass: 32 a wavefront
+// Rows of one of its tiles.
+constexpr int dkv_rows(int width, bool fast) { return fast && width == 128 ? 32 : 64; }
 
 // (lse / ln 2 - shift, delta) of every row; (+inf, 0) where the row has no
 // allowed key or is past q_len, which makes all of its p zero.
 template <class T, int DP, bool VEC>
 __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
   constexpr int LR = DP / 8;  // lanes of a row
-  const int64_t rows = (int64_t)a.B * a.Hkv * a.M;
+  const int64_t rows = (int64_t)a.B * a.Hq * a.Sq;
   const int64_t at = (int64_t)blockIdx.x * (256 / LR) + threadIdx.x / LR;
   const int d = 8 * (threadIdx.x % LR);
   float sum = 0.0f;
   if (at < rows) {
-    const int row = (int)(at % a.M), bg = (int)(at / a.M), g = bg % a.Hkv, b = bg / a.Hkv;
-    const int qi = row / a.G, head = g * a.G + row % a.G;
-    const float lse = a.lse[((int64_t)b * a.Hq + head) * a.Sq + qi];
+    // neighbours are the heads of one row, as they are in memory
+    const int head = (int)(at % a.Hq), bq = (int)(at / a.Hq), qi = bq % a.Sq, b = bq / a.Sq;
+    const int64_t out = ((int64_t)b * a.Hq + head) * a.Sq + qi;
+    const float lse = a.lse[out];
     const bool ok = qi < clamp_len(a.q_len, b, a.Sq) && lse != -INFINITY;
     const int n = ok ? min(a.D - d, 8) : 0;
     const uint4 x = load8<VEC>((const uint16_t*)a.o + b * a.os[0] + (int64_t)qi * a.os[1] +
@@ -44,7 +47,7 @@ __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
 #pragma unroll
     for (int m = LR / 2; m; m >>= 1) sum += __shfl_xor(sum, m);
     if (d == 0)
-      reinterpret_cast<floatx2*>(a.delta)[at] =
+      reinterpret_cast<floatx2*>(a.delta)[out] =
           ok ? floatx2{lse * 1.4426950408889634f - (float)a.shift, sum} : floatx2{INFINITY, 0.0f};
   }
 }
@@ -55,7 +58,7 @@ __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
 template <class T, int DP, bool FAST>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits, float* part) {
   constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32;
-  using Tile = KVTile<DP, 4>;
+  using Tile = RowTile<DP, 4>;
   __shared__ uint4 lds[FAST ? 2 : 1][2 * Tile::kPieces];  // keys, then values
 
   const int tiles_m = (a.M + 127) / 128;
@@ -77,8 +80,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
 
   const int64_t rows = (int64_t)a.B * a.Hkv * a.M;
   const int64_t at = ((int64_t)b * a.Hkv + g) * a.M + row;
+  floatx2* stat = reinterpret_cast<floatx2*>(a.delta) + ((int64_t)b * a.Hq + head) * a.Sq + qi;
   floatx2 st = floatx2{INFINITY, 0.0f};
-  if (row < a.M) st = reinterpret_cast<const floatx2*>(a.delta)[at];
+  if (row < a.M) st = *stat;
   const bool ok = st[0] != INFINITY;
 
   const uint16_t* qp = (const uint16_t*)a.q + b * a.qs[0] + (int64_t)qi * a.qs[1] + head * a.qs[2];
@@ -96,7 +100,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
 #pragma unroll
   for (int i = 0; i < ND; ++i) acc[i] = floatx16{};
 
-  const Tile kt(a.k, a.ks, b, g, a.D, wave, lane), vt(a.v, a.vs, b, g, a.D, wave, lane);
+  const Tile kt(a.k, b * a.ks[0] + g * a.ks[2], a.ks[1], a.D, wave, lane);
+  const Tile vt(a.v, b * a.vs[0] + g * a.vs[2], a.vs[1], a.D, wave, lane);
   const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[FAST])};
   auto load = [&](int t, uint64_t vm) {
     kt.load(to[t & 1], t, nk, vm, lane);
@@ -154,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
       float s0, s1;
       halves(sum, s0, s1);
       st[1] = ldexpf(s0 + s1, -a.shift);
-      if (h == 0 && ok) reinterpret_cast<floatx2*>(a.delta)[at] = st;
+      if (h == 0 && ok) *stat = st;
     }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -187,42 +192,19 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
   }
 }
 
-// The loads of tiles of 64 rows of one kv head's queries (or their gradients)
-// into LDS, by NW wavefronts: row i is query row i / G, head i % G.
-template <int DP, int NW>
-struct RowTile {
-  static constexpr int kLoads = kBN * DP / 8 / 64 / NW, kRows = 64 / (DP / 8);
-  const char* base;
-  int64_t s1, s2;  // bytes
-  int wave, D, G;
-  float inv_g;
-  __device__ __forceinline__ RowTile(const void* p, const int64_t s[3], int b, int g, int G_, int D_, int wave_)
-      : base((const char*)p + 2 * (b * s[0] + (int64_t)g * G_ * s[2])), s1(2 * s[1]), s2(2 * s[2]), wave(wave_),
-        D(D_), G(G_), inv_g(1.0f / G_) {}
-  __device__ __forceinline__ void load(uint32_t lds, int t, int n_rows, int lane) const {
-    const int q0 = t * kBN / G, h0 = t * kBN - q0 * G;
-    // rows past the last take the offset that is beyond every bound: the bound itself is not needed
-    const u32x4 desc = descriptor(base + q0 * s1, 0x7FFFFFFF);
-    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const int r = (n * NW + wave) * kRows + lane / (DP / 8);
-      const int c = (lane % (DP / 8)) ^ swz_bits(r);
-      const int x = h0 + r, q = (int)(((float)x + 0.5f) * inv_g), hd = x - q * G;  // x / G: x < 64 + G
-      const bool on = 8 * c < D && t * kBN + r < n_rows;
-      load_to_lds(to + n * NW * 1024,
-                  on ? (uint32_t)q * (uint32_t)s1 + (uint32_t)hd * (uint32_t)s2 + 16 * c : kOutside, desc);
-    }
-  }
-};
-
 // dk and dv: a wavefront holds 32 keys and values, as columns, and passes over
-// the rows of every query head of its kv head, in tiles that the workgroup's
-// wavefronts share.
+// the query heads of its kv head and their rows, in tiles of one head's rows
+// (whose addresses are a plain progression) that the workgroup's wavefronts share.
+// At the wide head the sums take 128 registers and the keys 32; the values, each
+// lane's its own, wait in LDS, which leaves registers for two wavefronts a SIMD
+// (4 x 4096 rows and keys, 16 heads of 128:
+// 1.05 PFLOP/s; with the values in registers and one wavefront a SIMD 0.70).  The tiles are then of 32 rows.
 template <class T, int DP, bool FAST>
 __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a, int splits, float* part) {
-  constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32, kPieces = kBN * CH;
+  constexpr bool kStash = FAST && DP == 128;
+  constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32, kR = dkv_rows(DP, FAST), kPieces = kR * CH;
   __shared__ uint4 lds[FAST ? 2 : 1][2 * kPieces + 64];  // queries, their gradients, (lse, delta) of each row
+  __shared__ uint4 stash[kStash ? 4 : 1][kStash ? NS : 1][64];
 
   const int tiles_k = (a.Sk + kKeys - 1) / kKeys;
   int id = xcd_order(blockIdx.x, gridDim.x);
@@ -236,8 +218,8 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
   const int key = kt * kKeys + wave * 32 + r;
   const int nq = clamp_len(a.q_len, b, a.Sq), nk = clamp_len(a.kv_len, b, a.Sk);
   const bool ok = key < nk && (!a.mask || a.mask[b * a.mask_stride + key]);
-  const int mrows = nq * a.G;
-  int t1 = (mrows + kBN - 1) / kBN;
+  const int tiles_q = (nq + kR - 1) / kR;  // of a head
+  int t1 = tiles_q * a.G;
   const int per = (t1 + splits - 1) / splits, t0 = min(sp * per, t1);
   t1 = min(t0 + per, t1);
   if (kt * kKeys >= nk) t1 = t0;
@@ -250,52 +232,69 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
     const int d = 16 * s + 8 * h, n = ok ? min(a.D - d, 8) : 0;
     kf[s] = load8<FAST>(kp + d, n);
     vf[s] = load8<FAST>(vp + d, n);
+    if (kStash) stash[wave][s][lane] = vf[s];
   }
   floatx16 dk[ND], dv[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) dk[i] = dv[i] = floatx16{};
 
-  const float* stat = a.delta + 2 * ((int64_t)b * a.Hkv + g) * a.M;
-  const RowTile<DP, 4> qt(a.q, a.qs, b, g, a.G, a.D, wave), gt(a.dout, a.dos, b, g, a.G, a.D, wave);
+  const float* stat = a.delta + 2 * ((int64_t)b * a.Hq + g * a.G) * a.Sq;
+  RowTile<DP, 4, kR> qt(a.q, b * a.qs[0] + (int64_t)g * a.G * a.qs[2], a.qs[1], a.D, wave, lane);
+  RowTile<DP, 4, kR> gt(a.dout, b * a.dos[0] + (int64_t)g * a.G * a.dos[2], a.dos[1], a.D, wave, lane);
   const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[FAST])};
-  auto load = [&](int t) {
-    qt.load(to[t & 1], t, mrows, lane);
-    gt.load(to[t & 1] + 16 * kPieces, t, mrows, lane);
-    if (wave == 0)  // zeros past the last row, whose query and gradient are zeros as well
-      load_to_lds(to[t & 1] + 32 * kPieces, lane < 32 ? 16 * lane : kOutside,
-                  descriptor(stat + 2 * t * kBN, (int64_t)(mrows - t * kBN) * 8));
+  int head = 0, tile = t0;  // of the next tile: its head and its number there
+  if (t0 < t1) {
+    head = t0 / tiles_q, tile = t0 - head * tiles_q;
+    qt.base += 2 * head * a.qs[2], gt.base += 2 * head * a.dos[2];
+    stat += 2 * (int64_t)head * a.Sq;
+  }
+  auto next = [&] {
+    if (++tile < tiles_q) return;
+    tile = 0;
+    ++head;
+    qt.base += 2 * a.qs[2], gt.base += 2 * a.dos[2];
+    stat += 2 * a.Sq;
   };
-  auto copy = [&](int t) {
+  auto load = [&](int buf) {  // the next tile; past the last row all is zeros
+    qt.load(to[buf], tile, nq, ~0ull, lane);
+    gt.load(to[buf] + 16 * kPieces, tile, nq, ~0ull, lane);
+    if (wave == 0)
+      load_to_lds(to[buf] + 32 * kPieces, lane < kR / 2 ? 16 * lane : kOutside,
+                  descriptor(stat + 2 * tile * kR, (int64_t)(nq - tile * kR) * 8));
+    next();
+  };
+  auto copy = [&] {
     __syncthreads();
     for (int e = tid; e < kPieces; e += 256) {
-      const int row = t * kBN + e / CH, qi = row / a.G, hd = g * a.G + row % a.G, d = 8 * (e % CH);
-      const int n = row < mrows ? min(a.D - d, 8) : 0, p = swz<CH>(e / CH, e % CH);
-      lds[0][p] = load8<false>((const uint16_t*)a.q + b * a.qs[0] + qi * a.qs[1] + hd * a.qs[2] + d, n);
-      lds[0][kPieces + p] = load8<false>((const uint16_t*)a.dout + b * a.dos[0] + qi * a.dos[1] + hd * a.dos[2] + d, n);
+      const int qi = tile * kR + e / CH, d = 8 * (e % CH);
+      const int n = qi < nq ? min(a.D - d, 8) : 0, p = swz<CH>(e / CH, e % CH);
+      lds[0][p] = load8<false>((const uint16_t*)qt.base + qi * a.qs[1] + d, n);
+      lds[0][kPieces + p] = load8<false>((const uint16_t*)gt.base + qi * a.dos[1] + d, n);
     }
-    if (tid < 2 * kBN)
-      reinterpret_cast<float*>(lds[0] + 2 * kPieces)[tid] = t * kBN + tid / 2 < mrows ? stat[2 * t * kBN + tid] : 0.0f;
+    if (tid < 2 * kR)
+      reinterpret_cast<float*>(lds[0] + 2 * kPieces)[tid] = tile * kR + tid / 2 < nq ? stat[2 * tile * kR + tid] : 0.0f;
     __syncthreads();
+    next();
   };
-  if (FAST && t0 < t1) load(t0);
+  if (FAST && t0 < t1) load(t0 & 1);
   for (int t = t0; t < t1; ++t) {
     if (FAST) {
       wait_loads();
       __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
-      if (t + 1 < t1) load(t + 1);
+      if (t + 1 < t1) load((t + 1) & 1);
     } else {
-      copy(t);
+      copy();
     }
     const uint4 *sq = lds[FAST ? t & 1 : 0], *sg = sq + kPieces;
     const floatx4* sst = reinterpret_cast<const floatx4*>(sg + kPieces);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < kR / 32; ++n) {
       floatx16 s = {}, dp = {};
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         const int p = swz<CH>(32 * n + r, 2 * i + h);
         s = T::mma(sq[p], kf[i], s);
-        dp = T::mma(sg[p], vf[i], dp);
+        dp = T::mma(sg[p], kStash ? stash[wave][i][lane] : vf[i], dp);
       }
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
@@ -369,15 +368,15 @@ int dq_splits(const AttnArgs& a) {
 }
 int dkv_splits(const AttnArgs& a) {
   const int64_t wgs = (int64_t)((a.Sk + kKeys - 1) / kKeys) * a.Hkv * a.B;
-  const int64_t tiles = ((int64_t)a.M + kBN - 1) / kBN;
+  const int rows = dkv_rows(padded(a.D), true);
+  const int64_t tiles = (int64_t)((a.Sq + rows - 1) / rows) * a.G;
   return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCUs / wgs, tiles / 4)) : 1;
 }
-// Whether the tiles of rows can go to LDS by 16-byte loads with 32-bit offsets.
+// Whether tiles of rows can go to LDS by 16-byte loads with 32-bit offsets, the
+// rows past the last beyond the descriptor's bound.
 bool fast_rows(const AttnArgs& a) {
-  auto fits = [&](const int64_t s[3]) {
-    return s[1] <= kMaxTileStride && s[2] <= kMaxTileStride && 2 * ((kBN / a.G + 2) * s[1] + a.G * s[2]) < (1ll << 31);
-  };
-  return fits(a.qs) && fits(a.dos);
+  auto fits = [&](int64_t stride) { return a.Sq == 1 || (stride >= a.D && stride <= kMaxTileStride); };
+  return fits(a.qs[1]) && fits(a.dos[1]);
 }
 int64_t stat_floats(const AttnArgs& a) { return ((int64_t)2 * a.B * a.Hkv * a.M + 3) / 4 * 4; }
 int64_t dq_floats(const AttnArgs& a) {

@@ -31,28 +31,43 @@ __device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// The loads of one kv head's tiles into LDS, by NW wavefronts.
-template <int DP, int NW>
-struct KVTile {
-  static constexpr int kPieces = kBN * DP / 8;         // 16-byte chunks of a tile
-  static constexpr int kLoads = kPieces / 64 / NW;     // of a wavefront
-  static constexpr int kRows = 64 / (DP / 8);          // rows of one
+// The loads of tiles of N rows (keys, values, or the query rows of one head) into
+// LDS, by NW wavefronts.
+template <int DP, int NW, int N = kBN>
+struct RowTile {
+  static constexpr int kPieces = N * DP / 8;         // 16-byte chunks of a tile
+  static constexpr int kLoads = kPieces / 64 / NW;   // of a wavefront
+  static constexpr int kRows = 64 / (DP / 8);        // rows of one load
+  static constexpr int kKinds = NW == 1 && kRows == 4 ? 2 : 1;  // see swz_bits: odd loads' rows differ in bit 2
   const char* base;
   int64_t row_bytes;
   int wave, D;
-  __device__ __forceinline__ KVTile(const void* p, const int64_t s[3], int b, int g, int D_, int wave_, int lane)
-      : base((const char*)p + 2 * (b * s[0] + g * s[2])), row_bytes(2 * s[1]), wave(wave_), D(D_) {}
-  // Tile t, whose keys that may be read are vm, to LDS at lds.
-  __device__ __forceinline__ void load(uint32_t lds, int t, int n_rows, uint64_t vm, int lane) const {
-    const u32x4 desc = descriptor(base + (int64_t)t * kBN * row_bytes,
-                                  (int64_t)(n_rows - t * kBN - 1) * row_bytes + 2 * D);
-    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
+  uint32_t off[kKinds];  // this lane's chunk of the tile's first load (of each kind)
+  __device__ __forceinline__ RowTile(const void* p, int64_t first, int64_t stride, int D_, int wave_, int lane)
+      : base((const char*)p + 2 * first), row_bytes(2 * stride), wave(wave_), D(D_) {
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const int r = (n * NW + wave) * kRows + lane / (DP / 8);
-      const int c = (lane % (DP / 8)) ^ swz_bits(r);
-      const bool on = 8 * c < D && ((vm >> r) & 1);
-      load_to_lds(to + n * NW * 1024, on ? (uint32_t)r * (uint32_t)row_bytes + 16 * c : kOutside, desc);
+    for (int i = 0; i < kKinds; ++i) {
+      const int r = wave * kRows + lane / (DP / 8), c = (lane % (DP / 8)) ^ swz_bits(r + i * kRows);
+      off[i] = 8 * c < D ? (uint32_t)r * (uint32_t)row_bytes + 16 * c : kOutside;
+    }
+  }
+  // Tile t of n_rows rows to LDS at lds.  on: its rows that may be read; a row past
+  // the last is beyond the descriptor's bound only where rows do not overlap.
+  __device__ __forceinline__ void load(uint32_t lds, int t, int n_rows, uint64_t on, int lane) const {
+    const u32x4 desc = descriptor(base + (int64_t)t * N * row_bytes,
+                                  (int64_t)(n_rows - t * N - 1) * row_bytes + 2 * D);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
+    const uint32_t step = NW * kRows * (uint32_t)row_bytes;
+    if (on == ~0ull) {
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) load_to_lds(to + n * NW * 1024, off[n % kKinds] + n * step, desc);
+    } else {
+      uint64_t mine = on >> (wave * kRows + lane / (DP / 8));
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n, mine >>= NW * kRows) {
+        const uint32_t o = off[n % kKinds] + n * step;
+        load_to_lds(to + n * NW * 1024, mine & 1 ? o : kOutside, desc);
+      }
     }
   }
 };
