@@ -74,8 +74,10 @@ struct Rows {
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
     float m0, m1;
     halves(mx, m0, m1);
+    // m may lag behind the maximum by 8 (p up to 2^8, exact in no other way than
+    // with it): the sums are rescaled a few times a pass, not in most tiles
     const float mn = fmaxf(m, c * fmaxf(m0, m1));
-    if (__any(mn > m)) {  // some row's maximum has grown
+    if (__any(mn > m + 8.0f)) {
       const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
       m = mn;
       l *= alpha;

@@ -197,8 +197,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
 // (whose addresses are a plain progression) that the workgroup's wavefronts share.
 // At the wide head the sums take 128 registers and the keys 32; the values, each
 // lane's its own, wait in LDS, which leaves registers for two wavefronts a SIMD
-// (4 x 4096 rows and keys, 16 heads of 128:
-// 1.05 PFLOP/s; with the values in registers and one wavefront a SIMD 0.70).  The tiles are then of 32 rows.
+// (4 x 4096 rows and keys, 16 heads of 128: 1.05 PFLOP/s; with the values in
+// registers and one wavefront a SIMD 0.70).  The tiles are then of 32 rows.
 template <class T, int DP, bool FAST>
 __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a, int splits, float* part) {
   constexpr bool kStash = FAST && DP == 128;
@@ -334,30 +334,30 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
   }
 }
 
-// Adds the parts up in order, one element a thread: dq (KV = false), dk and dv.
-template <class T, int DP, bool KV>
+// Adds the parts up in order, 4 elements a thread: dq (KV = false), dk and dv.
+template <class T, int DP, bool KV, bool VEC>
 __global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a, int splits, const float* part) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   const int len = KV ? a.Sk : a.M;
   const int64_t n = (int64_t)a.B * a.Hkv * len * (KV ? 2 : 1) * DP;
   const int d = (int)(e % DP);
   if (e >= n || d >= a.D) return;
-  float x = 0.0f;
-  for (int s = 0; s < splits; ++s) x += part[s * n + e];
+  floatx4 x = *reinterpret_cast<const floatx4*>(part + e);
+#pragma unroll 4
+  for (int s = 1; s < splits; ++s) x += *reinterpret_cast<const floatx4*>(part + s * n + e);
   int64_t i = e / DP;
   const bool val = KV && (i & 1);
   if (KV) i >>= 1;
   const int at = (int)(i % len), bg = (int)(i / len), g = bg % a.Hkv, b = bg / a.Hkv;
   const float f = ldexpf(val ? 1.0f : a.scale, -a.shift);
-  typename T::E* out;
+  uint16_t* out;
   if (!KV)
-    out = (typename T::E*)a.dq + b * a.dqs[0] + (int64_t)(at / a.G) * a.dqs[1] +
-          (g * a.G + at % a.G) * a.dqs[2];
+    out = (uint16_t*)a.dq + b * a.dqs[0] + (int64_t)(at / a.G) * a.dqs[1] + (g * a.G + at % a.G) * a.dqs[2];
   else if (val)
-    out = (typename T::E*)a.dv + b * a.dvs[0] + at * a.dvs[1] + g * a.dvs[2];
+    out = (uint16_t*)a.dv + b * a.dvs[0] + at * a.dvs[1] + g * a.dvs[2];
   else
-    out = (typename T::E*)a.dk + b * a.dks[0] + at * a.dks[1] + g * a.dks[2];
-  out[d] = (typename T::E)(x * f);
+    out = (uint16_t*)a.dk + b * a.dks[0] + at * a.dks[1] + g * a.dks[2];
+  store4<VEC>(out + d, make_uint2(T::pack(x[0] * f, x[1] * f), T::pack(x[2] * f, x[3] * f)), a.D - d);
 }
 
 // Parts of the contracted axis, so that the chip is busy also where the other is
@@ -397,14 +397,14 @@ void launch(const AttnArgs& a, float* part_q, float* part_kv, hipStream_t s) {
     const int ns = dq_splits(a);
     const int64_t n = (((int64_t)a.M + 127) / 128) * ns * a.Hkv * a.B;
     k_attn_dq<T, DP, FAST><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
-    if (ns > 1) k_attn_sum<T, DP, false><<<(unsigned)((rows * DP + 255) / 256), 256, 0, s>>>(a, ns, part_q);
+    if (ns > 1) k_attn_sum<T, DP, false, FAST><<<(unsigned)((rows * DP / 4 + 255) / 256), 256, 0, s>>>(a, ns, part_q);
   }
   if (keys) {
     const int ns = dkv_splits(a);
     const int64_t n = (int64_t)((a.Sk + kKeys - 1) / kKeys) * ns * a.Hkv * a.B;
     k_attn_dkv<T, DP, FAST><<<(unsigned)n, 256, 0, s>>>(a, ns, part_kv);
     if (ns > 1)
-      k_attn_sum<T, DP, true><<<(unsigned)((keys * 2 * DP + 255) / 256), 256, 0, s>>>(a, ns, part_kv);
+      k_attn_sum<T, DP, true, FAST><<<(unsigned)((keys * 2 * DP / 4 + 255) / 256), 256, 0, s>>>(a, ns, part_kv);
   }
 }
 

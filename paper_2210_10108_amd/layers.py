@@ -89,68 +89,74 @@ def _check(status: int):
 
 
 class _Call:
-    """One call: its device and stream, what it allocates, what it keeps alive."""
+    """One call: its device, data type and stream.  (A call takes about 10 us of
+    the host's time, more than the smallest take on the device: what is usual is
+    looked at first, and told apart only where it is not.)"""
+    __slots__ = ("index", "dtype", "code", "stream", "raw")
 
     def __init__(self, first, stream):
         import torch
         if not isinstance(first, torch.Tensor) or not first.is_cuda:
             raise TypeError("operands must be device tensors")
-        self.device, self.dtype = first.device, first.dtype
-        if self.dtype not in _dtypes():
+        self.index, self.dtype = first.get_device(), first.dtype
+        self.code = _dtypes().get(self.dtype)
+        if self.code is None:
             raise TypeError(f"unsupported data type {self.dtype}")
-        self.code = _dtypes()[self.dtype]
-        current = torch.cuda.current_stream(self.device)
-        self.stream = current if stream is None else stream
-        if self.stream.device != self.device:
-            raise ValueError(f"stream on {self.stream.device}, tensors on {self.device}")
-        self.foreign = self.stream != current
+        current = torch._C._cuda_getCurrentRawStream(self.index)
+        self.stream, self.raw = None, current  # stream: only where it is another one
+        if stream is not None:
+            if stream.device.index != self.index:
+                raise ValueError(f"stream on {stream.device}, tensors on cuda:{self.index}")
+            if stream.cuda_stream != current:
+                self.stream, self.raw = stream, stream.cuda_stream
 
     def tensor(self, t, name, shape, dtype=None, contiguous=False):
         """Checks a tensor and returns its address (None for None)."""
         if t is None:
             return None
-        if not t.is_cuda or t.device != self.device:
-            raise TypeError(f"{name} must be on {self.device}")
-        if t.dtype != (dtype or self.dtype):
+        if t.dtype is not (dtype or self.dtype):
             raise TypeError(f"{name} must be {dtype or self.dtype}, got {t.dtype}")
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-        if contiguous:
-            if not t.is_contiguous():
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.get_device() != self.index:  # -1 on the host
+            raise TypeError(f"{name} must be on cuda:{self.index}")
+        if not t.is_contiguous():
+            if contiguous:
                 raise ValueError(f"{name} must be contiguous")
-        elif t.stride(-1) != 1 and shape[-1] > 1:
-            raise ValueError(f"the last dimension of {name} must be contiguous")
-        if self.foreign:
+            if t.stride(-1) != 1 and shape[-1] > 1:
+                raise ValueError(f"the last dimension of {name} must be contiguous")
+        if self.stream is not None:
             t.record_stream(self.stream)
         return t.data_ptr()
 
-    def new(self, shape, dtype=None):
+    def new(self, like, shape, dtype=None):
         """An output or workspace: memory of the call's stream, which the current
         one may read as well."""
         import torch
-        if not self.foreign:
-            return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+        if self.stream is None:
+            return like.new_empty(shape, dtype=dtype or self.dtype)
         with torch.cuda.stream(self.stream):
-            t = torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
-        t.record_stream(torch.cuda.current_stream(self.device))
+            t = like.new_empty(shape, dtype=dtype or self.dtype)
+        t.record_stream(torch.cuda.current_stream(self.index))
         return t
 
-    def workspace(self, nbytes):
+    def workspace(self, like, nbytes):
         """(address, bytes, the tensor) of a workspace."""
         if not nbytes:
             return None, 0, None
         import torch
-        t = self.new((nbytes,), torch.uint8)
+        t = self.new(like, (nbytes,), torch.uint8)
         return t.data_ptr(), nbytes, t
 
     def run(self, fn, *args):
         import torch
-        s = C.c_void_p(self.stream.cuda_stream)
-        if torch.cuda.current_device() == self.device.index:
-            _check(fn(*args, s))
+        if torch._C._cuda_getDevice() == self.index:
+            status = fn(*args, self.raw)
         else:
-            with torch.cuda.device(self.device):
-                _check(fn(*args, s))
+            with torch.cuda.device(self.index):
+                status = fn(*args, self.raw)
+        if status != pnerf.OK:
+            _check(status)
 
 
 _DTYPES = None
@@ -185,9 +191,8 @@ def _attention(call, q, k, v, q_len, kv_len, kv_mask, scale):
             raise TypeError(f"kv_mask must be torch.bool or torch.uint8, got {kv_mask.dtype}")
         p.kv_mask = call.tensor(kv_mask, "kv_mask", (B, Sk), kv_mask.dtype)
         p.kv_mask_stride = kv_mask.stride(0)
-    qp, kp, vp = (call.tensor(q, "q", (B, Sq, Hq, D)), call.tensor(k, "k", (B, Sk, Hkv, D)),
-                  call.tensor(v, "v", (B, Sk, Hkv, D)))
-    return p, qp, kp, vp
+    kv = (B, Sk, Hkv, D)
+    return p, call.tensor(q, "q", q.shape), call.tensor(k, "k", kv), call.tensor(v, "v", kv)
 
 
 def cross_attention(q, k, v, q_len=None, kv_len=None, kv_mask=None, scale=None, o=None,
@@ -201,15 +206,17 @@ def cross_attention(q, k, v, q_len=None, kv_len=None, kv_mask=None, scale=None, 
     call = _Call(q, stream)
     p, qp, kp, vp = _attention(call, q, k, v, q_len, kv_len, kv_mask, scale)
     if o is None:
-        o = call.new(q.shape)
-    op = call.tensor(o, "o", tuple(q.shape))
+        o = call.new(q, q.shape)
+    op = call.tensor(o, "o", q.shape)
     p.o_stride[:] = o.stride()[:3]
-    lse = call.new((q.shape[0], q.shape[2], q.shape[1]), torch.float32) if return_lse else None
-    lp = call.tensor(lse, "lse", tuple(lse.shape), torch.float32) if return_lse else None
+    lse = lp = None
+    if return_lse:
+        lse = call.new(q, (p.batch, p.q_heads, p.q_rows), torch.float32)
+        lp = lse.data_ptr()
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_cross_attention_workspace(ref, 0, C.byref(n)))
-    ws, nb, _keep = call.workspace(n.value)
+    ws, nb, _keep = call.workspace(q, n.value)
     call.run(_lib.pnerf_cross_attention, ref, qp, kp, vp, op, lp, ws, nb)
     return (o, lse) if return_lse else o
 
@@ -221,20 +228,19 @@ def cross_attention_backward(do, q, k, v, o, lse, q_len=None, kv_len=None, kv_ma
     import torch
     call = _Call(q, stream)
     p, qp, kp, vp = _attention(call, q, k, v, q_len, kv_len, kv_mask, scale)
-    B, Sq, Hq, _ = shape = tuple(q.shape)
-    dq = call.new(shape) if dq is None else dq
-    dk = call.new(k.shape) if dk is None else dk
-    dv = call.new(k.shape) if dv is None else dv
+    shape = q.shape
+    dq = call.new(q, shape) if dq is None else dq
+    dk = call.new(k, k.shape) if dk is None else dk
+    dv = call.new(k, k.shape) if dv is None else dv
     op, dop = call.tensor(o, "o", shape), call.tensor(do, "do", shape)
-    lp = call.tensor(lse, "lse", (B, Hq, Sq), torch.float32, True)
-    dqp, dkp, dvp = (call.tensor(dq, "dq", shape), call.tensor(dk, "dk", tuple(k.shape)),
-                     call.tensor(dv, "dv", tuple(k.shape)))
+    lp = call.tensor(lse, "lse", (p.batch, p.q_heads, p.q_rows), torch.float32, True)
+    dqp, dkp, dvp = call.tensor(dq, "dq", shape), call.tensor(dk, "dk", k.shape), call.tensor(dv, "dv", k.shape)
     p.o_stride[:], p.do_stride[:] = o.stride()[:3], do.stride()[:3]
     p.dq_stride[:], p.dk_stride[:], p.dv_stride[:] = dq.stride()[:3], dk.stride()[:3], dv.stride()[:3]
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_cross_attention_workspace(ref, 1, C.byref(n)))
-    ws, nb, _keep = call.workspace(n.value)
+    ws, nb, _keep = call.workspace(q, n.value)
     call.run(_lib.pnerf_cross_attention_backward, ref, qp, kp, vp, op, lp, dop, dqp, dkp, dvp, ws, nb)
     return dq, dk, dv
 
@@ -249,22 +255,24 @@ def _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
         if table.dim() != 3 or table.shape[1] != 2:
             raise ValueError(f"table has shape {tuple(table.shape)}, expected (positions, 2, pairs)")
         p.n_positions, p.rotary_dim = table.shape[0], 2 * table.shape[2]
-        p.table = call.tensor(table, "table", tuple(table.shape), torch.float32, True)
-    ptrs = []
-    for side, x, w, pos in (("q", q, q_weight, q_pos), ("k", k, k_weight, k_pos)):
-        if x is None:
-            ptrs.append(None)
-            continue
-        if x.dim() != 3:
-            raise ValueError(f"{side} must have 3 dimensions: rows, heads, head width")
-        T, H, _ = x.shape
-        ptrs.append(call.tensor(x, side, (T, H, D)))
-        setattr(p, side + "_rows", T)
-        setattr(p, side + "_heads", H)
-        getattr(p, side + "_stride")[:] = x.stride()[:2]
-        setattr(p, side + "_weight", call.tensor(w, side + "_weight", (D,), None, True))
-        setattr(p, side + "_pos", call.tensor(pos, side + "_pos", (T,), torch.int32, True))
-    return p, ptrs
+        p.table = call.tensor(table, "table", table.shape, torch.float32, True)
+    if q.dim() != 3:
+        raise ValueError("q must have 3 dimensions: rows, heads, head width")
+    qp = call.tensor(q, "q", q.shape)
+    p.q_rows, p.q_heads, _ = q.shape
+    p.q_stride[:] = q.stride()[:2]
+    p.q_weight = call.tensor(q_weight, "q_weight", (D,), None, True)
+    p.q_pos = call.tensor(q_pos, "q_pos", q.shape[:1], torch.int32, True)
+    if k is None:
+        return p, qp, None
+    if k.dim() != 3 or k.shape[2] != D:
+        raise ValueError(f"k has shape {tuple(k.shape)}, expected (rows, heads, {D})")
+    kp = call.tensor(k, "k", k.shape)
+    p.k_rows, p.k_heads, _ = k.shape
+    p.k_stride[:] = k.stride()[:2]
+    p.k_weight = call.tensor(k_weight, "k_weight", (D,), None, True)
+    p.k_pos = call.tensor(k_pos, "k_pos", k.shape[:1], torch.int32, True)
+    return p, qp, kp
 
 
 def norm_rotate(q, k, q_weight, k_weight, table, q_pos, k_pos, eps: float = 1e-6,
@@ -274,14 +282,13 @@ def norm_rotate(q, k, q_weight, k_weight, table, q_pos, k_pos, eps: float = 1e-6
     sines) or None (no rotation), positions int32 [Tq] and [Tk].  Returns
     (q_out, k_out); an output may be its input."""
     call = _Call(q, stream)
-    p, (qp, kp) = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
-    q_out = call.new(q.shape) if q_out is None else q_out
-    qo = call.tensor(q_out, "q_out", tuple(q.shape))
+    p, qp, kp = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
+    q_out = call.new(q, q.shape) if q_out is None else q_out
+    qo, ko = call.tensor(q_out, "q_out", q.shape), None
     p.q_out_stride[:] = q_out.stride()[:2]
-    ko = None
     if k is not None:
-        k_out = call.new(k.shape) if k_out is None else k_out
-        ko = call.tensor(k_out, "k_out", tuple(k.shape))
+        k_out = call.new(k, k.shape) if k_out is None else k_out
+        ko = call.tensor(k_out, "k_out", k.shape)
         p.k_out_stride[:] = k_out.stride()[:2]
     call.run(lib().pnerf_norm_rotate, C.byref(p), qp, kp, qo, ko)
     return q_out, k_out if k is not None else None
@@ -293,28 +300,28 @@ def norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, q_pos,
     gradients of the outputs; dk and dk_weight are None where k is, a weight's
     gradient where the weight is.  dq may be dq_out, dk may be dk_out."""
     call = _Call(q, stream)
-    p, (qp, kp) = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
-    out, ptrs = [], []
-    for side, x, dy, dx, w in (("q", q, dq_out, dq, q_weight), ("k", k, dk_out, dk, k_weight)):
-        if x is None:
-            out += [None, None]
-            ptrs.append((None, None, None))
-            continue
-        dx = call.new(x.shape) if dx is None else dx
-        dw = None if w is None else call.new(w.shape)
-        ptrs.append((call.tensor(dy, f"d{side}_out", tuple(x.shape)),
-                     call.tensor(dx, f"d{side}", tuple(x.shape)),
-                     call.tensor(dw, f"d{side}_weight", tuple(x.shape[-1:]))))
-        getattr(p, f"d{side}_out_stride")[:] = dy.stride()[:2]
-        getattr(p, f"d{side}_stride")[:] = dx.stride()[:2]
-        out += [dx, dw]
+    p, qp, kp = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
+
+    def side(name, x, dy, dx, w):
+        dx = call.new(x, x.shape) if dx is None else dx
+        dw = None if w is None else call.new(w, w.shape)
+        ptrs = (call.tensor(dy, f"d{name}_out", x.shape), call.tensor(dx, f"d{name}", x.shape),
+                None if w is None else dw.data_ptr())
+        return dx, dw, ptrs
+    dq, dqw, (gq, dqp, wq) = side("q", q, dq_out, dq, q_weight)
+    p.dq_out_stride[:], p.dq_stride[:] = dq_out.stride()[:2], dq.stride()[:2]
+    dkw, (gk, dkp, wk) = None, (None, None, None)
+    if k is None:
+        dk = None
+    else:
+        dk, dkw, (gk, dkp, wk) = side("k", k, dk_out, dk, k_weight)
+        p.dk_out_stride[:], p.dk_stride[:] = dk_out.stride()[:2], dk.stride()[:2]
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_norm_rotate_workspace(ref, C.byref(n)))
-    ws, nb, _keep = call.workspace(n.value)
-    (gq, dqp, wq), (gk, dkp, wk) = ptrs
+    ws, nb, _keep = call.workspace(q, n.value)
     call.run(_lib.pnerf_norm_rotate_backward, ref, qp, kp, gq, gk, dqp, dkp, wq, wk, ws, nb)
-    return out[0], out[2], out[1], out[3]
+    return dq, dk, dqw, dkw
 
 
 # ---------------------------------------------------------------- linear
@@ -343,18 +350,17 @@ def linear(x, w, bias=None, residual=None, activation: str = "none", y=None,
     rp = call.tensor(residual, "residual", shape)
     if residual is not None:
         p.residual_stride = residual.stride(0)
-    y = call.new(shape) if y is None else y
+    y = call.new(x, shape) if y is None else y
     yp = call.tensor(y, "y", shape)
     p.y_stride = y.stride(0)
     z = zp = None
     if return_preact:
-        z = call.new(shape)
-        zp = call.tensor(z, "z", shape)
-        p.z_stride = z.stride(0)
+        z = call.new(x, shape)
+        zp, p.z_stride = z.data_ptr(), p.n
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_linear_workspace(ref, 0, C.byref(n)))
-    ws, nb, _keep = call.workspace(n.value)
+    ws, nb, _keep = call.workspace(x, n.value)
     call.run(_lib.pnerf_linear, ref, xp, wp, bp, rp, yp, zp, ws, nb)
     return (y, z) if return_preact else y
 
@@ -372,15 +378,15 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = Tru
     zp = call.tensor(z, "z", shape)
     if z is not None:
         p.z_stride = z.stride(0)
-    dx = call.new(x.shape) if dx is None else dx
-    dw = call.new(w.shape) if dw is None else dw
-    db = call.new((p.n,)) if bias else None
-    dxp, dwp = call.tensor(dx, "dx", tuple(x.shape)), call.tensor(dw, "dw", tuple(w.shape))
-    dbp = call.tensor(db, "db", (p.n,))
+    dx = call.new(x, x.shape) if dx is None else dx
+    dw = call.new(x, w.shape) if dw is None else dw
+    db = call.new(x, (p.n,)) if bias else None
+    dxp, dwp = call.tensor(dx, "dx", x.shape), call.tensor(dw, "dw", w.shape)
+    dbp = None if db is None else db.data_ptr()
     p.dx_stride, p.dw_stride = dx.stride(0), dw.stride(0)
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_linear_workspace(ref, 1, C.byref(n)))
-    ws, nb, _keep = call.workspace(n.value)
+    ws, nb, _keep = call.workspace(x, n.value)
     call.run(_lib.pnerf_linear_backward, ref, xp, wp, zp, gp, dxp, dwp, dbp, ws, nb)
     return dx, dw, db
