@@ -18,16 +18,22 @@ namespace pnerf {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kMaxPart = 512;  // workgroups of a side of the backward, each with one partial dw
+constexpr int kFwdBlocks = 16 * kCUs, kBwdBlocks = 2 * kCUs;  // workgroups, at most
 
+// 8 consecutive elements: as they are loaded, and as numbers.
 template <class E>
 struct Elem;
 template <>
 struct Elem<float> {
-  static __device__ __forceinline__ void load(const void* p, float v[8]) {
-    const floatx4 a = reinterpret_cast<const floatx4*>(p)[0], b = reinterpret_cast<const floatx4*>(p)[1];
+  struct Raw {
+    floatx4 a, b;
+  };
+  static __device__ __forceinline__ Raw raw(const void* p) {
+    return {reinterpret_cast<const floatx4*>(p)[0], reinterpret_cast<const floatx4*>(p)[1]};
+  }
+  static __device__ __forceinline__ void unpack(const Raw& r, float v[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    for (int i = 0; i < 4; ++i) v[i] = r.a[i], v[4 + i] = r.b[i];
   }
   static __device__ __forceinline__ void store(void* p, const float v[8]) {
     reinterpret_cast<floatx4*>(p)[0] = floatx4{v[0], v[1], v[2], v[3]};
@@ -36,8 +42,9 @@ struct Elem<float> {
 };
 template <class T>
 struct Elem16 {
-  static __device__ __forceinline__ void load(const void* p, float v[8]) {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
+  using Raw = uint4;
+  static __device__ __forceinline__ Raw raw(const void* p) { return *reinterpret_cast<const uint4*>(p); }
+  static __device__ __forceinline__ void unpack(const Raw& w, float v[8]) {
     v[0] = T::lo(w.x), v[1] = T::hi(w.x), v[2] = T::lo(w.y), v[3] = T::hi(w.y);
     v[4] = T::lo(w.z), v[5] = T::hi(w.z), v[6] = T::lo(w.w), v[7] = T::hi(w.w);
   }
@@ -50,11 +57,61 @@ template <>
 struct Elem<_Float16> : Elem16<F16> {};
 template <>
 struct Elem<__bf16> : Elem16<BF16> {};
+template <class E>
+__device__ __forceinline__ void load(const void* p, float v[8]) {
+  Elem<E>::unpack(Elem<E>::raw(p), v);
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {  // a move within rows of 16 lanes, all lanes active
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+
+// Sum over a row of LR lanes, in all of them.
+template <int LR>
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp<0xB1>(x);                       // quad_perm [1, 0, 3, 2]
+  x += dpp<0x4E>(x);                       // quad_perm [2, 3, 0, 1]
+  if (LR >= 8) x += dpp<0x141>(x);         // row_half_mirror
+  if (LR >= 16) x += dpp<0x140>(x);        // row_mirror
+  if (LR >= 32) x += __shfl_xor(x, 16);
+  if (LR >= 64) x += __shfl_xor(x, 32);
+  return x;
+}
+
+// Where the rotation partner of a lane's 8 elements is.
+enum Pairs {
+  kInside,  // interleaved: in the lane itself
+  kHalf,    // in the lane half a row away (the whole head turns and fills its LR lanes)
+  kAway     // in the lane R / 16 away
+};
+template <Pairs P, int LR>
+__device__ __forceinline__ void partners(const NormArgs& a, int d, const float v[8], float p[8]) {
+  if (P == kInside) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) p[i] = v[i + 1], p[i + 1] = v[i];
+  } else if (P == kHalf && LR <= 16) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (LR == 4) p[i] = dpp<0x4E>(v[i]);
+      if (LR == 8) p[i] = dpp<0x1B>(dpp<0x141>(v[i]));  // row_half_mirror, quad_perm [3, 2, 1, 0]
+      if (LR == 16) p[i] = dpp<0x128>(v[i]);            // row_ror 8
+    }
+  } else {
+    const int step = a.R / 16;  // lanes of half the rotated part
+    const int lane = threadIdx.x & 63;
+    const int from = d >= a.R ? lane : d < a.R / 2 ? lane + step : lane - step;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = __shfl(v[i], from);
+  }
+}
+
+__device__ __forceinline__ float inv_rms(float mean, float eps) { return __builtin_amdgcn_rsqf(mean + eps); }
 
 // Cosines and sines of a lane's 8 elements at position pos: element i turns
 // with its partner by (c[i], s[i]), s negated for the first of a pair; (1, 0)
 // past the rotated part, NaN for a position that is not in the table.
-template <bool INTER>
+template <Pairs P>
 __device__ __forceinline__ void angles(const NormArgs& a, int pos, int d, float c[8], float s[8]) {
   const int half = a.R / 2;
 #pragma unroll
@@ -62,7 +119,7 @@ __device__ __forceinline__ void angles(const NormArgs& a, int pos, int d, float 
   if (d >= a.R) return;
   const bool in = pos >= 0 && pos < a.n_pos;
   const float* t = a.table + (int64_t)(in ? pos : 0) * a.R;
-  if (INTER) {
+  if (P == kInside) {
     const floatx4 cc = *reinterpret_cast<const floatx4*>(t + d / 2);
     const floatx4 ss = *reinterpret_cast<const floatx4*>(t + half + d / 2);
 #pragma unroll
@@ -73,8 +130,8 @@ __device__ __forceinline__ void angles(const NormArgs& a, int pos, int d, float 
   } else {
     const int j = d < half ? d : d - half;
     float v[8];
-    Elem<float>::load(t + j, c);
-    Elem<float>::load(t + half + j, v);
+    load<float>(t + j, c);
+    load<float>(t + half + j, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = d < half ? -v[i] : v[i];
   }
@@ -83,122 +140,125 @@ __device__ __forceinline__ void angles(const NormArgs& a, int pos, int d, float 
     for (int i = 0; i < 8; ++i) c[i] = s[i] = __builtin_nanf("");
 }
 
-// The rotation partners of a lane's 8 elements.
-template <bool INTER, int LR>
-__device__ __forceinline__ void partners(const NormArgs& a, int d, const float v[8], float p[8]) {
-  if (INTER) {
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) p[i] = v[i + 1], p[i + 1] = v[i];
-  } else {
-    const int step = a.R / 16;  // lanes of half the rotated part
-    const int lane = threadIdx.x & 63;
-    const int from = d >= a.R ? lane : d < a.R / 2 ? lane + step : lane - step;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = __shfl(v[i], from);
+// The workgroups of the queries come first, then those of the keys.  Each side's
+// walk its heads in memory order, all of them together through one moving window
+// (walking each position's heads in one wavefront, which keeps the cosines in
+// registers, sends the wavefronts to addresses a position apart, and those to few
+// memory channels at a time: 58 us where this takes 45 for the 203 MB of 8192 x 32
+// and 16382 x 8 heads of 128).  A lane's row and head of the next step, by steps:
+struct Walk {
+  int row, head;        // current
+  int d_row, d_head, heads;
+  int64_t left;         // heads from the current one to the end
+  int64_t step;
+  __device__ __forceinline__ Walk(const NormSide& x, int64_t first, int64_t step_)
+      : heads(x.heads), left((int64_t)x.rows * x.heads - first), step(step_) {
+    row = (int)(first / heads), head = (int)(first - (int64_t)row * heads);
+    d_row = (int)(step / heads), d_head = (int)(step - (int64_t)d_row * heads);
   }
-}
-
-template <int LR>
-__device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-  for (int m = LR / 2; m; m >>= 1) x += __shfl_xor(x, m);
-  return x;
-}
-
-// Groups of the grid: of the queries first, then of the keys.
-struct Split {
-  int hpg[2];        // heads a group takes
-  int nhg[2];        // groups of a position
-  int64_t groups[2];
+  __device__ __forceinline__ bool on() const { return left > 0; }
+  __device__ __forceinline__ void next() {
+    left -= step;
+    row += d_row, head += d_head;
+    if (head >= heads) head -= heads, ++row;
+  }
 };
 
-template <class E, int LR, bool INTER>
-__global__ __launch_bounds__(kBlock) void k_norm_fwd(const NormArgs a, const Split sp) {
-  int64_t gid = (int64_t)blockIdx.x * (kBlock / LR) + threadIdx.x / LR;
-  const int d = 8 * (threadIdx.x % LR);
-  const bool second = gid >= sp.groups[0];
-  if (second) gid -= sp.groups[0];
+template <class E, int LR, Pairs P>
+__global__ __launch_bounds__(kBlock) void k_norm_fwd(const NormArgs a, int blocks0, int blocks1) {
+  constexpr int NG = kBlock / LR;
+  const bool second = (int)blockIdx.x >= blocks0;
   const NormSide& x = second ? a.side[1] : a.side[0];
-  const int nhg = second ? sp.nhg[1] : sp.nhg[0];
-  const bool on = gid < (second ? sp.groups[1] : sp.groups[0]);
-  const int row = on ? (int)(gid / nhg) : 0, h0 = (int)(gid % nhg);
-  const bool mine = on && d < a.D;
-  float w[8], c[8], s[8];
+  const int blk = second ? blockIdx.x - blocks0 : blockIdx.x, blocks = second ? blocks1 : blocks0;
+  const int d = 8 * (threadIdx.x % LR);
+  const bool col = d < a.D;
+  float w[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) w[i] = 1.0f;
-  if (mine && x.w) Elem<E>::load((const E*)x.w + d, w);
-  angles<INTER>(a, mine && a.R ? x.pos[row] : 0, mine ? d : a.R, c, s);
-  const E* xp = (const E*)x.x + row * x.xs[0] + d;
-  E* yp = (E*)x.y + row * x.ys[0] + d;
+  if (col && x.w) load<E>((const E*)x.w + d, w);
   const float inv_d = 1.0f / a.D;
+  Walk at(x, (int64_t)blk * NG + threadIdx.x / LR, (int64_t)blocks * NG);
+  typename Elem<E>::Raw raw = {};
+  int pos = 0;
+  auto fetch = [&] {
+    if (!at.on() || !col) return;
+    raw = Elem<E>::raw((const E*)x.x + at.row * x.xs[0] + at.head * x.xs[1] + d);
+    if (a.R) pos = x.pos[at.row];
+  };
+  fetch();
   // every lane of a wavefront makes the same number of rounds: the exchanges need them all
-  const int rounds = max(sp.hpg[0], sp.hpg[1]);
-  for (int i = 0; i < rounds; ++i) {
-    const int h = h0 + i * nhg;
-    const bool here = mine && h < x.heads;
-    float v[8] = {}, p[8];
-    if (here) Elem<E>::load(xp + h * x.xs[1], v);
+  while (__any(at.on())) {
+    float v[8], p[8], c[8], s[8];
+    const bool here = at.on() && col;
+    Elem<E>::unpack(raw, v);
+    angles<P>(a, pos, here ? d : a.R, c, s);
+    E* y = (E*)x.y + at.row * x.ys[0] + at.head * x.ys[1] + d;
+    at.next();
+    fetch();
     float q = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q += v[j] * v[j];
-    const float r = 1.0f / sqrtf(row_sum<LR>(q) * inv_d + a.eps);
+    for (int j = 0; j < 8; ++j) q += here ? v[j] * v[j] : 0.0f;
+    const float r = inv_rms(row_sum<LR>(q) * inv_d, a.eps);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= r * w[j];
-    partners<INTER, LR>(a, d, v, p);
+    partners<P, LR>(a, d, v, p);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = v[j] * c[j] + p[j] * s[j];
-    if (here) Elem<E>::store(yp + h * x.ys[1], v);
+    if (here) Elem<E>::store(y, v);
   }
 }
 
-// Workgroups of a side walk its groups in strides; each leaves its sum of dw.
-template <class E, int LR, bool INTER>
-__global__ __launch_bounds__(kBlock) void k_norm_bwd(const NormArgs a, const Split sp, int blocks0,
-                                                     int blocks1, float* part) {
+// Each workgroup leaves its sum of dw.
+template <class E, int LR, Pairs P>
+__global__ __launch_bounds__(kBlock) void k_norm_bwd(const NormArgs a, int blocks0, int blocks1, float* part) {
   constexpr int NG = kBlock / LR;
   __shared__ float red[NG][8 * LR];
   const bool second = (int)blockIdx.x >= blocks0;
   const NormSide& x = second ? a.side[1] : a.side[0];
-  const int nhg = second ? sp.nhg[1] : sp.nhg[0], hpg = second ? sp.hpg[1] : sp.hpg[0];
-  const int64_t groups = second ? sp.groups[1] : sp.groups[0];
   const int blk = second ? blockIdx.x - blocks0 : blockIdx.x, blocks = second ? blocks1 : blocks0;
   const int grp = threadIdx.x / LR, d = 8 * (threadIdx.x % LR);
+  const bool col = d < a.D;
   float w[8], dw[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) w[i] = 1.0f, dw[i] = 0.0f;
-  if (d < a.D && x.w) Elem<E>::load((const E*)x.w + d, w);
+  if (col && x.w) load<E>((const E*)x.w + d, w);
   const float inv_d = 1.0f / a.D;
-  for (int64_t g0 = (int64_t)blk * NG; g0 < groups; g0 += (int64_t)blocks * NG) {
-    const int64_t gid = g0 + grp;
-    const int row = gid < groups ? (int)(gid / nhg) : 0, h0 = (int)(gid % nhg);
-    const bool mine = gid < groups && d < a.D;
-    float c[8], s[8];
-    angles<INTER>(a, mine && a.R ? x.pos[row] : 0, mine ? d : a.R, c, s);
-    for (int i = 0; i < hpg; ++i) {
-      const int h = h0 + i * nhg;
-      const bool here = mine && h < x.heads;
-      float v[8] = {}, g[8] = {}, p[8];
-      if (here) {
-        Elem<E>::load((const E*)x.x + row * x.xs[0] + h * x.xs[1] + d, v);
-        Elem<E>::load((const E*)x.dy + row * x.dys[0] + h * x.dys[1] + d, g);
-      }
-      partners<INTER, LR>(a, d, g, p);
-      float q = 0.0f, dot = 0.0f;
+  Walk at(x, (int64_t)blk * NG + grp, (int64_t)blocks * NG);
+  typename Elem<E>::Raw raw_x = {}, raw_g = {};
+  int pos = 0;
+  auto fetch = [&] {
+    if (!at.on() || !col) return;
+    raw_x = Elem<E>::raw((const E*)x.x + at.row * x.xs[0] + at.head * x.xs[1] + d);
+    raw_g = Elem<E>::raw((const E*)x.dy + at.row * x.dys[0] + at.head * x.dys[1] + d);
+    if (a.R) pos = x.pos[at.row];
+  };
+  fetch();
+  while (__any(at.on())) {
+    float v[8], g[8], p[8], c[8], s[8];
+    const bool here = at.on() && col;
+    Elem<E>::unpack(raw_x, v);
+    Elem<E>::unpack(raw_g, g);
+    angles<P>(a, pos, here ? d : a.R, c, s);
+    E* dx = (E*)x.dx + at.row * x.dxs[0] + at.head * x.dxs[1] + d;
+    at.next();
+    fetch();
+    partners<P, LR>(a, d, g, p);
+    float q = 0.0f, dot = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        g[j] = g[j] * c[j] - p[j] * s[j];  // turned back
-        q += v[j] * v[j];
-        dot += g[j] * w[j] * v[j];
-      }
-      const float r = 1.0f / sqrtf(row_sum<LR>(q) * inv_d + a.eps);
-      const float k = row_sum<LR>(dot) * inv_d * r * r;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (here) dw[j] += g[j] * v[j] * r;
-        g[j] = r * (g[j] * w[j] - v[j] * k);
-      }
-      if (here) Elem<E>::store((E*)x.dx + row * x.dxs[0] + h * x.dxs[1] + d, g);
+    for (int j = 0; j < 8; ++j) {
+      g[j] = here ? g[j] * c[j] - p[j] * s[j] : 0.0f;  // turned back
+      v[j] = here ? v[j] : 0.0f;
+      q += v[j] * v[j];
+      dot += g[j] * w[j] * v[j];
     }
+    const float r = inv_rms(row_sum<LR>(q) * inv_d, a.eps);
+    const float k = row_sum<LR>(dot) * inv_d * r * r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (here) dw[j] += g[j] * v[j] * r;
+      g[j] = r * (g[j] * w[j] - v[j] * k);
+    }
+    if (here) Elem<E>::store(dx, g);
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) red[grp][d + j] = dw[j];
@@ -240,7 +300,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_any(const NormArgs a, int block
       w[i] = x.w ? (float)((const E*)x.w)[d] : 1.0f;
       q += v[i] * v[i];
     }
-    const float r = 1.0f / sqrtf(row_sum<64>(q) * inv_d + a.eps);
+    const float r = inv_rms(row_sum<64>(q) * inv_d, a.eps);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -286,23 +346,24 @@ __global__ __launch_bounds__(kBlock) void k_norm_any(const NormArgs a, int block
     part[(int64_t)blockIdx.x * a.D + e] = buf[0][e] + buf[1][e] + buf[2][e] + buf[3][e];
 }
 
-// dw: the workgroups' sums added up in order, 16 columns a workgroup, 16 rows at a time.
+// dw: the workgroups' sums added up in order, 16 columns a workgroup, 64 rows at a time.
 template <class E>
-__global__ __launch_bounds__(256) void k_norm_dw(const NormArgs a, int blocks0, int blocks1,
-                                                 const float* part) {
-  __shared__ float red[16][17];
+__global__ __launch_bounds__(1024) void k_norm_dw(const NormArgs a, int blocks0, int blocks1,
+                                                  const float* part) {
+  __shared__ float red[64][17];
   const int tiles = (a.D + 15) / 16, side = blockIdx.x / tiles;
   const int col = (blockIdx.x % tiles) * 16 + threadIdx.x % 16, r = threadIdx.x / 16;
   const int first = side ? blocks0 : 0, n = side ? blocks1 : blocks0;
   E* out = (E*)(side ? a.side[1].dw : a.side[0].dw);
   float t = 0.0f;
   if (col < a.D)
-    for (int i = r; i < n; i += 16) t += part[(int64_t)(first + i) * a.D + col];
+#pragma unroll 4
+    for (int i = r; i < n; i += 64) t += part[(int64_t)(first + i) * a.D + col];
   red[r][threadIdx.x % 16] = t;
   __syncthreads();
   if (r == 0 && col < a.D && out) {
     t = 0.0f;
-    for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
+    for (int i = 0; i < 64; ++i) t += red[i][threadIdx.x];
     out[col] = (E)t;
   }
 }
@@ -313,73 +374,62 @@ int lanes(int D) {
   return l;
 }
 
-// Heads a group takes: as many as leave the chip 16 wavefronts a compute unit.
-Split split_of(const NormArgs& a) {
-  Split sp;
-  for (int i = 0; i < 2; ++i) {
-    const NormSide& x = a.side[i];
-    const int64_t want = (int64_t)kCUs * 16 * 64 / lanes(a.D);  // groups
-    const int64_t all = (int64_t)x.rows * x.heads;
-    sp.hpg[i] = (int)std::max<int64_t>(1, std::min<int64_t>({x.heads, all / want, 8}));
-    sp.nhg[i] = std::max(1, (x.heads + sp.hpg[i] - 1) / sp.hpg[i]);
-    sp.groups[i] = (int64_t)x.rows * sp.nhg[i];
-  }
-  return sp;
+// Workgroups of both sides, in proportion to their heads: at most `most` in all
+// (the forward: what the chip holds; the backward, whose partial sums of dw each
+// cost a read: fewer).
+void blocks_of(const NormArgs& a, int64_t most, int b[2]) {
+  const int64_t per = a.vec ? kBlock / lanes(a.D) : 4;
+  int64_t want[2];
+  for (int i = 0; i < 2; ++i) want[i] = ((int64_t)a.side[i].rows * a.side[i].heads + per - 1) / per;
+  const int64_t all = want[0] + want[1];
+  for (int i = 0; i < 2; ++i) b[i] = (int)(all <= most ? want[i] : (want[i] * most + all - 1) / all);
 }
 
-void blocks_of(const NormArgs& a, int b[2]) {
-  for (int i = 0; i < 2; ++i) {
-    const int64_t n = (int64_t)a.side[i].rows * a.side[i].heads;
-    const int64_t per = a.vec ? kBlock / lanes(a.D) : 4;
-    b[i] = (int)std::min<int64_t>(kMaxPart, (n + per - 1) / per);
-  }
-}
-
-template <class E, int LR, bool INTER>
+template <class E, int LR, Pairs P>
 void launch_vec(const NormArgs& a, bool bwd, float* part, hipStream_t s) {
-  const Split sp = split_of(a);
-  constexpr int per = kBlock / LR;
-  if (!bwd) {
-    k_norm_fwd<E, LR, INTER><<<(unsigned)((sp.groups[0] + sp.groups[1] + per - 1) / per), kBlock, 0, s>>>(a, sp);
-  } else {
-    int b[2];
-    blocks_of(a, b);
-    k_norm_bwd<E, LR, INTER><<<b[0] + b[1], kBlock, 0, s>>>(a, sp, b[0], b[1], part);
-  }
+  int b[2];
+  blocks_of(a, bwd ? kBwdBlocks : kFwdBlocks, b);
+  if (bwd)
+    k_norm_bwd<E, LR, P><<<b[0] + b[1], kBlock, 0, s>>>(a, b[0], b[1], part);
+  else
+    k_norm_fwd<E, LR, P><<<b[0] + b[1], kBlock, 0, s>>>(a, b[0], b[1]);
+}
+template <class E, int LR>
+void launch_lr(const NormArgs& a, bool bwd, float* part, hipStream_t s) {
+  if (a.interleaved)
+    launch_vec<E, LR, kInside>(a, bwd, part, s);
+  else if (a.R == 8 * LR)
+    launch_vec<E, LR, kHalf>(a, bwd, part, s);
+  else
+    launch_vec<E, LR, kAway>(a, bwd, part, s);
 }
 
 template <class E>
 void launch_e(const NormArgs& a, bool bwd, float* part, hipStream_t s) {
   int b[2];
-  blocks_of(a, b);
+  blocks_of(a, bwd ? kBwdBlocks : kFwdBlocks, b);
   if (b[0] + b[1] == 0) return;
   if (!a.vec) {
     if (bwd)
       k_norm_any<E, true><<<b[0] + b[1], kBlock, 0, s>>>(a, b[0], b[1], part);
     else
       k_norm_any<E, false><<<b[0] + b[1], kBlock, 0, s>>>(a, b[0], b[1], part);
-  } else {
-    const int l = lanes(a.D);
-    if (a.interleaved) {
-      if (l == 4) launch_vec<E, 4, true>(a, bwd, part, s);
-      if (l == 8) launch_vec<E, 8, true>(a, bwd, part, s);
-      if (l == 16) launch_vec<E, 16, true>(a, bwd, part, s);
-      if (l == 32) launch_vec<E, 32, true>(a, bwd, part, s);
-    } else {
-      if (l == 4) launch_vec<E, 4, false>(a, bwd, part, s);
-      if (l == 8) launch_vec<E, 8, false>(a, bwd, part, s);
-      if (l == 16) launch_vec<E, 16, false>(a, bwd, part, s);
-      if (l == 32) launch_vec<E, 32, false>(a, bwd, part, s);
-    }
+    return;
+  }
+  switch (lanes(a.D)) {
+    case 4: launch_lr<E, 4>(a, bwd, part, s); break;
+    case 8: launch_lr<E, 8>(a, bwd, part, s); break;
+    case 16: launch_lr<E, 16>(a, bwd, part, s); break;
+    default: launch_lr<E, 32>(a, bwd, part, s); break;
   }
 }
 
 template <class E>
 void launch_dw(const NormArgs& a, float* part, hipStream_t s) {
   int b[2];
-  blocks_of(a, b);
+  blocks_of(a, kBwdBlocks, b);
   if (a.side[0].dw || a.side[1].dw)
-    k_norm_dw<E><<<2 * ((a.D + 15) / 16), 256, 0, s>>>(a, b[0], b[1], part);
+    k_norm_dw<E><<<2 * ((a.D + 15) / 16), 1024, 0, s>>>(a, b[0], b[1], part);
 }
 
 }  // namespace
@@ -393,7 +443,7 @@ hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s) {
 
 int64_t norm_bwd_bytes(const NormArgs& a) {
   int b[2];
-  blocks_of(a, b);
+  blocks_of(a, kBwdBlocks, b);
   return (int64_t)(b[0] + b[1]) * a.D * 4;
 }
 
