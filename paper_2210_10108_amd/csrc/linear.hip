@@ -94,18 +94,16 @@ __device__ __forceinline__ void finish4(const Product& p, int m, int n, float c[
   store4<VEC>((uint16_t*)p.c + m * p.cs + n, make_uint2(T::pack(c[0], c[1]), T::pack(c[2], c[3])), cnt);
 }
 
-// c[0..7] of row m, columns n..n+7, aligned rows.
+// c[0..7] of row m, columns n..n+7, aligned rows; bias and res: those 8 elements (zeros: none).
 template <class T, bool EPI>
-__device__ __forceinline__ void finish8(const Product& p, int m, int n, float c[8]) {
+__device__ __forceinline__ void finish8(const Product& p, int m, int n, float c[8], uint4 bias, uint4 res) {
   auto add = [&](const uint4 v) {
     c[0] += T::lo(v.x), c[1] += T::hi(v.x), c[2] += T::lo(v.y), c[3] += T::hi(v.y);
     c[4] += T::lo(v.z), c[5] += T::hi(v.z), c[6] += T::lo(v.w), c[7] += T::hi(v.w);
   };
   auto packed = [&] { return make_uint4(T::pack(c[0], c[1]), T::pack(c[2], c[3]), T::pack(c[4], c[5]), T::pack(c[6], c[7])); };
   if (EPI) {
-    uint4 res = make_uint4(0, 0, 0, 0);
-    if (p.res) res = *reinterpret_cast<const uint4*>((const uint16_t*)p.res + m * p.rs + n);
-    if (p.bias) add(*reinterpret_cast<const uint4*>((const uint16_t*)p.bias + n));
+    add(bias);
     if (p.z) *reinterpret_cast<uint4*>((uint16_t*)p.z + m * p.zs + n) = packed();
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = act_value(p.act, c[i]);
@@ -181,6 +179,7 @@ __global__ __launch_bounds__(256) void k_product_any(const Product p) {
 // the row so that the fragment reads cover all banks, which the lanes' addresses
 // in memory follow.  The buffer descriptor's bound gives zeros past the last row;
 // lanes past the end of a row take an offset beyond any bound.
+constexpr int WN256 = 4;
 constexpr int kBK = 64;                      // depth of a tile in LDS
 constexpr int64_t kMaxFastStride = 1 << 21;  // elements: a tile's offsets stay below 2^31 bytes
 
@@ -251,13 +250,14 @@ struct Tile {
 // 2 x 2; fragments are read one 16-deep step ahead, across the tiles' border, so
 // that the one barrier a tile falls between the last reads of a tile and the
 // last of its products.
-template <class T, bool EPI, bool AK, bool BK, int BM, int BN>
-__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(const Product p, int splits, float* part) {
-  constexpr int TM = BM / 64, TN = BN / 64;  // 32 x 32 results a wavefront
-  using TA = Tile<BM, 4, AK>;
-  using TB = Tile<BN, 4, BK>;
+template <class T, bool EPI, bool AK, bool BK, int BM, int BN, int WN>
+__global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const Product p, int splits, float* part) {
+  constexpr int NW = 2 * WN, TM = BM / 64, TN = BN / WN / 32;  // wavefronts; 32 x 32 results of one
+  using TA = Tile<BM, NW, AK>;
+  using TB = Tile<BN, NW, BK>;
   constexpr int kBuf = TA::kBytes + TB::kBytes;
-  __shared__ alignas(128) char lds[2 * kBuf];
+  constexpr int kLds = 2 * kBuf + (BN == 256 ? 8192 : 16384);  // the epilogue's need
+  __shared__ alignas(128) char lds[kLds];
 
   // tiles in the order of the XCDs, and within one XCD's run 8 rows of tiles at a
   // time, so that the tiles in flight share operands in its L2
@@ -270,14 +270,14 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(const Produc
   const int m0 = (band * 8 + in_band % height) * BM, n0 = in_band / height * BN;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave >> 1, wn = wave & 1;
+  const int wm = wave / WN, wn = wave % WN;
   const int all = (p.K + kBK - 1) / kBK, per = (all + splits - 1) / splits;
   const int t0 = min(sp * per, all), nt = min(t0 + per, all) - t0;
 
   TA a;
   TB b;
   a.init(p.a, m0, p.M, t0 * kBK, p.K, wave, lane, wm * (BM / 2));
-  b.init(p.b, n0, p.N, t0 * kBK, p.K, wave, lane, wn * (BN / 2));
+  b.init(p.b, n0, p.N, t0 * kBK, p.K, wave, lane, wn * (BN / WN));
   const uint32_t la = lds_address(lds), lb = la + TA::kBytes;
 
   floatx16 acc[TM][TN];
@@ -333,12 +333,30 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(const Produc
   }
 
   // Results by way of LDS, 32 rows of the wavefront at a time, so that a lane
-  // has 8 neighbours of a row and a row's lanes are neighbours.
-  constexpr int kRow = BN / 2 + 4, kLanes = BN / 16;
-  static_assert(4 * 32 * kRow * 4 <= 2 * kBuf, "results fit the tiles' LDS");
+  // has 8 neighbours of a row and a row's lanes are neighbours.  The residual of
+  // the next 32 rows is on its way into LDS (each lane's own pieces) meanwhile: a
+  // wavefront is alone on its SIMD and nothing else would hide its latency.
+  constexpr int kRow = BN / WN + 4, kLanes = BN / WN / 8, kStep = 64 / kLanes, kSteps = 32 / kStep;
+  static_assert(NW * (32 * kRow * 4 + 2 * kSteps * 1024) <= kLds, "results and residual fit LDS");
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kRow;
-  const int r = lane & 31, h = lane >> 5, n = n0 + wn * (BN / 2) + 8 * (lane % kLanes);
+  const char* res = lds + NW * 32 * kRow * 4 + wave * 2 * kSteps * 1024;
+  const int r = lane & 31, h = lane >> 5, n = n0 + wn * (BN / WN) + 8 * (lane % kLanes);
+  const int first = m0 + wm * (BM / 2) + lane / kLanes;  // this lane's first row
+  uint4 bias = make_uint4(0, 0, 0, 0);
+  const bool with_res = EPI && p.res && splits == 1;
+  if (EPI && p.bias && n < p.N) bias = *reinterpret_cast<const uint4*>((const uint16_t*)p.bias + n);
+  auto load_res = [&](int i) {
+    const char* base = (const char*)p.res + 2 * ((int64_t)(m0 + wm * (BM / 2) + 32 * i) * p.rs + n0 + wn * (BN / WN));
+    const u32x4 desc = descriptor(base, 0x7FFFFFFF);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(res) + (i & 1) * kSteps * 1024);
+    const uint32_t off = (uint32_t)(lane / kLanes) * (uint32_t)(2 * p.rs) + 16 * (lane % kLanes);
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+      load_to_lds(to + 1024 * k, first + 32 * i + k * kStep < p.M && n < p.N ? off + k * kStep * (uint32_t)(2 * p.rs) : kOutside, desc);
+  };
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();  // every wavefront has read its last fragments
+  if (with_res) load_res(0);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -347,19 +365,25 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(const Produc
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<floatx4*>(mine + r * kRow + 32 * j + 8 * q + 4 * h) =
             floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    if (with_res) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      if (i + 1 < TM) load_res(i + 1);
+    }
     wave_fence();
 #pragma unroll 1
-    for (int row = lane / kLanes; row < 32; row += 64 / kLanes) {
-      const int m = m0 + wm * (BM / 2) + 32 * i + row;
+    for (int k = 0; k < kSteps; ++k) {
+      const int m = first + 32 * i + k * kStep;
       if (m >= p.M || n >= p.N) continue;
-      const floatx4* from = reinterpret_cast<const floatx4*>(mine + row * kRow + 8 * (lane % kLanes));
+      const floatx4* from = reinterpret_cast<const floatx4*>(mine + (lane / kLanes + k * kStep) * kRow + 8 * (lane % kLanes));
       const floatx4 x = from[0], y = from[1];
       if (splits > 1) {
         floatx4* to = reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.N + n);
         to[0] = x, to[1] = y;
       } else {
         float c[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-        finish8<T, EPI>(p, m, n, c);
+        const uint4 add = with_res ? *reinterpret_cast<const uint4*>(res + ((i & 1) * kSteps + k) * 1024 + 16 * lane)
+                                   : make_uint4(0, 0, 0, 0);
+        finish8<T, EPI>(p, m, n, c, bias, add);
       }
     }
     wave_fence();
@@ -516,18 +540,21 @@ __global__ __launch_bounds__(256) void k_linear_dz(const LinearArgs a, uint16_t*
   }
 }
 
-// db: the row blocks' sums added up in order, 64 columns a workgroup, 4 rows at a time.
+// db: the row blocks' sums added up in order, 16 columns a workgroup, 16 rows at a time.
 template <class T>
 __global__ __launch_bounds__(256) void k_linear_db(const float* part, int blocks, int N, typename T::E* db) {
-  __shared__ float red[4][64];
-  const int c = blockIdx.x * 64 + threadIdx.x % 64, r = threadIdx.x / 64;
+  __shared__ float red[16][17];
+  const int c = blockIdx.x * 16 + threadIdx.x % 16, r = threadIdx.x / 16;
   float t = 0.0f;
   if (c < N)
-    for (int i = r; i < blocks; i += 4) t += part[(int64_t)i * N + c];
-  red[r][threadIdx.x % 64] = t;
+#pragma unroll 4
+    for (int i = r; i < blocks; i += 16) t += part[(int64_t)i * N + c];
+  red[r][threadIdx.x % 16] = t;
   __syncthreads();
-  if (r == 0 && c < N) db[c] = (typename T::E)(red[0][threadIdx.x] + red[1][threadIdx.x] +
-                                               red[2][threadIdx.x] + red[3][threadIdx.x]);
+  if (r != 0 || c >= N) return;
+  t = 0.0f;
+  for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
+  db[c] = (typename T::E)t;
 }
 
 // How a product is run: which kernel, and into how many parts its contracted
@@ -557,7 +584,8 @@ Plan plan_of(int M, int N, int K, bool fast, bool few) {
 int64_t plan_bytes(const Plan& pl, int64_t M, int64_t N) { return pl.splits > 1 ? pl.splits * M * N * 4 : 0; }
 
 bool fast_strides(const Product& p, bool AK, bool BK) {
-  return (AK ? p.a.si : p.a.sk) <= kMaxFastStride && (BK ? p.b.si : p.b.sk) <= kMaxFastStride;
+  return (AK ? p.a.si : p.a.sk) <= kMaxFastStride && (BK ? p.b.si : p.b.sk) <= kMaxFastStride &&
+         p.rs <= kMaxFastStride;
 }
 
 template <class T, bool EPI, bool AK, bool BK>
@@ -578,10 +606,10 @@ void product(const Product& p, const Plan& pl, float* part, hipStream_t s) {
       }
       break;
     case kTile128:
-      k_product<T, EPI, AK, BK, 128, 128><<<tiles(128, 128) * pl.splits, 256, 0, s>>>(p, pl.splits, part);
+      k_product<T, EPI, AK, BK, 128, 128, 2><<<tiles(128, 128) * pl.splits, 256, 0, s>>>(p, pl.splits, part);
       break;
     case kTile256:
-      k_product<T, EPI, AK, BK, 256, 256><<<tiles(256, 256), 256, 0, s>>>(p, 1, part);
+      k_product<T, EPI, AK, BK, 256, 256, WN256><<<tiles(256, 256), 128 * WN256, 0, s>>>(p, 1, part);
       break;
   }
   if (pl.splits > 1)
@@ -640,7 +668,7 @@ void backward(const LinearArgs& a, void* ws, hipStream_t s) {
     else
       k_linear_dz<T, false><<<(unsigned)n, 256, 0, s>>>(a, (uint16_t*)ws, dzs, part);
   }
-  if (a.db) k_linear_db<T><<<(a.N + 63) / 64, 256, 0, s>>>(part, blocks, a.N, (typename T::E*)a.db);
+  if (a.db) k_linear_db<T><<<(a.N + 15) / 16, 256, 0, s>>>(part, blocks, a.N, (typename T::E*)a.db);
   if (a.dx) {
     const Product p = dx_product(a, dz, dzs);
     product<T, false, true, true>(p, plan_of(p.M, p.N, p.K, a.vec && fast_strides(p, true, true), false), sums, s);

@@ -3,11 +3,12 @@
 Argument marshalling only, as in `pnerf`: every operator runs in libpnerf.so,
 torch provides device memory and the stream.  Tensors may have any strides as
 long as their last dimension is contiguous; outputs that are not passed in are
-allocated contiguous.  A call enqueues its kernels on `stream` (default: the
-device's current stream) and returns.  Outputs and workspaces that it allocates
-are torch's memory of that stream, and inputs used on another stream than the
-current one are recorded on it, so tensors may be dropped while the work is
-queued; what the streams wait for is the caller's, as everywhere in torch.
+torch.empty_like their input where they have its shape, else contiguous.  A call
+enqueues its kernels on `stream` (default: the device's current stream) and
+returns.  Outputs and workspaces that it allocates are torch's memory of that
+stream, and inputs used on another stream than the current one are recorded on
+it, so tensors may be dropped while the work is queued; what the streams wait
+for is the caller's, as everywhere in torch.
 """
 from __future__ import annotations
 
@@ -129,16 +130,27 @@ class _Call:
             t.record_stream(self.stream)
         return t.data_ptr()
 
-    def new(self, like, shape, dtype=None):
-        """An output or workspace: memory of the call's stream, which the current
-        one may read as well."""
+    def new(self, like, shape=None, dtype=None):
+        """An output (as `like`, or of another shape) or workspace: memory of the
+        call's stream, which the current one may read as well."""
         import torch
         if self.stream is None:
-            return like.new_empty(shape, dtype=dtype or self.dtype)
+            return torch.empty_like(like) if shape is None else like.new_empty(shape, dtype=dtype)
         with torch.cuda.stream(self.stream):
-            t = like.new_empty(shape, dtype=dtype or self.dtype)
+            t = torch.empty_like(like) if shape is None else like.new_empty(shape, dtype=dtype)
         t.record_stream(torch.cuda.current_stream(self.index))
         return t
+
+    def out(self, t, like, name, strides):
+        """The output t, or one like `like`; its strides go into the call's params."""
+        if t is None:
+            t = self.new(like)
+            at = t.data_ptr()
+        else:
+            at = self.tensor(t, name, like.shape)
+        if strides is not None:
+            strides[:] = t.stride()[:-1]
+        return t, at
 
     def workspace(self, like, nbytes):
         """(address, bytes, the tensor) of a workspace."""
@@ -205,10 +217,7 @@ def cross_attention(q, k, v, q_len=None, kv_len=None, kv_mask=None, scale=None, 
     import torch
     call = _Call(q, stream)
     p, qp, kp, vp = _attention(call, q, k, v, q_len, kv_len, kv_mask, scale)
-    if o is None:
-        o = call.new(q, q.shape)
-    op = call.tensor(o, "o", q.shape)
-    p.o_stride[:] = o.stride()[:3]
+    o, op = call.out(o, q, "o", p.o_stride)
     lse = lp = None
     if return_lse:
         lse = call.new(q, (p.batch, p.q_heads, p.q_rows), torch.float32)
@@ -228,15 +237,12 @@ def cross_attention_backward(do, q, k, v, o, lse, q_len=None, kv_len=None, kv_ma
     import torch
     call = _Call(q, stream)
     p, qp, kp, vp = _attention(call, q, k, v, q_len, kv_len, kv_mask, scale)
-    shape = q.shape
-    dq = call.new(q, shape) if dq is None else dq
-    dk = call.new(k, k.shape) if dk is None else dk
-    dv = call.new(k, k.shape) if dv is None else dv
-    op, dop = call.tensor(o, "o", shape), call.tensor(do, "do", shape)
+    op, dop = call.tensor(o, "o", q.shape), call.tensor(do, "do", q.shape)
     lp = call.tensor(lse, "lse", (p.batch, p.q_heads, p.q_rows), torch.float32, True)
-    dqp, dkp, dvp = call.tensor(dq, "dq", shape), call.tensor(dk, "dk", k.shape), call.tensor(dv, "dv", k.shape)
     p.o_stride[:], p.do_stride[:] = o.stride()[:3], do.stride()[:3]
-    p.dq_stride[:], p.dk_stride[:], p.dv_stride[:] = dq.stride()[:3], dk.stride()[:3], dv.stride()[:3]
+    dq, dqp = call.out(dq, q, "dq", p.dq_stride)
+    dk, dkp = call.out(dk, k, "dk", p.dk_stride)
+    dv, dvp = call.out(dv, v, "dv", p.dv_stride)
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_cross_attention_workspace(ref, 1, C.byref(n)))
@@ -283,15 +289,14 @@ def norm_rotate(q, k, q_weight, k_weight, table, q_pos, k_pos, eps: float = 1e-6
     (q_out, k_out); an output may be its input."""
     call = _Call(q, stream)
     p, qp, kp = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
-    q_out = call.new(q, q.shape) if q_out is None else q_out
-    qo, ko = call.tensor(q_out, "q_out", q.shape), None
-    p.q_out_stride[:] = q_out.stride()[:2]
-    if k is not None:
-        k_out = call.new(k, k.shape) if k_out is None else k_out
-        ko = call.tensor(k_out, "k_out", k.shape)
-        p.k_out_stride[:] = k_out.stride()[:2]
+    q_out, qo = call.out(q_out, q, "q_out", p.q_out_stride)
+    ko = None
+    if k is None:
+        k_out = None
+    else:
+        k_out, ko = call.out(k_out, k, "k_out", p.k_out_stride)
     call.run(lib().pnerf_norm_rotate, C.byref(p), qp, kp, qo, ko)
-    return q_out, k_out if k is not None else None
+    return q_out, k_out
 
 
 def norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, q_pos, k_pos,
@@ -302,25 +307,24 @@ def norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, q_pos,
     call = _Call(q, stream)
     p, qp, kp = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
 
-    def side(name, x, dy, dx, w):
-        dx = call.new(x, x.shape) if dx is None else dx
-        dw = None if w is None else call.new(w, w.shape)
-        ptrs = (call.tensor(dy, f"d{name}_out", x.shape), call.tensor(dx, f"d{name}", x.shape),
-                None if w is None else dw.data_ptr())
-        return dx, dw, ptrs
-    dq, dqw, (gq, dqp, wq) = side("q", q, dq_out, dq, q_weight)
-    p.dq_out_stride[:], p.dq_stride[:] = dq_out.stride()[:2], dq.stride()[:2]
-    dkw, (gk, dkp, wk) = None, (None, None, None)
+    gq, gk, dkp, dqw, dkw, wqp, wkp = call.tensor(dq_out, "dq_out", q.shape), *(None,) * 6
+    p.dq_out_stride[:] = dq_out.stride()[:2]
+    dq, dqp = call.out(dq, q, "dq", p.dq_stride)
+    if q_weight is not None:
+        dqw, wqp = call.out(None, q_weight, "", None)
     if k is None:
         dk = None
     else:
-        dk, dkw, (gk, dkp, wk) = side("k", k, dk_out, dk, k_weight)
-        p.dk_out_stride[:], p.dk_stride[:] = dk_out.stride()[:2], dk.stride()[:2]
+        gk = call.tensor(dk_out, "dk_out", k.shape)
+        p.dk_out_stride[:] = dk_out.stride()[:2]
+        dk, dkp = call.out(dk, k, "dk", p.dk_stride)
+        if k_weight is not None:
+            dkw, wkp = call.out(None, k_weight, "", None)
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_norm_rotate_workspace(ref, C.byref(n)))
     ws, nb, _keep = call.workspace(q, n.value)
-    call.run(_lib.pnerf_norm_rotate_backward, ref, qp, kp, gq, gk, dqp, dkp, wq, wk, ws, nb)
+    call.run(_lib.pnerf_norm_rotate_backward, ref, qp, kp, gq, gk, dqp, dkp, wqp, wkp, ws, nb)
     return dq, dk, dqw, dkw
 
 
@@ -350,9 +354,11 @@ def linear(x, w, bias=None, residual=None, activation: str = "none", y=None,
     rp = call.tensor(residual, "residual", shape)
     if residual is not None:
         p.residual_stride = residual.stride(0)
-    y = call.new(x, shape) if y is None else y
-    yp = call.tensor(y, "y", shape)
-    p.y_stride = y.stride(0)
+    if y is None:
+        y = call.new(x, shape)
+        yp, p.y_stride = y.data_ptr(), p.n
+    else:
+        yp, p.y_stride = call.tensor(y, "y", shape), y.stride(0)
     z = zp = None
     if return_preact:
         z = call.new(x, shape)
@@ -378,12 +384,11 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = Tru
     zp = call.tensor(z, "z", shape)
     if z is not None:
         p.z_stride = z.stride(0)
-    dx = call.new(x, x.shape) if dx is None else dx
-    dw = call.new(x, w.shape) if dw is None else dw
-    db = call.new(x, (p.n,)) if bias else None
-    dxp, dwp = call.tensor(dx, "dx", x.shape), call.tensor(dw, "dw", w.shape)
-    dbp = None if db is None else db.data_ptr()
+    dx, dxp = call.out(dx, x, "dx", None)
+    dw, dwp = call.out(dw, w, "dw", None)
     p.dx_stride, p.dw_stride = dx.stride(0), dw.stride(0)
+    db = call.new(x, (p.n,)) if bias else None
+    dbp = None if db is None else db.data_ptr()
     n = C.c_int64()
     ref = C.byref(p)
     _check(lib().pnerf_linear_workspace(ref, 1, C.byref(n)))
