@@ -179,7 +179,6 @@ __global__ __launch_bounds__(256) void k_product_any(const Product p) {
 // the row so that the fragment reads cover all banks, which the lanes' addresses
 // in memory follow.  The buffer descriptor's bound gives zeros past the last row;
 // lanes past the end of a row take an offset beyond any bound.
-constexpr int WN256 = 4;
 constexpr int kBK = 64;                      // depth of a tile in LDS
 constexpr int64_t kMaxFastStride = 1 << 21;  // elements: a tile's offsets stay below 2^31 bytes
 
@@ -246,10 +245,13 @@ struct Tile {
 };
 
 // BM x BN tiles, 64 deep, two of them in LDS: while the products of one run, the
-// loads of the one after the next fill the buffer just read.  Four wavefronts,
-// 2 x 2; fragments are read one 16-deep step ahead, across the tiles' border, so
-// that the one barrier a tile falls between the last reads of a tile and the
-// last of its products.
+// loads of the one after the next fill the buffer just read.  2 x WN wavefronts;
+// fragments are read one 16-deep step ahead, across the tiles' border, so that the
+// one barrier a tile falls between the last reads of a tile and the last of its
+// products.  LDS bounds the 256 x 256 tile: 192 KB read and 64 KB written for
+// 2048 cycles of products a SIMD, all of the 128 bytes a cycle.  Eight wavefronts,
+// two a SIMD, measured 1.05 to 1.12 PFLOP/s on 4096^3 (1.07 to 1.17 on 8192^3)
+// where four, which read a third less, reached 0.88 to 0.97 (0.98 to 1.08).
 template <class T, bool EPI, bool AK, bool BK, int BM, int BN, int WN>
 __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const Product p, int splits, float* part) {
   constexpr int NW = 2 * WN, TM = BM / 64, TN = BN / WN / 32;  // wavefronts; 32 x 32 results of one
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
   const int r = lane & 31, h = lane >> 5, n = n0 + wn * (BN / WN) + 8 * (lane % kLanes);
   const int first = m0 + wm * (BM / 2) + lane / kLanes;  // this lane's first row
   uint4 bias = make_uint4(0, 0, 0, 0);
-  const bool with_res = EPI && p.res && splits == 1;
+  const bool with_res = EPI && p.res && splits == 1, full = m0 + BM <= p.M && n0 + BN <= p.N;
   if (EPI && p.bias && n < p.N) bias = *reinterpret_cast<const uint4*>((const uint16_t*)p.bias + n);
   auto load_res = [&](int i) {
     const char* base = (const char*)p.res + 2 * ((int64_t)(m0 + wm * (BM / 2) + 32 * i) * p.rs + n0 + wn * (BN / WN));
@@ -366,7 +368,15 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
         *reinterpret_cast<floatx4*>(mine + r * kRow + 32 * j + 8 * q + 4 * h) =
             floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     if (with_res) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      // these 32 rows' residual is there; the stores of the 32 before, which were
+      // issued after its loads, may still be on their way (their number is known
+      // where no row or column of the tile is outside)
+      if (i > 0 && full && p.z)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kSteps) : "memory");
+      else if (i > 0 && full)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kSteps) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       if (i + 1 < TM) load_res(i + 1);
     }
     wave_fence();
@@ -511,22 +521,37 @@ __global__ __launch_bounds__(256) void k_linear_dz(const LinearArgs a, uint16_t*
   const int n = (blockIdx.x % tiles_n) * 256 + 8 * (threadIdx.x % 32);
   const int rb = blockIdx.x / tiles_n, grp = threadIdx.x / 32, cnt = min(a.N - n, 8);
   float sum[8] = {};
-  for (int i = grp; i < 64; i += 8) {
-    const int m = rb * 64 + i;
-    if (m >= a.M || cnt <= 0) break;
-    const uint4 w = load8<VEC>((const uint16_t*)a.dy + m * a.dys + n, cnt);
-    float g[8] = {T::lo(w.x), T::hi(w.x), T::lo(w.y), T::hi(w.y), T::lo(w.z), T::hi(w.z), T::lo(w.w), T::hi(w.w)};
-    if (a.act != kNone) {
-      const uint4 u = load8<VEC>((const uint16_t*)a.z + m * a.zs + n, cnt);
-      const float z[8] = {T::lo(u.x), T::hi(u.x), T::lo(u.y), T::hi(u.y), T::lo(u.z), T::hi(u.z), T::lo(u.w), T::hi(u.w)};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) g[j] *= act_slope(a.act, z[j]);
-      uint16_t* o = dz + m * dz_stride + n;
-      store4<VEC>(o, make_uint2(T::pack(g[0], g[1]), T::pack(g[2], g[3])), cnt);
-      store4<VEC>(o + 4, make_uint2(T::pack(g[4], g[5]), T::pack(g[6], g[7])), cnt - 4);
+  for (int i0 = 0; i0 < 64; i0 += 32) {  // four rows' loads at once
+    uint4 w[4], u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int m = rb * 64 + i0 + 8 * i + grp, here = m < a.M ? cnt : 0;
+      w[i] = load8<VEC>((const uint16_t*)a.dy + m * a.dys + n, here);
+      if (a.act != kNone) u[i] = load8<VEC>((const uint16_t*)a.z + m * a.zs + n, here);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] += g[j];
+    for (int i = 0; i < 4; ++i) {
+      const int m = rb * 64 + i0 + 8 * i + grp, here = m < a.M ? cnt : 0;
+      float g[8] = {T::lo(w[i].x), T::hi(w[i].x), T::lo(w[i].y), T::hi(w[i].y),
+                    T::lo(w[i].z), T::hi(w[i].z), T::lo(w[i].w), T::hi(w[i].w)};
+      if (a.act != kNone) {
+        const float z[8] = {T::lo(u[i].x), T::hi(u[i].x), T::lo(u[i].y), T::hi(u[i].y),
+                            T::lo(u[i].z), T::hi(u[i].z), T::lo(u[i].w), T::hi(u[i].w)};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] *= act_slope(a.act, z[j]);
+        const uint4 o = make_uint4(T::pack(g[0], g[1]), T::pack(g[2], g[3]), T::pack(g[4], g[5]), T::pack(g[6], g[7]));
+        uint16_t* to = dz + m * dz_stride + n;
+        if (VEC) {
+          if (here > 0) *reinterpret_cast<uint4*>(to) = o;
+        } else {
+          store4<false>(to, make_uint2(o.x, o.y), here);
+          store4<false>(to + 4, make_uint2(o.z, o.w), here - 4);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += j < here ? g[j] : 0.0f;
+    }
   }
   if (!part) return;
 #pragma unroll
@@ -609,7 +634,7 @@ void product(const Product& p, const Plan& pl, float* part, hipStream_t s) {
       k_product<T, EPI, AK, BK, 128, 128, 2><<<tiles(128, 128) * pl.splits, 256, 0, s>>>(p, pl.splits, part);
       break;
     case kTile256:
-      k_product<T, EPI, AK, BK, 256, 256, WN256><<<tiles(256, 256), 128 * WN256, 0, s>>>(p, 1, part);
+      k_product<T, EPI, AK, BK, 256, 256, 4><<<tiles(256, 256), 512, 0, s>>>(p, 1, part);
       break;
   }
   if (pl.splits > 1)
