@@ -157,38 +157,76 @@ struct Place {
 
 // Many rows: four wavefronts of 32 rows share the tiles, two of them in LDS: the
 // loads of the next run while the products of one do.  One barrier a tile.
-template <class T, int DP>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
+// KS = 2: two such groups with the same rows take the tiles in turn, each with its
+// own LDS, and join at the end.  Where there are fewer workgroups than the chip
+// holds twice over, that puts a second wavefront on every SIMD (1024 rows, 1200
+// keys, 2 x 16 heads of 64, one workgroup a CU: HYP1 us with one group, HYP2 with two).
+template <class T, int DP, int KS>
+__global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_fwd(const AttnArgs a) {
   using Tile = RowTile<DP, 4>;
-  __shared__ uint4 lds[2][2 * Tile::kPieces];  // keys, then values
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  __shared__ uint4 lds[KS][2][2 * Tile::kPieces];  // keys, then values
+  const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int wave = all_waves & 3, grp = all_waves >> 2;
   const Place at(a, 128, wave * 32 + (lane & 31));
   const Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, wave, lane);
   const Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, wave, lane);
   Rows<T, DP> x;
   x.template init<true>(at.q, at.ok, a.D, h);
-  const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[1])};
-  auto load = [&](int t, uint64_t vm) {
-    kt.load(to[t & 1], t, at.nk, vm, lane);
-    vt.load(to[t & 1] + 16 * Tile::kPieces, t, at.nk, vm, lane);
+  const uint32_t to[2] = {lds_address(lds[grp][0]), lds_address(lds[grp][1])};
+  auto load = [&](int buf, int t, uint64_t vm) {
+    kt.load(to[buf], t, at.nk, vm, lane);
+    vt.load(to[buf] + 16 * Tile::kPieces, t, at.nk, vm, lane);
   };
   uint64_t vm = 0, vm_next = 0;
   bool allowed = false;  // key `lane` of the tile after the next
-  if (at.t0 < at.t1) {
-    vm_next = __ballot(at.allowed(at.t0 * kBN + lane));
-    load(at.t0, vm_next);
-    allowed = at.allowed((at.t0 + 1) * kBN + lane);
+  int t = at.t0 + grp;
+  if (t < at.t1) {
+    vm_next = __ballot(at.allowed(t * kBN + lane));
+    load(0, t, vm_next);
+    allowed = at.allowed((t + KS) * kBN + lane);
   }
-  for (int t = at.t0; t < at.t1; ++t) {
+  const int rounds = (at.t1 - at.t0 + KS - 1) / KS;  // the same for both groups: they share the barrier
+  for (int i = 0; i < rounds; ++i, t += KS) {
+    const int buf = i & 1;
     wait_loads();
     __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
     vm = vm_next;
     vm_next = __ballot(allowed);
-    if (t + 1 < at.t1) {
-      load(t + 1, vm_next);
-      allowed = at.allowed((t + 2) * kBN + lane);
+    if (t + KS < at.t1) {
+      load(buf ^ 1, t + KS, vm_next);
+      allowed = at.allowed((t + 2 * KS) * kBN + lane);
     }
-    x.tile(lds[t & 1], lds[t & 1] + Tile::kPieces, vm, a.c, lane, [] {});
+    if (t < at.t1) x.tile(lds[grp][buf], lds[grp][buf] + Tile::kPieces, vm, a.c, lane, [] {});
+  }
+  if constexpr (KS == 2) {
+    static_assert(4 * 64 * (DP / 8 * 16 + 8) <= sizeof(lds), "a group's sums fit LDS");
+    floatx4* red = reinterpret_cast<floatx4*>(lds) + wave * (DP / 8) * 64 + lane;
+    floatx2* red_ml = reinterpret_cast<floatx2*>(reinterpret_cast<floatx4*>(lds) + 4 * (DP / 8) * 64) + wave * 64 + lane;
+    wait_reads();
+    __syncthreads();
+    if (grp == 1) {
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          red[(4 * d + i) * 64] = floatx4{x.o[d][4 * i], x.o[d][4 * i + 1], x.o[d][4 * i + 2], x.o[d][4 * i + 3]};
+      *red_ml = floatx2{x.m, x.l};
+    }
+    __syncthreads();
+    if (grp == 1) return;
+    const floatx2 ml = *red_ml;
+    const float m = fmaxf(x.m, ml[0]), base = m == -INFINITY ? 0.0f : m;
+    const float f0 = __builtin_amdgcn_exp2f(x.m - base), f1 = __builtin_amdgcn_exp2f(ml[0] - base);
+    x.m = m;
+    x.l = x.l * f0 + ml[1] * f1;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const floatx4 o = red[(4 * d + i) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.o[d][4 * i + j] = x.o[d][4 * i + j] * f0 + o[j] * f1;
+      }
   }
   x.close(at.ok);
   if (at.row >= a.M) return;
@@ -356,8 +394,10 @@ void launch(const AttnArgs& a, hipStream_t s) {
     k_attn_any<T, DP><<<n, 256, 0, s>>>(a);
   else if (few)
     k_attn_few<T, DP><<<n, 256, 0, s>>>(a);
+  else if (two_groups(n, a))
+    k_attn_fwd<T, DP, 2><<<n, 512, 0, s>>>(a);
   else
-    k_attn_fwd<T, DP><<<n, 256, 0, s>>>(a);
+    k_attn_fwd<T, DP, 1><<<n, 256, 0, s>>>(a);
   if (a.splits > 1) k_attn_join<T, DP><<<(unsigned)(a.B * a.Hkv * a.M), 256, 0, s>>>(a);
 }
 

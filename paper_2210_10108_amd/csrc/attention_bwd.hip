@@ -54,12 +54,13 @@ __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
 
 // dq: four wavefronts of 32 rows share the tiles of keys and values, two of them
 // in LDS (FAST; else one, by way of registers).  As in the forward kernel the row
-// is the column of every product: its lse and delta are a lane's own.
-template <class T, int DP, bool FAST>
-__global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits, float* part) {
+// is the column of every product: its lse and delta are a lane's own; and KS = 2
+// groups of wavefronts take the tiles in turn where workgroups are few.
+template <class T, int DP, bool FAST, int KS>
+__global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, int splits, float* part) {
   constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32;
   using Tile = RowTile<DP, 4>;
-  __shared__ uint4 lds[FAST ? 2 : 1][2 * Tile::kPieces];  // keys, then values
+  __shared__ uint4 lds[KS][FAST ? 2 : 1][2 * Tile::kPieces];  // keys, then values
 
   const int tiles_m = (a.M + 127) / 128;
   int id = xcd_order(blockIdx.x, gridDim.x);
@@ -68,7 +69,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
   const int sp = id % splits;
   id /= splits;
   const int g = id % a.Hkv, b = id / a.Hkv;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = all_waves & 3, grp = all_waves >> 2;
   const int r = lane & 31, h = lane >> 5;
   const int row = mt * 128 + wave * 32 + r;
   const int qi = row / a.G, head = g * a.G + row % a.G;
@@ -102,35 +104,39 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
 
   const Tile kt(a.k, b * a.ks[0] + g * a.ks[2], a.ks[1], a.D, wave, lane);
   const Tile vt(a.v, b * a.vs[0] + g * a.vs[2], a.vs[1], a.D, wave, lane);
-  const uint32_t to[2] = {lds_address(lds[0]), lds_address(lds[FAST])};
-  auto load = [&](int t, uint64_t vm) {
-    kt.load(to[t & 1], t, nk, vm, lane);
-    vt.load(to[t & 1] + 16 * Tile::kPieces, t, nk, vm, lane);
+  const uint32_t to[2] = {lds_address(lds[grp][0]), lds_address(lds[grp][FAST])};
+  auto load = [&](int buf, int t, uint64_t vm) {
+    kt.load(to[buf], t, nk, vm, lane);
+    vt.load(to[buf] + 16 * Tile::kPieces, t, nk, vm, lane);
   };
   uint64_t vm_next = 0;
   bool allowed = false;  // key `lane` of the tile after the next
-  if (FAST && t0 < t1) {
-    vm_next = __ballot(may_read(t0 * kBN + lane));
-    load(t0, vm_next);
-    allowed = may_read((t0 + 1) * kBN + lane);
+  int t = t0 + grp;
+  if (FAST && t < t1) {
+    vm_next = __ballot(may_read(t * kBN + lane));
+    load(0, t, vm_next);
+    allowed = may_read((t + KS) * kBN + lane);
   }
-  for (int t = t0; t < t1; ++t) {
-    const uint4 *sk = lds[FAST ? t & 1 : 0], *sv = sk + Tile::kPieces;
+  const int rounds = (t1 - t0 + KS - 1) / KS;  // the same for both groups: they share the barrier
+  for (int round = 0; round < rounds; ++round, t += KS) {
+    const int buf = FAST ? round & 1 : 0;
+    const uint4 *sk = lds[grp][buf], *sv = sk + Tile::kPieces;
     uint64_t vm;
     if (FAST) {
       wait_loads();
       __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
       vm = vm_next;
       vm_next = __ballot(allowed);
-      if (t + 1 < t1) {
-        load(t + 1, vm_next);
-        allowed = may_read((t + 2) * kBN + lane);
+      if (t + KS < t1) {
+        load(buf ^ 1, t + KS, vm_next);
+        allowed = may_read((t + 2 * KS) * kBN + lane);
       }
+      if (t >= t1) break;  // the last round has no tile for this group
     } else {
       vm = __ballot(may_read(t * kBN + lane));
       __syncthreads();
-      copy_tile<DP>(lds[0], a.k, a.ks, b, g, a.D, t, vm);
-      copy_tile<DP>(lds[0] + Tile::kPieces, a.v, a.vs, b, g, a.D, t, vm);
+      copy_tile<DP>(lds[0][0], a.k, a.ks, b, g, a.D, t, vm);
+      copy_tile<DP>(lds[0][0] + Tile::kPieces, a.v, a.vs, b, g, a.D, t, vm);
       __syncthreads();
     }
     auto first = [&](int n, floatx16& s, floatx16& dp) {
@@ -182,6 +188,28 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a, int splits
           acc[d] = T::mma(tr_frag<CH>(sk, 32 * n + 16 * k, 32 * d, lane), f, acc[d]);
       }
     }
+  }
+  if constexpr (KS == 2) {
+    static_assert(4 * 64 * (DP / 8) * 16 <= sizeof(lds), "a group's sums fit LDS");
+    floatx4* red = reinterpret_cast<floatx4*>(lds) + wave * (DP / 8) * 64 + lane;
+    wait_reads();
+    __syncthreads();
+    if (grp == 1)
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          red[(4 * d + i) * 64] = floatx4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+    __syncthreads();
+    if (grp == 1) return;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const floatx4 o = red[(4 * d + i) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[d][4 * i + j] += o[j];
+      }
   }
   if (row >= a.M) return;
   if (splits > 1) {
@@ -396,7 +424,14 @@ void launch(const AttnArgs& a, float* part_q, float* part_kv, hipStream_t s) {
     k_attn_stat<T, DP, FAST><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(a);
     const int ns = dq_splits(a);
     const int64_t n = (((int64_t)a.M + 127) / 128) * ns * a.Hkv * a.B;
-    k_attn_dq<T, DP, FAST><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
+    if constexpr (FAST) {
+      if (two_groups(n, a))
+        k_attn_dq<T, DP, true, 2><<<(unsigned)n, 512, 0, s>>>(a, ns, part_q);
+      else
+        k_attn_dq<T, DP, true, 1><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
+    } else {
+      k_attn_dq<T, DP, false, 1><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
+    }
     if (ns > 1) k_attn_sum<T, DP, false, FAST><<<(unsigned)((rows * DP / 4 + 255) / 256), 256, 0, s>>>(a, ns, part_q);
   }
   if (keys) {

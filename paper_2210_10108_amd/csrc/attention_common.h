@@ -13,6 +13,12 @@ inline int padded(int D) { return D <= 64 ? 64 : 128; }  // head width in the ke
 inline bool fast_loads(const AttnArgs& a) {
   return a.vec && a.ks[1] <= kMaxTileStride && a.vs[1] <= kMaxTileStride;
 }
+// Whether two groups of wavefronts share a workgroup's rows (KS = 2): where the
+// workgroups are fewer than the chip holds of that kind (by LDS, one a compute
+// unit at the wide head).
+inline bool two_groups(int64_t workgroups, const AttnArgs& a) {
+  return workgroups <= (padded(a.D) == 128 ? 1 : 2) * kCUs && a.Sk > 2 * kBN;
+}
 
 #if defined(__HIP_DEVICE_COMPILE__) || defined(PNERF_LAYERS_DEVICE)
 // The bits of row r that are xored into the position of its 16-byte chunks: 8
