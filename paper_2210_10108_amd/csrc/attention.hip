@@ -29,8 +29,8 @@ namespace {
 template <class T, int DP>
 struct Rows {
   uint4 qf[DP / 16];
-  floatx16 o[DP / 32];
-  float m, l;
+  floatx16 o[DP / 32], s[2];
+  float m, l, top;
 
   template <bool VEC>
   __device__ __forceinline__ void init(const uint16_t* q, bool ok, int D, int h) {
@@ -44,13 +44,11 @@ struct Rows {
     m = -INFINITY, l = 0.0f;
   }
 
-  // One tile; vm: its keys that may be read; before_values runs between the two products.
-  template <class F>
-  __device__ __forceinline__ void tile(const uint4* sk, const uint4* sv, uint64_t vm, float c, int lane,
-                                       F before_values) {
+  // The scores of one tile, in units of 1 / c; vm: its keys that may be read.  Sets
+  // `top`, the maximum with them.
+  __device__ __forceinline__ void scores(const uint4* sk, uint64_t vm, float c, int lane) {
     constexpr int CH = DP / 8;
     const int r = lane & 31, h = lane >> 5;
-    floatx16 s[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       s[n] = floatx16{};
@@ -66,7 +64,6 @@ struct Rows {
           if (!((w >> (8 * (i / 4) + i % 4)) & 1)) s[n][i] = -INFINITY;
       }
     }
-    before_values();
     float mx = -INFINITY;
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -74,16 +71,21 @@ struct Rows {
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
     float m0, m1;
     halves(mx, m0, m1);
-    // m may lag behind the maximum by 8 (p up to 2^8, exact in no other way than
-    // with it): the sums are rescaled a few times a pass, not in most tiles
-    const float mn = fmaxf(m, c * fmaxf(m0, m1));
-    if (__any(mn > m + 8.0f)) {
-      const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
-      m = mn;
-      l *= alpha;
+    top = fmaxf(m, c * fmaxf(m0, m1));
+  }
+  // m may lag behind the maximum by 8 (p is then up to 2^8, and as exact as with
+  // it): the sums are rescaled a few times a pass, not in most tiles.
+  __device__ __forceinline__ bool grown() const { return __any(top > m + 8.0f); }
+  __device__ __forceinline__ void rescale() {
+    const float alpha = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    m = top;
+    l *= alpha;
 #pragma unroll
-      for (int i = 0; i < DP / 32; ++i) o[i] *= alpha;
-    }
+    for (int i = 0; i < DP / 32; ++i) o[i] *= alpha;
+  }
+  // Adds the tile whose scores are there.
+  __device__ __forceinline__ void add(const uint4* sv, float c, int lane) {
+    constexpr int CH = DP / 8;
     const float base = m == -INFINITY ? 0.0f : m;  // no allowed key yet
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -97,6 +99,21 @@ struct Rows {
       const uint4 pf = pack8<T>(s[n / 2], 8 * (n % 2));
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) o[d] = T::mma(tr_frag<CH>(sv, 16 * n, 32 * d, lane), pf, o[d]);
+    }
+  }
+  // All tiles: next() makes the following one's scores, false where there is none;
+  // values() is where its values are.  (The rescaling stands outside the inner
+  // loop: in a branch of it the sums, tuples of registers, would be copied on the
+  // path that does not take it.)
+  template <class N, class V>
+  __device__ __forceinline__ void run(float c, int lane, N next, V values) {
+    bool more = next();
+    while (more) {
+      rescale();
+      do {
+        add(values(), c, lane);
+        more = next();
+      } while (more && !grown());
     }
   }
 
@@ -186,18 +203,28 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_fwd(const AttnArgs a)
     allowed = at.allowed((t + KS) * kBN + lane);
   }
   const int rounds = (at.t1 - at.t0 + KS - 1) / KS;  // the same for both groups: they share the barrier
-  for (int i = 0; i < rounds; ++i, t += KS) {
-    const int buf = i & 1;
-    wait_loads();
-    __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
-    vm = vm_next;
-    vm_next = __ballot(allowed);
-    if (t + KS < at.t1) {
-      load(buf ^ 1, t + KS, vm_next);
-      allowed = at.allowed((t + 2 * KS) * kBN + lane);
-    }
-    if (t < at.t1) x.tile(lds[grp][buf], lds[grp][buf] + Tile::kPieces, vm, a.c, lane, [] {});
-  }
+  int round = 0;
+  x.run(
+      a.c, lane,
+      [&] {
+        if (round == rounds) return false;
+        const int buf = round & 1;
+        wait_loads();
+        __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
+        vm = vm_next;
+        vm_next = __ballot(allowed);
+        const bool here = t < at.t1;  // the last round may have no tile for the second group
+        t += KS;
+        if (t < at.t1) {
+          load(buf ^ 1, t, vm_next);
+          allowed = at.allowed((t + KS) * kBN + lane);
+        }
+        if (!here) return false;
+        x.scores(lds[grp][buf], vm, a.c, lane);
+        ++round;
+        return true;
+      },
+      [&] { return lds[grp][(round - 1) & 1] + Tile::kPieces; });
   if constexpr (KS == 2) {
     static_assert(4 * 64 * (DP / 8 * 16 + 8) <= sizeof(lds), "a group's sums fit LDS");
     floatx4* red = reinterpret_cast<floatx4*>(lds) + wave * (DP / 8) * 64 + lane;
@@ -253,30 +280,37 @@ __global__ __launch_bounds__(256) void k_attn_few(const AttnArgs a) {
   x.template init<true>(at.q, at.ok, a.D, h);
   uint4 *sk = lds[wave], *sv = sk + Tile::kPieces;
   const uint32_t to_k = lds_address(sk), to_v = lds_address(sv);
-  int t = at.t0 + wave;
-  uint64_t vm = 0;
-  bool allowed = false;
+  int t = at.t0 + wave;    // of the next scores
+  uint64_t vm_next = 0;    // its keys that may be read
+  bool allowed = false, first = true;
   if (t < at.t1) {
-    vm = __ballot(at.allowed(t * kBN + lane));
-    kt.load(to_k, t, at.nk, vm, lane);
-    vt.load(to_v, t, at.nk, vm, lane);
+    vm_next = __ballot(at.allowed(t * kBN + lane));
+    kt.load(to_k, t, at.nk, vm_next, lane);
+    vt.load(to_v, t, at.nk, vm_next, lane);
     allowed = at.allowed((t + 4) * kBN + lane);
   }
-  for (; t < at.t1; t += 4) {
-    wait_loads();
-    const uint64_t vm_next = __ballot(allowed);
-    const bool more = t + 4 < at.t1;
-    x.tile(sk, sv, vm, a.c, lane, [&] {
-      wait_reads();
-      if (more) {
-        kt.load(to_k, t + 4, at.nk, vm_next, lane);
-        allowed = at.allowed((t + 8) * kBN + lane);
-      }
-    });
-    wait_reads();
-    if (more) vt.load(to_v, t + 4, at.nk, vm_next, lane);
-    vm = vm_next;
-  }
+  x.run(
+      a.c, lane,
+      [&] {
+        if (!first) {
+          wait_reads();  // the values before have been used
+          if (t < at.t1) vt.load(to_v, t, at.nk, vm_next, lane);
+        }
+        if (t >= at.t1) return false;
+        first = false;
+        wait_loads();
+        const uint64_t vm = vm_next;
+        vm_next = __ballot(allowed);
+        x.scores(sk, vm, a.c, lane);
+        wait_reads();
+        t += 4;
+        if (t < at.t1) {
+          kt.load(to_k, t, at.nk, vm_next, lane);
+          allowed = at.allowed((t + 4) * kBN + lane);
+        }
+        return true;
+      },
+      [&] { return sv; });
 
   // the wavefronts' sums at the largest of their maxima
   __syncthreads();
@@ -326,14 +360,21 @@ __global__ __launch_bounds__(256) void k_attn_any(const AttnArgs a) {
   const Place at(a, 128, wave * 32 + (lane & 31));
   Rows<T, DP> x;
   x.template init<false>(at.q, at.ok, a.D, h);
-  for (int t = at.t0; t < at.t1; ++t) {
-    const uint64_t vm = __ballot(at.allowed(t * kBN + lane));
-    __syncthreads();
-    copy_tile<DP>(sk, a.k, a.ks, at.b, at.g, a.D, t, vm);
-    copy_tile<DP>(sv, a.v, a.vs, at.b, at.g, a.D, t, vm);
-    __syncthreads();
-    x.tile(sk, sv, vm, a.c, lane, [] {});
-  }
+  int t = at.t0;
+  x.run(
+      a.c, lane,
+      [&] {
+        if (t >= at.t1) return false;
+        const uint64_t vm = __ballot(at.allowed(t * kBN + lane));
+        __syncthreads();
+        copy_tile<DP>(sk, a.k, a.ks, at.b, at.g, a.D, t, vm);
+        copy_tile<DP>(sv, a.v, a.vs, at.b, at.g, a.D, t, vm);
+        __syncthreads();
+        x.scores(sk, vm, a.c, lane);
+        ++t;
+        return true;
+      },
+      [&] { return sv; });
   x.close(at.ok);
   if (at.row >= a.M) return;
   if (a.splits > 1)

@@ -34,8 +34,20 @@ __device__ __forceinline__ int swz(int r, int c) {
 __device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
   return len ? min(max(len[b], 0), most) : most;
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// Waits: for all loads (into LDS and registers) and LDS accesses; for LDS accesses.
+// By the builtin, which the compiler takes into account: after a wait that it does
+// not know it would wait again for its own earlier loads, at their first use, and
+// with them for the loads into LDS that were issued since.
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_reads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
 
 // The loads of tiles of N rows (keys, values, or the query rows of one head) into
 // LDS, by NW wavefronts.
