@@ -144,7 +144,7 @@ pnerf_status pnerf_norm_rotate_backward(const pnerf_norm_rotate_params* params, 
  * residual is dy.  z may be NULL when activation is 0; dx, dw and db may each be
  * NULL (not wanted).
  *
- * Requires 0 <= m, 1 <= n, k, each at most 2^30, and m * n, m * k, k * n at most 2^35;
+ * Requires 0 <= m, 1 <= n, k, each at most 2^30, and m * n, m * k, k * n at most 2^34;
  * dtype PNERF_F16 or PNERF_BF16. */
 #define PNERF_ACT_NONE 0
 #define PNERF_ACT_RELU 1 /* derivative 0 at 0 */

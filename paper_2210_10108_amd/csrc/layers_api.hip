@@ -213,9 +213,9 @@ pnerf_status linear_args(const pnerf_linear_params* p, LinearArgs* out) {
     return fail(PNERF_ERR_INVALID_ARG, "activation=%d outside 0..3", p->activation);
   if (p->m < 0 || p->n < 1 || p->k < 1)
     return fail(PNERF_ERR_INVALID_ARG, "m=%d must be >= 0, n=%d and k=%d >= 1", p->m, p->n, p->k);
-  const int64_t m = p->m, n = p->n, k = p->k, most = (int64_t)1 << 35;
+  const int64_t m = p->m, n = p->n, k = p->k, most = (int64_t)1 << 34;
   if (std::max({m, n, k}) > (1 << 30) || m * n > most || m * k > most || k * n > most)
-    return fail(PNERF_ERR_CAPACITY, "m=%d n=%d k=%d: a size exceeds 2^30 or a product of two 2^35", p->m, p->n, p->k);
+    return fail(PNERF_ERR_CAPACITY, "m=%d n=%d k=%d: a size exceeds 2^30 or a product of two 2^34", p->m, p->n, p->k);
   LinearArgs a = {};
   a.dtype = p->dtype, a.act = p->activation, a.M = p->m, a.N = p->n, a.K = p->k;
   a.xs = p->x_stride, a.ws = p->w_stride, a.rs = p->residual_stride, a.ys = p->y_stride, a.zs = p->z_stride;
@@ -334,11 +334,9 @@ pnerf_status pnerf_linear(const pnerf_linear_params* p, const void* x, const voi
                      {"residual", residual, 2, {a.M, a.N}, {a.rs, 1}},
                      {"y", y, 2, {a.M, a.N}, {a.ys, 1}},
                      {"z", z, 2, {a.M, a.N}, {a.zs, 1}}};
-  a.vec = a.N % 8 == 0 && a.K % 8 == 0 && aligned(bias, 16);
   for (int i = 0; i < 5; ++i) {
     if ((i == 2 || i == 4) && !t[i].p) continue;
     TRY(check_view(t[i], 2, i >= 3));
-    a.vec = a.vec && rows_aligned(t[i], 2);
   }
   if (!aligned(bias, 2)) return fail(PNERF_ERR_INVALID_ARG, "bias is not aligned to its elements");
   TRY(check_workspace(workspace, workspace_bytes, linear_fwd_bytes(a)));
@@ -354,14 +352,12 @@ pnerf_status pnerf_linear_backward(const pnerf_linear_params* p, const void* x, 
   const View t[6] = {{"x", x, 2, {a.M, a.K}, {a.xs, 1}},   {"w", w, 2, {a.K, a.N}, {a.ws, 1}},
                      {"z", z, 2, {a.M, a.N}, {a.zs, 1}},   {"dy", dy, 2, {a.M, a.N}, {a.dys, 1}},
                      {"dx", dx, 2, {a.M, a.K}, {a.dxs, 1}}, {"dw", dw, 2, {a.K, a.N}, {a.dws, 1}}};
-  a.vec = a.N % 8 == 0 && a.K % 8 == 0;
   for (int i = 0; i < 6; ++i) {
     if (i == 0 && !dw) continue;  // x is read for dw alone, w for dx alone
     if (i == 1 && !dx) continue;
     if (i == 2 && a.act == PNERF_ACT_NONE) continue;
     if (i >= 4 && !t[i].p) continue;
     TRY(check_view(t[i], 2, i >= 4));
-    a.vec = a.vec && rows_aligned(t[i], 2);
   }
   if (!aligned(db, 2)) return fail(PNERF_ERR_INVALID_ARG, "db is not aligned to its elements");
   a.x = x, a.w = w, a.z = (void*)z, a.dy = dy, a.dx = dx, a.dw = dw, a.db = db;

@@ -68,7 +68,6 @@ struct LinearArgs {
   void *y, *z;            // forward: z is written; backward: z is read
   void *dx, *dw, *db;
   int64_t xs, ws, rs, ys, zs, dys, dxs, dws;
-  int vec;                // every row of every tensor starts on 16 bytes; N % 8 == 0 and K % 8 == 0
 };
 int64_t linear_fwd_bytes(const LinearArgs& a);
 hipError_t launch_linear_fwd(const LinearArgs& a, void* ws, hipStream_t s);

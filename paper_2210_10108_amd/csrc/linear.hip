@@ -64,6 +64,8 @@ struct Product {
   Operand a, b;  // rows of A (i = m), columns of B (i = n)
   void* c;
   int64_t cs;
+  int vec;       // rows of 8 elements of C and of the epilogue's tensors start on 16 bytes, N % 8 == 0
+  int row;       // N rounded up to 8: a row of the parts' sums
   // epilogue of the forward product
   int act;
   const void *bias, *res;
@@ -72,29 +74,45 @@ struct Product {
   int64_t zs;
 };
 
-// c[0..3] of row m, columns n..n+3: the epilogue.
-template <class T, bool EPI, bool VEC>
-__device__ __forceinline__ void finish4(const Product& p, int m, int n, float c[4]) {
+// c[0..n-1] of row m, columns n0.. (W of them, at most 8): the epilogue, element
+// by element.
+template <class T, bool EPI, int W>
+__device__ __forceinline__ void finish_any(const Product& p, int m, int n0, float c[W]) {
   using E = typename T::E;
-  const int cnt = min(p.N - n, 4);
-  if (EPI) {
-    if (p.bias)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < cnt) c[i] += (float)((const E*)p.bias)[n + i];
-    if (p.z)
-      store4<VEC>((uint16_t*)p.z + m * p.zs + n, make_uint2(T::pack(c[0], c[1]), T::pack(c[2], c[3])), cnt);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = act_value(p.act, c[i]);
-    if (p.res)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < cnt) c[i] += (float)((const E*)p.res)[m * p.rs + n + i];
+  for (int i = 0; i < W; ++i) {
+    if (n0 + i >= p.N) break;
+    float v = c[i];
+    if (EPI) {
+      if (p.bias) v += (float)((const E*)p.bias)[n0 + i];
+      if (p.z) ((E*)p.z)[m * p.zs + n0 + i] = (E)v;
+      v = act_value(p.act, v);
+      if (p.res) v += (float)((const E*)p.res)[m * p.rs + n0 + i];
+    }
+    ((E*)p.c)[m * p.cs + n0 + i] = (E)v;
   }
-  store4<VEC>((uint16_t*)p.c + m * p.cs + n, make_uint2(T::pack(c[0], c[1]), T::pack(c[2], c[3])), cnt);
 }
 
-// c[0..7] of row m, columns n..n+7, aligned rows; bias and res: those 8 elements (zeros: none).
+// c[0..3] of row m, columns n..n+3: the epilogue.
+template <class T, bool EPI>
+__device__ __forceinline__ void finish4(const Product& p, int m, int n, float c[4]) {
+  if (!p.vec) return finish_any<T, EPI, 4>(p, m, n, c);
+  auto add = [&](const void* q) {
+    const uint2 v = *reinterpret_cast<const uint2*>(q);
+    c[0] += T::lo(v.x), c[1] += T::hi(v.x), c[2] += T::lo(v.y), c[3] += T::hi(v.y);
+  };
+  auto put = [&](void* q) { *reinterpret_cast<uint2*>(q) = make_uint2(T::pack(c[0], c[1]), T::pack(c[2], c[3])); };
+  if (EPI) {
+    if (p.bias) add((const uint16_t*)p.bias + n);
+    if (p.z) put((uint16_t*)p.z + m * p.zs + n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = act_value(p.act, c[i]);
+    if (p.res) add((const uint16_t*)p.res + m * p.rs + n);
+  }
+  put((uint16_t*)p.c + m * p.cs + n);
+}
+
+// c[0..7] of row m, columns n..n+7, where p.vec; bias and res: those 8 elements (zeros: none).
 template <class T, bool EPI>
 __device__ __forceinline__ void finish8(const Product& p, int m, int n, float c[8], uint4 bias, uint4 res) {
   auto add = [&](const uint4 v) {
@@ -169,7 +187,7 @@ __global__ __launch_bounds__(256) void k_product_any(const Product p) {
   for (int i = 0; i < 4; ++i) {
     const int n = n0 + 32 * (wave & 1) + 8 * i + 4 * h;
     float c[4] = {acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
-    if (n < p.N) finish4<T, EPI, false>(p, m, n, c);
+    if (n < p.N) finish_any<T, EPI, 4>(p, m, n, c);
   }
 }
 
@@ -203,7 +221,7 @@ struct Tile {
     base = (const char*)o.p + 2 * (i0 * o.si + k0 * o.sk);
     row_bytes = 2 * (KC ? o.si : o.sk);
     rows = KC ? most - i0 : K - k0;
-    inner = KC ? K - k0 : most - i0;
+    inner = ((KC ? K - k0 : most - i0) + 7) & ~7;  // what a row holds past its end is zeros, to whole chunks
     const int p = wave * 64 + lane, r = p / kChunks;
     chunk = (p % kChunks) ^ (KC ? r & 7 : (r & 3) << 1);
     off = (uint32_t)(r * row_bytes + 16 * chunk);
@@ -345,8 +363,8 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
   const int r = lane & 31, h = lane >> 5, n = n0 + wn * (BN / WN) + 8 * (lane % kLanes);
   const int first = m0 + wm * (BM / 2) + lane / kLanes;  // this lane's first row
   uint4 bias = make_uint4(0, 0, 0, 0);
-  const bool with_res = EPI && p.res && splits == 1, full = m0 + BM <= p.M && n0 + BN <= p.N;
-  if (EPI && p.bias && n < p.N) bias = *reinterpret_cast<const uint4*>((const uint16_t*)p.bias + n);
+  const bool with_res = EPI && p.res && p.vec && splits == 1, full = m0 + BM <= p.M && n0 + BN <= p.N;
+  if (EPI && p.bias && p.vec && n < p.N) bias = *reinterpret_cast<const uint4*>((const uint16_t*)p.bias + n);
   auto load_res = [&](int i) {
     const char* base = (const char*)p.res + 2 * ((int64_t)(m0 + wm * (BM / 2) + 32 * i) * p.rs + n0 + wn * (BN / WN));
     const u32x4 desc = descriptor(base, 0x7FFFFFFF);
@@ -387,10 +405,14 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
       const floatx4* from = reinterpret_cast<const floatx4*>(mine + (lane / kLanes + k * kStep) * kRow + 8 * (lane % kLanes));
       const floatx4 x = from[0], y = from[1];
       if (splits > 1) {
-        floatx4* to = reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.N + n);
+        floatx4* to = reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.row + n);
         to[0] = x, to[1] = y;
       } else {
         float c[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        if (!p.vec) {
+          finish_any<T, EPI, 8>(p, m, n, c);
+          continue;
+        }
         const uint4 add = with_res ? *reinterpret_cast<const uint4*>(res + ((i & 1) * kSteps + k) * 1024 + 16 * lane)
                                    : make_uint4(0, 0, 0, 0);
         finish8<T, EPI>(p, m, n, c, bias, add);
@@ -404,13 +426,14 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
 // elements of a row a thread.
 template <class T, bool EPI>
 __global__ __launch_bounds__(256) void k_product_join(const Product p, int splits, const float* part) {
-  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (e >= (int64_t)p.M * p.N) return;
+  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (int64_t)p.M * p.row;
+  const int m = (int)(e / p.row), n = (int)(e - (int64_t)m * p.row);
+  if (e >= all || n >= p.N) return;
   floatx4 x = *reinterpret_cast<const floatx4*>(part + e);
-  for (int s = 1; s < splits; ++s)
-    x += *reinterpret_cast<const floatx4*>(part + (int64_t)s * p.M * p.N + e);
+#pragma unroll 4
+  for (int s = 1; s < splits; ++s) x += *reinterpret_cast<const floatx4*>(part + s * all + e);
   float c[4] = {x[0], x[1], x[2], x[3]};
-  finish4<T, EPI, true>(p, (int)(e / p.N), (int)(e % p.N), c);
+  finish4<T, EPI>(p, m, n, c);
 }
 
 // Few rows (at most 32): the weights' bytes are the time.  They go from memory
@@ -503,10 +526,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_product_few(const Product p,
 #pragma unroll
     for (int i = 0; i < kFewWaves; ++i) t += *reinterpret_cast<const floatx4*>(&red[i][m][c]);
     if (splits > 1) {
-      *reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.N + n0 + c) = t;
+      *reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.row + n0 + c) = t;
     } else {
       float v[4] = {t[0], t[1], t[2], t[3]};
-      finish4<T, true, true>(p, m, n0 + c, v);
+      finish4<T, true>(p, m, n0 + c, v);
     }
   }
 }
@@ -541,13 +564,8 @@ __global__ __launch_bounds__(256) void k_linear_dz(const LinearArgs a, uint16_t*
 #pragma unroll
         for (int j = 0; j < 8; ++j) g[j] *= act_slope(a.act, z[j]);
         const uint4 o = make_uint4(T::pack(g[0], g[1]), T::pack(g[2], g[3]), T::pack(g[4], g[5]), T::pack(g[6], g[7]));
-        uint16_t* to = dz + m * dz_stride + n;
-        if (VEC) {
-          if (here > 0) *reinterpret_cast<uint4*>(to) = o;
-        } else {
-          store4<false>(to, make_uint2(o.x, o.y), here);
-          store4<false>(to + 4, make_uint2(o.z, o.w), here - 4);
-        }
+        // dz's own rows are of whole chunks; past N they are zeros, as g is
+        if (here > 0) *reinterpret_cast<uint4*>(dz + m * dz_stride + n) = o;
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] += j < here ? g[j] : 0.0f;
@@ -582,6 +600,50 @@ __global__ __launch_bounds__(256) void k_linear_db(const float* part, int blocks
   db[c] = (typename T::E)t;
 }
 
+// Rows of a matrix copied to rows of whole 16-byte chunks, zeros past their end.
+__global__ __launch_bounds__(256) void k_lay_out(const uint16_t* p, int64_t stride, int64_t rows, int inner, uint16_t* out) {
+  const int chunks = (inner + 7) / 8;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = e / chunks;
+  const int d = 8 * (int)(e - r * chunks);
+  if (r < rows) *reinterpret_cast<uint4*>(out + 8 * e) = load8<false>(p + r * stride + d, min(inner - d, 8));
+}
+
+// A matrix with contiguous rows, as the aligned products read it: rows of whole
+// chunks on 16 bytes that do not overlap.
+struct Mat {
+  const void* p;
+  int64_t rows, stride;
+  int inner;
+};
+int64_t chunked(int64_t n) { return (n + 7) / 8 * 8; }
+bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
+bool laid_out(const Mat& m) {
+  return m.inner % 8 == 0 &&
+         (m.rows <= 1 || (m.stride % 8 == 0 && m.stride >= m.inner && m.stride <= kMaxFastStride));
+}
+bool ready(const Mat& m) { return laid_out(m) && aligned16(m.p); }
+int64_t copy_bytes(const Mat& m) { return m.rows * chunked(m.inner) * 2; }
+// The matrix itself where it is ready, else its copy at ws, which moves on in any case.
+Mat lay_out(const Mat& m, char*& ws, hipStream_t s) {
+  Mat r = m;
+  if (!ready(m) && m.rows > 0) {
+    r.p = ws, r.stride = chunked(m.inner);
+    const int64_t n = m.rows * (r.stride / 8);
+    k_lay_out<<<(unsigned)((n + 255) / 256), 256, 0, s>>>((const uint16_t*)m.p, m.stride, m.rows, m.inner, (uint16_t*)ws);
+  }
+  ws += copy_bytes(m);
+  return r;
+}
+// Whether a product whose operands' sizes or strides are not those of whole chunks
+// is worth their copies: two launches and the operands' bytes against a product
+// element by element (55 TFLOP/s on 6355 x 3389 x 5488, where the copies and
+// their products reach COPYRATE; the weights of few rows at a fraction of the
+// memory's rate).
+bool worth_copies(int64_t M, int64_t N, int64_t K) {
+  return std::max(N, K) <= kMaxFastStride && (M * N * K >= 1 << 27 || K * N >= 1 << 21);
+}
+
 // How a product is run: which kernel, and into how many parts its contracted
 // axis is cut.
 enum Kind { kAny, kFew, kTile128, kTile256 };
@@ -606,16 +668,15 @@ Plan plan_of(int M, int N, int K, bool fast, bool few) {
   const int64_t small = std::max<int64_t>(1, over(M, 128) * over(N, 128));  // M may be 0
   return {kTile128, (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCUs / small, over(K, kBK) / 4))};
 }
-int64_t plan_bytes(const Plan& pl, int64_t M, int64_t N) { return pl.splits > 1 ? pl.splits * M * N * 4 : 0; }
-
-bool fast_strides(const Product& p, bool AK, bool BK) {
-  return (AK ? p.a.si : p.a.sk) <= kMaxFastStride && (BK ? p.b.si : p.b.sk) <= kMaxFastStride &&
-         p.rs <= kMaxFastStride;
-}
+int64_t plan_bytes(const Plan& pl, int64_t M, int64_t N) { return pl.splits > 1 ? pl.splits * M * chunked(N) * 4 : 0; }
 
 template <class T, bool EPI, bool AK, bool BK>
-void product(const Product& p, const Plan& pl, float* part, hipStream_t s) {
+void product(Product p, bool fast, float* part, hipStream_t s) {
   if (p.M == 0) return;
+  const Plan pl = plan_of(p.M, p.N, p.K, fast, EPI);
+  auto whole = [&](const void* q, int64_t stride) { return !q || (aligned16(q) && (p.M == 1 || stride % 8 == 0)); };
+  p.row = (int)chunked(p.N);
+  p.vec = p.N % 8 == 0 && whole(p.c, p.cs) && whole(p.z, p.zs) && whole(p.res, p.rs) && p.rs <= kMaxFastStride && aligned16(p.bias);
   auto tiles = [&](int a, int b) { return (unsigned)(((int64_t)p.M + a - 1) / a * (((int64_t)p.N + b - 1) / b)); };
   switch (pl.kind) {
     case kAny:
@@ -638,77 +699,95 @@ void product(const Product& p, const Plan& pl, float* part, hipStream_t s) {
       break;
   }
   if (pl.splits > 1)
-    k_product_join<T, EPI><<<(unsigned)(((int64_t)p.M * p.N / 4 + 255) / 256), 256, 0, s>>>(p, pl.splits, part);
+    k_product_join<T, EPI><<<(unsigned)(((int64_t)p.M * p.row / 4 + 255) / 256), 256, 0, s>>>(p, pl.splits, part);
 }
 
-Product forward_product(const LinearArgs& a) {
-  Product p = {};
-  p.M = a.M, p.N = a.N, p.K = a.K;
-  p.a = {a.x, a.xs, 1};
-  p.b = {a.w, 1, a.ws};
-  p.c = a.y, p.cs = a.ys;
-  p.act = a.act, p.bias = a.bias, p.res = a.res, p.rs = a.rs, p.z = a.z, p.zs = a.zs;
-  return p;
-}
-int64_t dz_row(const LinearArgs& a) { return ((int64_t)a.N + 7) / 8 * 8; }
-int64_t dz_bytes(const LinearArgs& a) {  // dz, where it is not dy itself
-  return a.act == kNone ? 0 : ((int64_t)a.M * dz_row(a) * 2 + 15) / 16 * 16;
-}
-int64_t db_bytes(const LinearArgs& a) { return ((int64_t)((a.M + 63) / 64) * a.N * 4 + 15) / 16 * 16; }
-Product dx_product(const LinearArgs& a, const void* dz, int64_t dzs) {  // [M][K], over N
-  Product p = {};
-  p.M = a.M, p.N = a.K, p.K = a.N;
-  p.a = {dz, dzs, 1};
-  p.b = {a.w, a.ws, 1};
-  p.c = a.dx, p.cs = a.dxs;
-  return p;
-}
-Product dw_product(const LinearArgs& a, const void* dz, int64_t dzs) {  // [K][N], over M
-  Product p = {};
-  p.M = a.K, p.N = a.N, p.K = a.M;
-  p.a = {a.x, 1, a.xs};
-  p.b = {dz, 1, dzs};
-  p.c = a.dw, p.cs = a.dws;
-  return p;
+// (The stride of a single row is not what the caller's may be.)
+Mat mat(const void* p, int64_t rows, int64_t stride, int inner) { return {p, rows, rows <= 1 ? chunked(inner) : stride, inner}; }
+Mat x_of(const LinearArgs& a) { return mat(a.x, a.M, a.xs, a.K); }
+Mat w_of(const LinearArgs& a) { return mat(a.w, a.K, a.ws, a.N); }
+Mat dy_of(const LinearArgs& a) { return mat(a.dy, a.M, a.dys, a.N); }
+
+// dz, where it is not dy itself: rows of whole chunks in the workspace.
+int64_t dz_bytes(const LinearArgs& a) { return a.act == kNone ? 0 : (int64_t)a.M * chunked(a.N) * 2; }
+int64_t db_bytes(const LinearArgs& a) { return (int64_t)((a.M + 63) / 64) * chunked(a.N) * 4; }
+// Whether the operands are copied, by their sizes and strides alone.
+bool copies(const LinearArgs& a, bool backward) {
+  if (!worth_copies(a.M, a.N, a.K)) return false;
+  return !laid_out(x_of(a)) || !laid_out(w_of(a)) || (backward && a.act == kNone && !laid_out(dy_of(a)));
 }
 
 template <class T>
 void forward(const LinearArgs& a, void* ws, hipStream_t s) {
-  const Product p = forward_product(a);
-  product<T, true, true, false>(p, plan_of(p.M, p.N, p.K, a.vec && fast_strides(p, true, false), true),
-                                (float*)ws, s);
+  Mat x = x_of(a), w = w_of(a);
+  char* at = (char*)ws;
+  const bool copy = a.M && copies(a, false);
+  if (copy) x = lay_out(x, at, s), w = lay_out(w, at, s);
+  Product p = {};
+  p.M = a.M, p.N = a.N, p.K = a.K;
+  p.a = {x.p, x.stride, 1};
+  p.b = {w.p, 1, w.stride};
+  p.c = a.y, p.cs = a.ys;
+  p.act = a.act, p.bias = a.bias, p.res = a.res, p.rs = a.rs, p.z = a.z, p.zs = a.zs;
+  product<T, true, true, false>(p, copy || (ready(x) && ready(w)), (float*)at, s);
 }
 
 template <class T>
 void backward(const LinearArgs& a, void* ws, hipStream_t s) {
   const int blocks = (a.M + 63) / 64;
-  const void* dz = a.act == kNone ? a.dy : ws;
-  const int64_t dzs = a.act == kNone ? a.dys : dz_row(a);
-  float* part = a.db ? (float*)((char*)ws + dz_bytes(a)) : nullptr;
-  float* sums = (float*)((char*)ws + dz_bytes(a) + db_bytes(a));
+  char* at = (char*)ws;
+  Mat x = x_of(a), w = w_of(a), dz = dy_of(a);
+  if (a.act != kNone) dz.p = at, dz.stride = chunked(a.N);
+  at += dz_bytes(a);
+  float* part = a.db ? (float*)at : nullptr;
+  at += db_bytes(a);
   if (blocks && (a.act != kNone || a.db)) {
     const int64_t n = (int64_t)blocks * ((a.N + 255) / 256);
-    if (a.vec)
-      k_linear_dz<T, true><<<(unsigned)n, 256, 0, s>>>(a, (uint16_t*)ws, dzs, part);
+    auto whole = [&](const void* q, int64_t stride) { return aligned16(q) && (a.M == 1 || stride % 8 == 0); };
+    if (a.N % 8 == 0 && whole(a.dy, a.dys) && (a.act == kNone || whole(a.z, a.zs)))
+      k_linear_dz<T, true><<<(unsigned)n, 256, 0, s>>>(a, (uint16_t*)dz.p, dz.stride, part);
     else
-      k_linear_dz<T, false><<<(unsigned)n, 256, 0, s>>>(a, (uint16_t*)ws, dzs, part);
+      k_linear_dz<T, false><<<(unsigned)n, 256, 0, s>>>(a, (uint16_t*)dz.p, dz.stride, part);
   }
   if (a.db) k_linear_db<T><<<(a.N + 15) / 16, 256, 0, s>>>(part, blocks, a.N, (typename T::E*)a.db);
-  if (a.dx) {
-    const Product p = dx_product(a, dz, dzs);
-    product<T, false, true, true>(p, plan_of(p.M, p.N, p.K, a.vec && fast_strides(p, true, true), false), sums, s);
+  // dz of the workspace is ready whatever N: past its end a row holds zeros
+  const bool copy = a.M && copies(a, true);
+  bool dz_ready = a.act != kNone ? dz.stride <= kMaxFastStride : ready(dz);
+  if (copy) {
+    if (a.dw)
+      x = lay_out(x, at, s);
+    else
+      at += copy_bytes(x);
+    if (a.dx)
+      w = lay_out(w, at, s);
+    else
+      at += copy_bytes(w);
+    if (a.act == kNone) dz = lay_out(dz, at, s), dz_ready = true;
   }
-  if (a.dw) {
-    const Product p = dw_product(a, dz, dzs);
-    product<T, false, false, false>(p, plan_of(p.M, p.N, p.K, a.vec && fast_strides(p, false, false), false), sums, s);
+  if (a.dx) {  // [M][K], over N
+    Product p = {};
+    p.M = a.M, p.N = a.K, p.K = a.N;
+    p.a = {dz.p, dz.stride, 1};
+    p.b = {w.p, w.stride, 1};
+    p.c = a.dx, p.cs = a.dxs;
+    product<T, false, true, true>(p, dz_ready && (copy || ready(w)), (float*)at, s);
+  }
+  if (a.dw) {  // [K][N], over M
+    Product p = {};
+    p.M = a.K, p.N = a.N, p.K = a.M;
+    p.a = {x.p, 1, x.stride};
+    p.b = {dz.p, 1, dz.stride};
+    p.c = a.dw, p.cs = a.dws;
+    product<T, false, false, false>(p, dz_ready && (copy || ready(x)), (float*)at, s);
   }
 }
 
 }  // namespace
 
-// The workspace is the same whatever the tensors' alignment.
+// The workspace follows from sizes and strides alone, whatever the pointers' alignment.
 int64_t linear_fwd_bytes(const LinearArgs& a) {
-  return plan_bytes(plan_of(a.M, a.N, a.K, true, true), a.M, a.N);
+  return (copies(a, false) ? copy_bytes(x_of(a)) + copy_bytes(w_of(a)) : 0) +
+         plan_bytes(plan_of(a.M, a.N, a.K, true, true), a.M, a.N);
 }
 
 hipError_t launch_linear_fwd(const LinearArgs& a, void* ws, hipStream_t s) {
@@ -717,8 +796,9 @@ hipError_t launch_linear_fwd(const LinearArgs& a, void* ws, hipStream_t s) {
 }
 
 int64_t linear_bwd_bytes(const LinearArgs& a) {
-  return dz_bytes(a) + db_bytes(a) + std::max(plan_bytes(plan_of(a.M, a.K, a.N, true, false), a.M, a.K),
-                                              plan_bytes(plan_of(a.K, a.N, a.M, true, false), a.K, a.N));
+  const int64_t copied = copies(a, true) ? copy_bytes(x_of(a)) + copy_bytes(w_of(a)) + (a.act == kNone ? copy_bytes(dy_of(a)) : 0) : 0;
+  return dz_bytes(a) + db_bytes(a) + copied + std::max(plan_bytes(plan_of(a.M, a.K, a.N, true, false), a.M, a.K),
+                                                       plan_bytes(plan_of(a.K, a.N, a.M, true, false), a.K, a.N));
 }
 
 hipError_t launch_linear_bwd(const LinearArgs& a, void* ws, hipStream_t s) {

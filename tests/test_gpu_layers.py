@@ -65,6 +65,22 @@ def test_attention(L, shape, dt):
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", [(9, 300, 333, 16, 8, 128), (17, 257, 200, 16, 16, 64), (2, 3000, 130, 8, 8, 64),
+                                   (1, 2000, 515, 16, 1, 128)], ids=str)
+def test_attention_filling_the_chip(L, shape, dt):
+    # more workgroups than compute units, and masks on top
+    B, Sq, Sk, Hq, Hkv, D = shape
+    g = gen_of(21)
+    q, do = normal(g, B, Sq, Hq, D, dt=dt), normal(g, B, Sq, Hq, D, dt=dt)
+    k, v = normal(g, B, Sk, Hkv, D, dt=dt), normal(g, B, Sk, Hkv, D, dt=dt)
+    check_attention(L, q, k, v, do, "many")
+    kv_len = torch.randint(0, Sk + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    q_len = torch.randint(0, Sq + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    mask = torch.rand(B, Sk, generator=g, device="cuda") > 0.3
+    check_attention(L, q, k, v, do, "many, masked", q_len=q_len, kv_len=kv_len, kv_mask=mask)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
 @pytest.mark.parametrize("D", [1, 7, 33, 100, 127])
 def test_attention_odd_head_widths(L, D, dt):
     g = gen_of(2)
@@ -381,6 +397,20 @@ def test_linear(L, case, dt):
         check_linear(L, x, w, b, res, act, dy, str(case))
     check_linear(L, x, w, None, None, "none", dy, f"{case} product alone")
     check_linear(L, x, w, None, res, "silu", dy, f"{case} no bias")
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("case", [(3500, 136, 3600), (3584, 64, 3840), (3400, 3500, 72), (77, 3480, 3610),
+                                  (3333, 129, 3601), (5, 2100, 1001), (20, 1023, 2050), (700, 1000, 301)], ids=str)
+def test_linear_large(L, case, dt):
+    # sizes at which the largest tiles run, in each of the three products, inside
+    # and at ragged edges; and sizes whose operands are copied to whole chunks first
+    M, K, N = case
+    g = gen_of(19)
+    x, w = normal(g, M, K, dt=dt), normal(g, K, N, dt=dt, std=K ** -0.5)
+    b, res, dy = normal(g, N, dt=dt), normal(g, M, N, dt=dt), normal(g, M, N, dt=dt)
+    check_linear(L, x, w, b, res, "gelu", dy, str(case))
+    check_linear(L, x, w, None, None, "none", dy, f"{case} product alone")
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
