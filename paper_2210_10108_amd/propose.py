@@ -1,0 +1,222 @@
+"""Pose proposals: a small network that reads the observed image and moves each
+pose hypothesis towards it before the optimisation starts (Sec. IV-B starts
+from random hypotheses).
+
+The network is one decoder block whose tokens are the hypotheses and whose
+encoder's states are the image's patches, made of the layer operators alone:
+
+  h  = norm(x)                       q = h Wq          (k, v) = states Wkv
+  q', k' = norm and rotation of every head at its position
+  x1 = cross attention(q', k', v) Wo + bo + x
+  x2 = gelu(norm(x1) W1 + b1) W2 + b2 + x1,   correction = x2 Wout + bout
+
+ProposalBlock runs it forward, for a batch of hypotheses or one at a time, and
+backward.  `python -m paper_2210_10108_amd.propose` trains it on views of a
+synthetic field and reports how far the hypotheses are from the true pose
+before and after; the proposals are what Field.render_loss_grad starts from.
+"""
+from __future__ import annotations
+
+import argparse
+import math
+
+import numpy as np
+
+from . import layers as L
+from . import pnerf, synth
+
+POSE_FEATURES = 16  # a pose's 12 numbers, padded to a whole chunk
+
+
+class ProposalBlock:
+    """The block's parameters (float32 masters and copies in `dtype`) and its
+    passes.  width: a multiple of 64 up to 256 (the norms' width); heads of 64,
+    kv_heads of which the states have; state_dim: features of a patch."""
+
+    def __init__(self, width=256, kv_heads=2, state_dim=48, n_positions=4096, dtype=None, seed=0,
+                 device="cuda"):
+        import torch
+        self.width, self.heads, self.kv_heads, self.D = width, width // 64, kv_heads, 64
+        self.dtype = dtype or torch.bfloat16
+        g = torch.Generator(device).manual_seed(seed)
+
+        def matrix(k, n, gain=1.0):
+            return torch.randn(k, n, generator=g, device=device) * (gain / math.sqrt(k))
+        kv = 2 * kv_heads * self.D
+        one, zero = torch.ones, torch.zeros
+        self.master = {
+            "w_in": matrix(POSE_FEATURES, width), "b_in": zero(width, device=device),
+            "n1": one(width, device=device), "w_q": matrix(width, width), "w_kv": matrix(state_dim, kv),
+            "nq": one(self.D, device=device), "nk": one(self.D, device=device),
+            "w_o": matrix(width, width, 0.5), "b_o": zero(width, device=device),
+            "n2": one(width, device=device), "w_1": matrix(width, 4 * width),
+            "b_1": zero(4 * width, device=device), "w_2": matrix(4 * width, width, 0.5),
+            "b_2": zero(width, device=device), "w_out": matrix(width, 8, 0.1),
+            "b_out": zero(8, device=device)}
+        freq = 10000.0 ** (-torch.arange(self.D // 2, device=device, dtype=torch.float64) / (self.D // 2))
+        angle = torch.arange(n_positions, device=device, dtype=torch.float64)[:, None] * freq
+        self.table = torch.stack([angle.cos(), angle.sin()], 1).float()
+        self.refresh()
+
+    def refresh(self):
+        """The parameters as the operators take them, after a change of the masters."""
+        self.p = {k: v.to(self.dtype) for k, v in self.master.items()}
+
+    def _norm(self, x, w):
+        return L.norm_rotate(x[:, None], None, w, None, None, None, None)[0][:, 0]
+
+    def forward(self, poses, states, q_pos, k_pos, kv_len=None, kv_mask=None, keep=False):
+        """poses [B, S, POSE_FEATURES], states [B, T, state_dim] (of `dtype`),
+        positions int32 [B * S] and [B * T]: corrections [B, S, 8], of which 6
+        are used (rotation, translation); keep: also what backward needs."""
+        p, W, D = self.p, self.width, self.D
+        (B, S, _), T = poses.shape, states.shape[1]
+        st = states.reshape(B * T, -1)
+        x = L.linear(poses.reshape(B * S, -1), p["w_in"], p["b_in"])
+        h = self._norm(x, p["n1"])
+        q = L.linear(h, p["w_q"]).view(B * S, self.heads, D)
+        kv = L.linear(st, p["w_kv"]).view(B * T, 2, self.kv_heads, D)
+        qr, kr = L.norm_rotate(q, kv[:, 0], p["nq"], p["nk"], self.table, q_pos, k_pos)
+        qa, ka, va = (qr.view(B, S, self.heads, D), kr.view(B, T, self.kv_heads, D),
+                      kv.view(B, T, 2, self.kv_heads, D)[:, :, 1])
+        o, lse = L.cross_attention(qa, ka, va, kv_len=kv_len, kv_mask=kv_mask, return_lse=True)
+        x1 = L.linear(o.view(B * S, W), p["w_o"], p["b_o"], x)
+        h2 = self._norm(x1, p["n2"])
+        u, z = L.linear(h2, p["w_1"], p["b_1"], activation="gelu", return_preact=True)
+        x2 = L.linear(u, p["w_2"], p["b_2"], x1)
+        y = L.linear(x2, p["w_out"], p["b_out"]).view(B, S, 8)
+        if not keep:
+            return y
+        return y, (poses, st, q_pos, k_pos, kv_len, kv_mask, x, h, q, kv, qa, ka, va, o, lse, x1, h2, u, z, x2)
+
+    def backward(self, dy, kept):
+        """Gradients of every parameter for dy = dL/d(corrections)."""
+        import torch
+        poses, st, q_pos, k_pos, kv_len, kv_mask, x, h, q, kv, qa, ka, va, o, lse, x1, h2, u, z, x2 = kept
+        p, g, W = self.p, {}, self.width
+        B, S, T = qa.shape[0], qa.shape[1], ka.shape[1]
+        dx2, g["w_out"], g["b_out"] = L.linear_backward(dy.view(B * S, 8), x2, p["w_out"])
+        du, g["w_2"], g["b_2"] = L.linear_backward(dx2, u, p["w_2"])
+        dh2, g["w_1"], g["b_1"] = L.linear_backward(du, h2, p["w_1"], z, activation="gelu")
+        dn, _, dw, _ = L.norm_rotate_backward(dh2[:, None], None, x1[:, None], None, p["n2"], None, None, None, None)
+        dx1, g["n2"] = dx2.add_(dn[:, 0]), dw
+        do, g["w_o"], g["b_o"] = L.linear_backward(dx1, o.view(B * S, W), p["w_o"])
+        dkv = torch.empty_like(kv)  # the keys' and the values' gradients side by side
+        side = dkv.view(B, T, 2, self.kv_heads, self.D)
+        dq, dk, _ = L.cross_attention_backward(do.view_as(o), qa, ka, va, o, lse, kv_len=kv_len,
+                                               kv_mask=kv_mask, dk=side[:, :, 0], dv=side[:, :, 1])
+        dq, _, g["nq"], g["nk"] = L.norm_rotate_backward(
+            dq.view(q.shape), dkv[:, 0], q, kv[:, 0], p["nq"], p["nk"], self.table, q_pos, k_pos, dk=dkv[:, 0])
+        _, g["w_kv"], _ = L.linear_backward(dkv.view(B * T, -1), st, p["w_kv"], bias=False)
+        dh, g["w_q"], _ = L.linear_backward(dq.view(B * S, W), h, p["w_q"], bias=False)
+        dn, _, g["n1"], _ = L.norm_rotate_backward(dh[:, None], None, x[:, None], None, p["n1"], None, None, None, None)
+        dx = dx1.add_(dn[:, 0])
+        _, g["w_in"], g["b_in"] = L.linear_backward(dx, poses.reshape(B * S, -1), p["w_in"])
+        return g
+
+
+# ---------------------------------------------------------------- poses and views
+def corrections(poses, target):
+    """(w, t) with Exp(w) R = R_target, o + t = o_target, of poses [..., 3, 4]."""
+    R = target[..., :3] @ np.swapaxes(poses[..., :3], -1, -2)
+    c = np.clip((np.trace(R, axis1=-2, axis2=-1) - 1) / 2, -1, 1)
+    a = np.arccos(c)
+    v = np.stack([R[..., 2, 1] - R[..., 1, 2], R[..., 0, 2] - R[..., 2, 0], R[..., 1, 0] - R[..., 0, 1]], -1)
+    w = v * (a / np.maximum(2 * np.sin(a), 1e-8))[..., None]
+    return np.concatenate([w, target[..., 3] - poses[..., 3]], -1)
+
+
+def corrected(poses, c):
+    """poses moved by corrections (w, t)."""
+    w, out = c[..., :3], poses.copy()
+    a = np.linalg.norm(w, axis=-1)[..., None, None]
+    K = np.zeros(w.shape[:-1] + (3, 3))
+    K[..., 2, 1], K[..., 0, 2], K[..., 1, 0] = w[..., 0], w[..., 1], w[..., 2]
+    K = K - np.swapaxes(K, -1, -2)
+    s = np.where(a > 1e-8, np.sin(a) / np.maximum(a, 1e-8), 1.0)
+    t = np.where(a > 1e-8, (1 - np.cos(a)) / np.maximum(a * a, 1e-16), 0.5)
+    out[..., :3] = (np.eye(3) + s * K + t * (K @ K)) @ poses[..., :3]
+    out[..., 3] += c[..., 3:6]
+    return out
+
+
+class Views:
+    """Batches of observed views of a field: their patches, hypotheses around
+    their poses and the corrections that lead to them."""
+
+    def __init__(self, workload="tiny_bump", patch=4, seed=0):
+        self.w, self.patch = synth.WORKLOADS[workload], patch
+        self.field = pnerf.Field(synth.field_spec(self.w, synth.make_field(self.w, seed)))
+        self.intr = synth.intrinsics(self.w)
+        self.gt = synth.ground_truth_pose(self.w, seed)
+        self.tokens = (self.w.width // patch) * (self.w.height // patch)
+        self.state_dim = 3 * patch * patch
+
+    def batch(self, B, S, seed, dtype):
+        import torch
+        w, n = self.w, self.w.width * self.w.height
+        views = synth.perturb_poses(self.gt, B, w.max_rot_deg, w.max_trans, seed)
+        hyps = np.stack([synth.perturb_poses(v, S, w.max_rot_deg, w.max_trans, seed * 1000 + i)
+                         for i, v in enumerate(views)])
+        pix = torch.arange(n, dtype=torch.int32, device="cuda").repeat(B, 1)
+        rgb = self.field.render(torch.from_numpy(views.astype(np.float32)).cuda(), pix, self.intr)
+        h, v, p = w.height // self.patch, w.width // self.patch, self.patch
+        states = rgb.view(B, h, p, v, p, 3).permute(0, 1, 3, 2, 4, 5).reshape(B, h * v, -1)
+        feat = np.zeros((B, S, POSE_FEATURES), np.float32)
+        feat[..., :12] = (hyps - self.gt).reshape(B, S, 12) * 4
+        target = corrections(hyps, views[:, None])
+        q_pos = torch.zeros(B * S, dtype=torch.int32, device="cuda")
+        k_pos = torch.arange(h * v, dtype=torch.int32, device="cuda").repeat(B)
+        return (torch.from_numpy(feat).cuda().to(dtype), ((states - 0.5) * 2).to(dtype), q_pos, k_pos,
+                torch.from_numpy(target.astype(np.float32)).cuda(), hyps, views)
+
+
+def train(block, views, steps, B=16, S=64, lr=2e-3, report=None):
+    """Adam on the mean squared error of the corrections; the losses."""
+    import torch
+    m = {k: torch.zeros_like(v) for k, v in block.master.items()}
+    v2 = {k: torch.zeros_like(v) for k, v in block.master.items()}
+    losses = []
+    for i in range(1, steps + 1):
+        poses, states, q_pos, k_pos, target, _, _ = views.batch(B, S, i, block.dtype)
+        y, kept = block.forward(poses, states, q_pos, k_pos, keep=True)
+        diff = torch.zeros_like(y, dtype=torch.float32)
+        diff[..., :6] = y[..., :6].float() - target
+        losses.append(float(diff.square().sum() / target.numel()))
+        # the gradient is scaled to the order of 1 for its way through 16-bit tensors; Adam's step does not see it
+        for k, g in block.backward(diff.to(block.dtype), kept).items():
+            m[k].mul_(0.9).add_(g.float(), alpha=0.1)
+            v2[k].mul_(0.99).addcmul_(g.float(), g.float(), value=0.01)
+            step = m[k] / (1 - 0.9 ** i) / ((v2[k] / (1 - 0.99 ** i)).sqrt() + 1e-8)
+            block.master[k].sub_(step, alpha=lr * min(1.0, 2 * (1 - i / (steps + 1))))
+        block.refresh()
+        if report and i % report == 0:
+            print(f"step {i}: mean squared error {np.mean(losses[-report:]):.5f}", flush=True)
+    return losses
+
+
+def errors(poses, target):
+    """Mean rotation error (degrees) and translation error."""
+    c = corrections(poses, np.broadcast_to(target, poses.shape))
+    return (float(np.degrees(np.linalg.norm(c[..., :3], axis=-1)).mean()),
+            float(np.linalg.norm(c[..., 3:], axis=-1).mean()))
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--steps", type=int, default=300)
+    ap.add_argument("--workload", default="tiny_bump", choices=synth.ORDER)
+    args = ap.parse_args()
+    views = Views(args.workload)
+    block = ProposalBlock(state_dim=views.state_dim)
+    train(block, views, args.steps, report=max(1, args.steps // 10))
+    poses, states, q_pos, k_pos, _, hyps, gt = views.batch(4, 64, 10 ** 6, block.dtype)
+    y = block.forward(poses, states, q_pos, k_pos)
+    moved = corrected(hyps, y[..., :6].double().cpu().numpy())
+    for name, p in (("hypotheses", hyps), ("proposals", moved)):
+        r, t = errors(p, gt[:, None])
+        print(f"{name}: {r:.2f} degrees, {t:.4f} from the true pose")
+
+
+if __name__ == "__main__":
+    main()
