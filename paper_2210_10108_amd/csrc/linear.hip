@@ -4,6 +4,7 @@
 // differ in which axis of each operand is contiguous in memory.
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
+#include <type_traits>
 
 #include "layers_internal.h"
 
@@ -262,14 +263,26 @@ struct Tile {
   }
 };
 
+// Tells the scheduler to issue READS LDS reads evenly between MFMAS products.
+template <int READS, int MFMAS, int I = 0>
+__device__ __forceinline__ void spread_reads() {
+  if constexpr (I < MFMAS) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+    constexpr int n = READS * (I + 1) / MFMAS - READS * I / MFMAS;
+    if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x100, n, 0);  // LDS reads
+    spread_reads<READS, MFMAS, I + 1>();
+  }
+}
+
 // BM x BN tiles, 64 deep, two of them in LDS: while the products of one run, the
 // loads of the one after the next fill the buffer just read.  2 x WN wavefronts;
 // fragments are read one 16-deep step ahead, across the tiles' border, so that the
 // one barrier a tile falls between the last reads of a tile and the last of its
 // products.  LDS bounds the 256 x 256 tile: 192 KB read and 64 KB written for
 // 2048 cycles of products a SIMD, all of the 128 bytes a cycle.  Eight wavefronts,
-// two a SIMD, measured 1.05 to 1.12 PFLOP/s on 4096^3 (1.07 to 1.17 on 8192^3)
-// where four, which read a third less, reached 0.88 to 0.97 (0.98 to 1.08).
+// two a SIMD, measured 1.05 to 1.12 PFLOP/s on 4096^3 where four, which read a third
+// less, reached 0.88 to 0.97; with no branch in a tile and its LDS reads spread
+// between its products 1.17 to 1.25 (8192^3: 1.19 to 1.26).
 template <class T, bool EPI, bool AK, bool BK, int BM, int BN, int WN>
 __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const Product p, int splits, float* part) {
   constexpr int NW = 2 * WN, TM = BM / 64, TN = BN / WN / 32;  // wavefronts; 32 x 32 results of one
@@ -314,34 +327,26 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
     for (int j = 0; j < TN; ++j) fb[set][j] = b.fragment(buf + TA::kBytes, j, s);
   };
   constexpr int HA = TA::kLoads / 2, HB = TB::kLoads / 2;
-  if (nt > 0) {
-    a.template load<0, TA::kLoads>(la, wave), b.template load<0, TB::kLoads>(lb, wave);
-    a.next(), b.next();
-    if (nt > 1) {
-      a.template load<0, TA::kLoads>(la + kBuf, wave), b.template load<0, TB::kLoads>(lb + kBuf, wave);
-      a.next(), b.next();
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    fragments(0, lds, 0);
-  }
-  for (int t = 0; t < nt; ++t) {
-    const int cur = (t & 1) * kBuf, oth = kBuf - cur;
+  // One tile.  after: how many follow it (2: two or more).  No branches: the
+  // fragment reads of the next step are spread between the products of this one.
+  auto tile = [&](int cur, auto after) {
+    const int oth = kBuf - cur;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       if (s < 3) {
         fragments((s + 1) & 1, lds + cur, s + 1);
-      } else if (t + 1 < nt) {
+      } else if (after.value > 0) {
         // the next tile is in LDS, and every wavefront has read this one
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         fragments(0, lds + oth, 0);
       }
-      // the tile after the next, into the buffer that the last barrier freed
-      if (s == 3 && t + 2 < nt) {
+      // the tile after the next, into the buffer that the last barrier freed: its
+      // first half now, its second during the next tile
+      if (s == 3 && after.value > 1) {
         a.template load<0, HA>(la + cur, wave), b.template load<0, HB>(lb + cur, wave);
       }
-      if (s == 0 && t > 0 && t + 1 < nt) {
+      if (s == 0 && after.value > 0) {
         a.template load<HA, TA::kLoads>(la + oth, wave), b.template load<HB, TB::kLoads>(lb + oth, wave);
         a.next(), b.next();
       }
@@ -349,7 +354,23 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = T::mma(fb[s & 1][j], fa[s & 1][i], acc[i][j]);
+      if (s < 3 || after.value > 0) {
+        constexpr int kReads = TM * (AK ? 1 : 2) + TN * (BK ? 1 : 2), kMfma = TM * TN;
+        spread_reads<kReads, kMfma>();
+      }
     }
+  };
+  if (nt > 0) {
+    a.template load<0, TA::kLoads>(la, wave), b.template load<0, TB::kLoads>(lb, wave);
+    a.next(), b.next();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (nt > 1) a.template load<0, HA>(la + kBuf, wave), b.template load<0, HB>(lb + kBuf, wave);
+    __builtin_amdgcn_s_barrier();
+    fragments(0, lds, 0);
+    int t = 0;
+    for (; t + 2 < nt; ++t) tile((t & 1) * kBuf, std::integral_constant<int, 2>());
+    if (t + 1 < nt) tile((t++ & 1) * kBuf, std::integral_constant<int, 1>());
+    tile((t & 1) * kBuf, std::integral_constant<int, 0>());
   }
 
   // Results by way of LDS, 32 rows of the wavefront at a time, so that a lane

@@ -544,3 +544,42 @@ def test_captured_into_a_graph(L):
         want = run()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out)), seed
+
+
+def test_binding_refusals(L):
+    g = gen_of(70)
+    q, k = normal(g, 2, 5, 4, 64), normal(g, 2, 9, 2, 64)
+    bad = [
+        (TypeError, lambda: L.cross_attention(q, k.bfloat16(), k)),
+        (TypeError, lambda: L.cross_attention(q, k.cpu(), k)),
+        (TypeError, lambda: L.cross_attention(q.double(), k, k)),
+        (ValueError, lambda: L.cross_attention(q, k, k[:, :4])),
+        (ValueError, lambda: L.cross_attention(q[0], k, k)),
+        (ValueError, lambda: L.cross_attention(q.transpose(2, 3).contiguous().transpose(2, 3), k, k)),
+        (ValueError, lambda: L.cross_attention(q, k, k, kv_len=torch.ones(3, dtype=torch.int32, device="cuda"))),
+        (TypeError, lambda: L.cross_attention(q, k, k, kv_len=torch.ones(2, device="cuda"))),
+        (TypeError, lambda: L.cross_attention(q, k, k, kv_mask=torch.ones(2, 9, device="cuda"))),
+        (ValueError, lambda: L.cross_attention(q, k, k, kv_mask=torch.ones(2, 8, device="cuda", dtype=torch.bool))),
+        (ValueError, lambda: L.cross_attention(q, k, k, o=q[:, :3])),
+        (ValueError, lambda: L.linear(q[0, 0], k[0, 0], activation="tanh")),
+        (ValueError, lambda: L.linear(q[0, 0], k[0, 0])),
+        (ValueError, lambda: L.linear(q, k)),
+        (ValueError, lambda: L.norm_rotate(q, None, None, None, None, None, None)),
+        (ValueError, lambda: L.norm_rotate(q[0], k[0, :, :, :32], None, None, None, None, None)),
+        (ValueError, lambda: L.norm_rotate(q[0], None, None, None, torch.ones(3, 32, device="cuda"), None, None)),
+    ]
+    for kind, fn in bad:
+        with pytest.raises(kind):
+            fn()
+    from paper_2210_10108_amd import pnerf
+    for fn in (lambda: L.cross_attention(q.float(), k.float(), k.float()), lambda: L.linear(q[0, 0].float(), q[0, 0].float().t().contiguous()),
+               lambda: L.cross_attention(normal(g, 1, 2, 1, 129), normal(g, 1, 2, 1, 129), normal(g, 1, 2, 1, 129))):
+        with pytest.raises(pnerf.PnerfError) as e:
+            fn()
+        assert e.value.status == pnerf.ERR_NOT_SUPPORTED
+    for fn in (lambda: L.cross_attention(normal(g, 1, 2, 3, 64), normal(g, 1, 2, 2, 64), normal(g, 1, 2, 2, 64)),
+               lambda: L.cross_attention(q, k, k, scale=-1.0), lambda: L.cross_attention(q, k, k, o=q[:1].expand(2, -1, -1, -1)),
+               lambda: L.norm_rotate(q[0], None, None, None, torch.ones(3, 2, 16, device="cuda"), None, None)):
+        with pytest.raises(pnerf.PnerfError) as e:
+            fn()
+        assert e.value.status == pnerf.ERR_INVALID_ARG
