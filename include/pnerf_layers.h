@@ -30,7 +30,8 @@
  *    an input, save where stated.  Any stride and any pointer aligned to its
  *    elements will do; the fast kernels want every row to start on 16 bytes
  *    (pointers and strides), as contiguous tensors with rows of a multiple of 8
- *    16-bit elements do.
+ *    16-bit elements do.  (Linear layers copy large operands of other sizes and
+ *    strides to such rows in the workspace.)
  *  - The same inputs give the same bits on every call (no atomics on results).
  */
 #ifndef PNERF_LAYERS_H
@@ -53,14 +54,15 @@ extern "C" {
  * A row without an allowed key, or with i >= q_len[b], has o_i = 0 and
  * lse_i = -inf.  What keys, values and mask hold at j >= kv_len[b], keys and
  * values where the mask is 0, and queries at i >= q_len[b] has no influence,
- * infinities and NaN among them.  exp(a - max) is rounded to the data type
- * before it meets the values.
+ * infinities and NaN among them.  exp(a - m), m at most 8 ln 2 below the row's
+ * running maximum, is rounded to the data type before it meets the values.
  * Backward, given do = dL/do:
  *   p_ij = exp(a_ij - lse_i),  delta_i = do_i . o_i,
  *   ds_ij = p_ij (do_i . v_j - delta_i),  dv_j = sum p_ij do_i,
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum ds_ij q_i
  * (dk, dv: summed over the rows and the query heads that share the kv head; 0
- * where the key is not allowed).  p and ds are rounded to the data type.  A
+ * where the key is not allowed).  p and ds are rounded to the data type (float16:
+ * times a power of two that grows with kv_rows beyond 8192, which keeps them normal).  A
  * batch entry's dk and dv are its own also where k and v are one tensor
  * broadcast over the batch.
  *
@@ -144,7 +146,7 @@ pnerf_status pnerf_norm_rotate_backward(const pnerf_norm_rotate_params* params, 
  * residual is dy.  z may be NULL when activation is 0; dx, dw and db may each be
  * NULL (not wanted).
  *
- * Requires 0 <= m, 1 <= n, k, each at most 2^30, and m * n, m * k, k * n at most 2^34;
+ * Requires 0 <= m, 1 <= n, k, each at most 2^27, and m * n, m * k, k * n at most 2^34;
  * dtype PNERF_F16 or PNERF_BF16. */
 #define PNERF_ACT_NONE 0
 #define PNERF_ACT_RELU 1 /* derivative 0 at 0 */

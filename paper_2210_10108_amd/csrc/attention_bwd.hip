@@ -4,8 +4,10 @@
 // Three kernels, no atomics: the rows' (lse, delta); dq by workgroups that own
 // rows and pass over the keys; dk and dv by workgroups that own keys and pass
 // over the rows of all the query heads that share their kv head, so that the
-// sum over those heads never leaves the registers.  s and dp are computed twice
-// (7 products where 5 would do), which costs less than adding dq up in memory.
+// sum over those heads never leaves the registers.  s and dp are computed twice (7
+// products where 5 would do): dq from the second kernel would have to be added up
+// in memory, by atomics, whose order changes the result, or from as many partial
+// sums as there are tiles of keys.
 //
 // Fragments as in the forward kernel: what the second products contract over is
 // in the registers of the first ones' results, as their B operand.
@@ -403,7 +405,7 @@ int dkv_splits(const AttnArgs& a) {
 // Whether tiles of rows can go to LDS by 16-byte loads with 32-bit offsets, the
 // rows past the last beyond the descriptor's bound.
 bool fast_rows(const AttnArgs& a) {
-  auto fits = [&](int64_t stride) { return a.Sq == 1 || (stride >= a.D && stride <= kMaxTileStride); };
+  auto fits = [&](int64_t stride) { return stride >= a.D && stride <= kMaxTileStride; };
   return fits(a.qs[1]) && fits(a.dos[1]);
 }
 int64_t stat_floats(const AttnArgs& a) { return ((int64_t)2 * a.B * a.Hkv * a.M + 3) / 4 * 4; }

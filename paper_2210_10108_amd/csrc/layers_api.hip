@@ -127,6 +127,11 @@ pnerf_status attention_args(const pnerf_attention_params* p, AttnArgs* out, bool
     a.qs[i] = p->q_stride[i], a.ks[i] = p->k_stride[i], a.vs[i] = p->v_stride[i], a.os[i] = p->o_stride[i];
     a.dos[i] = p->do_stride[i], a.dqs[i] = p->dq_stride[i], a.dks[i] = p->dk_stride[i], a.dvs[i] = p->dv_stride[i];
   }
+  // the stride of a single row is not what the caller's may be: the tiles' loads
+  // want one that keeps the rows after it apart
+  const int64_t apart = (p->head_dim + 7) / 8 * 8;
+  if (a.Sq == 1) a.qs[1] = a.os[1] = a.dos[1] = a.dqs[1] = apart;
+  if (a.Sk == 1) a.ks[1] = a.vs[1] = a.dks[1] = a.dvs[1] = apart;
   a.q_len = p->q_len, a.kv_len = p->kv_len, a.mask = p->kv_mask, a.mask_stride = p->kv_mask_stride;
   if (a.mask && (a.mask_stride < 0 || a.mask_stride > ((int64_t)1 << 40)))
     return fail(PNERF_ERR_INVALID_ARG, "kv_mask has stride %lld", (long long)a.mask_stride);
@@ -214,8 +219,8 @@ pnerf_status linear_args(const pnerf_linear_params* p, LinearArgs* out) {
   if (p->m < 0 || p->n < 1 || p->k < 1)
     return fail(PNERF_ERR_INVALID_ARG, "m=%d must be >= 0, n=%d and k=%d >= 1", p->m, p->n, p->k);
   const int64_t m = p->m, n = p->n, k = p->k, most = (int64_t)1 << 34;
-  if (std::max({m, n, k}) > (1 << 30) || m * n > most || m * k > most || k * n > most)
-    return fail(PNERF_ERR_CAPACITY, "m=%d n=%d k=%d: a size exceeds 2^30 or a product of two 2^34", p->m, p->n, p->k);
+  if (std::max({m, n, k}) > (1 << 27) || m * n > most || m * k > most || k * n > most)
+    return fail(PNERF_ERR_CAPACITY, "m=%d n=%d k=%d: a size exceeds 2^27 or a product of two 2^34", p->m, p->n, p->k);
   LinearArgs a = {};
   a.dtype = p->dtype, a.act = p->activation, a.M = p->m, a.N = p->n, a.K = p->k;
   a.xs = p->x_stride, a.ws = p->w_stride, a.rs = p->residual_stride, a.ys = p->y_stride, a.zs = p->z_stride;

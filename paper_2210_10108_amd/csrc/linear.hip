@@ -659,8 +659,8 @@ Mat lay_out(const Mat& m, char*& ws, hipStream_t s) {
 // Whether a product whose operands' sizes or strides are not those of whole chunks
 // is worth their copies: two launches and the operands' bytes against a product
 // element by element (55 TFLOP/s on 6355 x 3389 x 5488, where the copies and
-// their products reach COPYRATE; the weights of few rows at a fraction of the
-// memory's rate).
+// their products take a training step at 720 TFLOP/s; the weights of few rows at a
+// fraction of the memory's rate).
 bool worth_copies(int64_t M, int64_t N, int64_t K) {
   return std::max(N, K) <= kMaxFastStride && (M * N * K >= 1 << 27 || K * N >= 1 << 21);
 }

@@ -182,6 +182,28 @@ def test_attention_layouts(L, kind, Sq, dt):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_attention_stride_of_a_single_row(L, dt):
+    # whatever the stride of a dimension of one row says, no other row is there
+    g = gen_of(22)
+    for Sq, Sk in ((1, 200), (40, 1), (1, 1)):
+        q, do, k, v = (normal(g, 3, n, h, 64, dt=dt) for n, h in ((Sq, 4), (Sq, 4), (Sk, 2), (Sk, 2)))
+        for step in (0, 3, 1 << 33):
+            ins = [t.as_strided(t.shape, (t.stride(0), step if t.shape[1] == 1 else t.stride(1), 64, 1))
+                   for t in (q, k, v, do)]
+            check_attention(L, *ins, f"stride {step}")
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_linear_stride_of_a_single_row(L, dt):
+    g = gen_of(23)
+    for M, K, N in ((1, 64, 128), (40, 1, 64), (1, 2048, 1024), (1, 1, 8)):
+        x, w, res, dy = (normal(g, *s, dt=dt) for s in ((M, K), (K, N), (M, N), (M, N)))
+        for step in (0, 3, 1 << 33):
+            one = [t.as_strided(t.shape, (step if t.shape[0] == 1 else t.stride(0), 1)) for t in (x, w, res, dy)]
+            check_linear(L, one[0], one[1], None, one[2], "gelu", one[3], f"stride {step}")
+
+
 def test_attention_broadcast_states(L):
     # one image's states for every batch entry: each entry's gradient is its own
     g = gen_of(6)

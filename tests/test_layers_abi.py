@@ -133,7 +133,7 @@ CASES = [
     (linear, dict(dtype=5), INVALID, "dtype"), (linear, dict(dtype=0), UNSUPPORTED, "dtype"),
     (linear, dict(activation=4), INVALID, "activation"), (linear, dict(m=-1), INVALID, "m="),
     (linear, dict(n=0), INVALID, "n="), (linear, dict(k=0), INVALID, "k="),
-    (linear, dict(m=1 << 25, n=1 << 25), CAPACITY, "2^34"), (linear, dict(y_stride=15), INVALID, "y overlaps"),
+    (linear, dict(m=1 << 25, n=1 << 25), CAPACITY, "2^34"), (linear, dict(m=1 << 28), CAPACITY, "2^27"), (linear, dict(y_stride=15), INVALID, "y overlaps"),
     (linear, dict(x_stride=-8), INVALID, "x has stride"),
 ]
 
