@@ -149,14 +149,10 @@ struct Place {
   bool ok;
   const uint16_t* q;
   const uint8_t* mask;
-  __device__ __forceinline__ Place(const AttnArgs& a, int rows_wg, int row_in) {
-    const int tiles_m = (a.M + rows_wg - 1) / rows_wg;
-    int id = xcd_order(blockIdx.x, gridDim.x);
-    const int mt = id % tiles_m;
-    id /= tiles_m;
-    sp = id % a.splits;
-    id /= a.splits;
-    g = id % a.Hkv, b = id / a.Hkv;
+  __device__ __forceinline__ Place(const AttnArgs& a, const Order& order, int rows_wg, int row_in) {
+    const Item item(order, a.splits, a.Hkv, a.B);
+    const int mt = item.tile;  // past the last: every row is, too
+    sp = item.sp, g = item.g, b = item.b;
     row = mt * rows_wg + row_in;
     qi = row / a.G, head = g * a.G + row % a.G;
     const int nq = clamp_len(a.q_len, b, a.Sq);
@@ -180,12 +176,12 @@ struct Place {
 // workgroup a CU: 33 us with one group, 22 with two; 2048 rows, 4096 keys, 16 heads
 // of 128: 0.84 PFLOP/s with two, 0.54 with one on 17 heads).
 template <class T, int DP, int KS>
-__global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_fwd(const AttnArgs a) {
+__global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_fwd(const AttnArgs a, const Order order) {
   using Tile = RowTile<DP, 4>;
   __shared__ uint4 lds[KS][2][2 * Tile::kPieces];  // keys, then values
   const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int wave = all_waves & 3, grp = all_waves >> 2;
-  const Place at(a, 128, wave * 32 + (lane & 31));
+  const Place at(a, order, 128, wave * 32 + (lane & 31));
   const Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, wave, lane);
   const Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, wave, lane);
   Rows<T, DP> x;
@@ -270,11 +266,11 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_fwd(const AttnArgs a)
 // scores are there, values as soon as they have been used.  At the end the
 // wavefronts' sums meet in LDS.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_few(const AttnArgs a) {
+__global__ __launch_bounds__(256) void k_attn_few(const AttnArgs a, const Order order) {
   using Tile = RowTile<DP, 1>;
   __shared__ uint4 lds[4][2 * Tile::kPieces];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const Place at(a, 32, lane & 31);
+  const Place at(a, order, 32, lane & 31);
   const Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, 0, lane);
   const Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, 0, lane);
   Rows<T, DP> x;
@@ -355,10 +351,10 @@ __global__ __launch_bounds__(256) void k_attn_few(const AttnArgs a) {
 // Any strides, alignment and head width: as k_attn_fwd, the tiles by way of
 // registers, element by element.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_any(const AttnArgs a) {
+__global__ __launch_bounds__(256) void k_attn_any(const AttnArgs a, const Order order) {
   __shared__ uint4 sk[kBN * DP / 8], sv[kBN * DP / 8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const Place at(a, 128, wave * 32 + (lane & 31));
+  const Place at(a, order, 128, wave * 32 + (lane & 31));
   Rows<T, DP> x;
   x.template init<false>(at.q, at.ok, a.D, h);
   int t = at.t0;
@@ -431,15 +427,16 @@ template <class T, int DP>
 void launch(const AttnArgs& a, hipStream_t s) {
   const bool few = a.M <= 32;
   const int rows = few ? 32 : 128;
-  const unsigned n = (unsigned)((int64_t)((a.M + rows - 1) / rows) * a.splits * a.Hkv * a.B);
+  const Order o = order_of(((int64_t)a.M + rows - 1) / rows, a.Hkv);
+  const unsigned n = (unsigned)workgroups(o, a.splits, a);
   if (!fast_loads(a))
-    k_attn_any<T, DP><<<n, 256, 0, s>>>(a);
+    k_attn_any<T, DP><<<n, 256, 0, s>>>(a, o);
   else if (few)
-    k_attn_few<T, DP><<<n, 256, 0, s>>>(a);
+    k_attn_few<T, DP><<<n, 256, 0, s>>>(a, o);
   else if (two_groups(n, a))
-    k_attn_fwd<T, DP, 2><<<n, 512, 0, s>>>(a);
+    k_attn_fwd<T, DP, 2><<<n, 512, 0, s>>>(a, o);
   else
-    k_attn_fwd<T, DP, 1><<<n, 256, 0, s>>>(a);
+    k_attn_fwd<T, DP, 1><<<n, 256, 0, s>>>(a, o);
   if (a.splits > 1) k_attn_join<T, DP><<<(unsigned)(a.B * a.Hkv * a.M), 256, 0, s>>>(a);
 }
 

@@ -59,18 +59,13 @@ __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
 // is the column of every product: its lse and delta are a lane's own; and KS = 2
 // groups of wavefronts take the tiles in turn where workgroups are few.
 template <class T, int DP, bool FAST, int KS>
-__global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, int splits, float* part) {
+__global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, const Order order, int splits, float* part) {
   constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32;
   using Tile = RowTile<DP, 4>;
   __shared__ uint4 lds[KS][FAST ? 2 : 1][2 * Tile::kPieces];  // keys, then values
 
-  const int tiles_m = (a.M + 127) / 128;
-  int id = xcd_order(blockIdx.x, gridDim.x);
-  const int mt = id % tiles_m;
-  id /= tiles_m;
-  const int sp = id % splits;
-  id /= splits;
-  const int g = id % a.Hkv, b = id / a.Hkv;
+  const Item item(order, splits, a.Hkv, a.B);
+  const int mt = item.tile, sp = item.sp, g = item.g, b = item.b;  // past the last tile every row is past the last
   const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave = all_waves & 3, grp = all_waves >> 2;
   const int r = lane & 31, h = lane >> 5;
@@ -230,19 +225,14 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, 
 // (4 x 4096 rows and keys, 16 heads of 128: 1.05 PFLOP/s; with the values in
 // registers and one wavefront a SIMD 0.70).  The tiles are then of 32 rows.
 template <class T, int DP, bool FAST>
-__global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a, int splits, float* part) {
+__global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a, const Order order, int splits, float* part) {
   constexpr bool kStash = FAST && DP == 128;
   constexpr int CH = DP / 8, NS = DP / 16, ND = DP / 32, kR = dkv_rows(DP, FAST), kPieces = kR * CH;
   __shared__ uint4 lds[FAST ? 2 : 1][2 * kPieces + 64];  // queries, their gradients, (lse, delta) of each row
   __shared__ uint4 stash[kStash ? 4 : 1][kStash ? NS : 1][64];
 
-  const int tiles_k = (a.Sk + kKeys - 1) / kKeys;
-  int id = xcd_order(blockIdx.x, gridDim.x);
-  const int kt = id % tiles_k;
-  id /= tiles_k;
-  const int sp = id % splits;
-  id /= splits;
-  const int g = id % a.Hkv, b = id / a.Hkv;
+  const Item item(order, splits, a.Hkv, a.B);
+  const int kt = item.tile, sp = item.sp, g = item.g, b = item.b;  // past the last tile every key is past the last
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
   const int key = kt * kKeys + wave * 32 + r;
@@ -425,21 +415,23 @@ void launch(const AttnArgs& a, float* part_q, float* part_kv, hipStream_t s) {
     const int per = 256 / (DP / 8);
     k_attn_stat<T, DP, FAST><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(a);
     const int ns = dq_splits(a);
-    const int64_t n = (((int64_t)a.M + 127) / 128) * ns * a.Hkv * a.B;
+    const Order o = order_of(((int64_t)a.M + 127) / 128, a.Hkv);
+    const int64_t n = workgroups(o, ns, a);
     if constexpr (FAST) {
       if (two_groups(n, a))
-        k_attn_dq<T, DP, true, 2><<<(unsigned)n, 512, 0, s>>>(a, ns, part_q);
+        k_attn_dq<T, DP, true, 2><<<(unsigned)n, 512, 0, s>>>(a, o, ns, part_q);
       else
-        k_attn_dq<T, DP, true, 1><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
+        k_attn_dq<T, DP, true, 1><<<(unsigned)n, 256, 0, s>>>(a, o, ns, part_q);
     } else {
-      k_attn_dq<T, DP, false, 1><<<(unsigned)n, 256, 0, s>>>(a, ns, part_q);
+      k_attn_dq<T, DP, false, 1><<<(unsigned)n, 256, 0, s>>>(a, o, ns, part_q);
     }
     if (ns > 1) k_attn_sum<T, DP, false, FAST><<<(unsigned)((rows * DP / 4 + 255) / 256), 256, 0, s>>>(a, ns, part_q);
   }
   if (keys) {
     const int ns = dkv_splits(a);
-    const int64_t n = (int64_t)((a.Sk + kKeys - 1) / kKeys) * ns * a.Hkv * a.B;
-    k_attn_dkv<T, DP, FAST><<<(unsigned)n, 256, 0, s>>>(a, ns, part_kv);
+    const Order o = order_of(((int64_t)a.Sk + kKeys - 1) / kKeys, a.Hkv);
+    const int64_t n = workgroups(o, ns, a);
+    k_attn_dkv<T, DP, FAST><<<(unsigned)n, 256, 0, s>>>(a, o, ns, part_kv);
     if (ns > 1)
       k_attn_sum<T, DP, true, FAST><<<(unsigned)((keys * 2 * DP / 4 + 255) / 256), 256, 0, s>>>(a, ns, part_kv);
   }

@@ -13,11 +13,39 @@ inline int padded(int D) { return D <= 64 ? 64 : 128; }  // head width in the ke
 inline bool fast_loads(const AttnArgs& a) {
   return a.vec && a.ks[1] <= kMaxTileStride && a.vs[1] <= kMaxTileStride;
 }
+// Which workgroup takes which tile of rows (or keys), part, kv head and batch
+// entry.  The tiles of one kv head read the same keys and values, so they go to
+// one XCD; but batch entries may be of very different lengths, so every XCD takes
+// its share of each: the order is kv head, chunk of its tiles, batch entry, part,
+// tile, with as many chunks of tiles as make kv heads times chunks a multiple of
+// the XCDs.  (With batch entries outermost, two of lengths 4 to 1 left half the
+// XCDs idle most of the time.)  Single tiles share nothing and go round the XCDs.
+struct Order {
+  int tiles, chunks, per;  // per: tiles of a chunk
+};
+inline Order order_of(int64_t tiles, int Hkv) {
+  int gcd = kXCDs;
+  while (Hkv % gcd) gcd /= 2;
+  const int chunks = (int)(tiles < kXCDs / gcd ? tiles : kXCDs / gcd);
+  return {(int)tiles, chunks, (int)((tiles + chunks - 1) / chunks)};
+}
+inline int64_t workgroups(const Order& o, int splits, const AttnArgs& a) {
+  return (int64_t)o.chunks * o.per * splits * a.Hkv * a.B;
+}
+
 // Whether two groups of wavefronts share a workgroup's rows (KS = 2): where the
-// workgroups are fewer than the chip holds of that kind (by LDS, one a compute
-// unit at the wide head).
+// workgroups are fewer than the chip holds of that kind -- by registers two a
+// compute unit at the narrow head, one at the wide one.  257 to 512 wide ones of
+// equal length run better as single groups, two a compute unit (2048 rows and 4096
+// keys, bf16, 17 / 24 / 32 heads: single 136 / 147 / 158 us and dq 182 / 197 / 212,
+// two groups 147 / 153 / 164 and 203 / 213 / 226).  Where lengths are given they mostly
+// differ, and a compute unit left with one long workgroup needs its second group
+// (16 heads, rows and keys 2011 x 2500 and 502 x 625: 88 us against 95 and dq 108
+// against 118; 2011 x 625 and 502 x 2500: 65 against 89 and 79 against 110).  The host
+// does not see the lengths: given but equal ones pay the first line's difference.
 inline bool two_groups(int64_t workgroups, const AttnArgs& a) {
-  return workgroups <= (padded(a.D) == 128 ? 1 : 2) * kCUs && a.Sk > 2 * kBN;
+  const bool two = padded(a.D) == 64 || a.q_len || a.kv_len;
+  return workgroups <= (two ? 2 : 1) * kCUs && a.Sk > 2 * kBN;
 }
 
 #if defined(__HIP_DEVICE_COMPILE__) || defined(PNERF_LAYERS_DEVICE)
@@ -30,6 +58,29 @@ template <int CH>
 __device__ __forceinline__ int swz(int r, int c) {
   return r * CH + (c ^ swz_bits(r));
 }
+
+struct Item {
+  int tile, sp, g, b;  // tile may be past the last one: nothing to do
+  __device__ __forceinline__ Item(const Order& o, int splits, int Hkv, int B) {
+    if (o.tiles == 1) {
+      int id = blockIdx.x;
+      tile = 0, sp = id % splits;
+      id /= splits;
+      g = id % Hkv, b = id / Hkv;
+      return;
+    }
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int t = id % o.per;
+    id /= o.per;
+    sp = id % splits;
+    id /= splits;
+    b = id % B;
+    id /= B;
+    tile = id % o.chunks * o.per + t;
+    if (t >= o.per || tile >= o.tiles) tile = o.tiles;
+    g = id / o.chunks;
+  }
+};
 
 __device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
   return len ? min(max(len[b], 0), most) : most;
