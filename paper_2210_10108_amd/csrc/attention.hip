@@ -380,47 +380,62 @@ __global__ __launch_bounds__(256) void k_attn_any(const AttnArgs a, const Order 
     x.template store<false>(a, at.b, at.qi, at.head, h);
 }
 
-// Joins the parts of the key axis, a workgroup per row: the parts' sums meet at
-// the largest of their maxima, in a fixed order.
-template <class T, int DP>
+// Joins the parts of the key axis, in a fixed order: the parts' sums meet at the
+// largest of their maxima.  A row is NG groups of DP / 4 lanes, each with every
+// NG-th part: one group where rows are many and parts fewer than a workgroup's
+// groups (16384 rows of two parts, heads of 64: 4.5 us, 20.6 with a workgroup each), a
+// whole workgroup elsewhere (128 rows of 8 parts: 3.3 us, 6.4 with a group each).
+template <class T, int DP, int NG>
 __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
-  constexpr int NG = 256 / (DP / 4);  // groups of lanes, each with every NG-th part
-  __shared__ float red[NG][DP];
-  __shared__ float red_l[NG];
-  const int row = blockIdx.x % a.M;
-  const int bg = blockIdx.x / a.M, g = bg % a.Hkv, b = bg / a.Hkv;
-  const int qi = row / a.G, head = g * a.G + row % a.G;
-  const int64_t rows = (int64_t)a.B * a.Hkv * a.M, at = blockIdx.x;
+  constexpr int kLanes = DP / 4, kRowsWg = 256 / (kLanes * NG);
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.M;
+  const int64_t at = (int64_t)blockIdx.x * kRowsWg + threadIdx.x / (kLanes * NG);
+  const bool ok = at < rows;
   const floatx2* ml = reinterpret_cast<const floatx2*>(a.part + (int64_t)a.splits * rows * DP);
   float m = -INFINITY;
-  for (int s = threadIdx.x & 63; s < a.splits; s += 64) m = fmaxf(m, ml[s * rows + at][0]);
-  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-
-  const int grp = threadIdx.x / (DP / 4), d4 = 4 * (threadIdx.x % (DP / 4));
+  if constexpr (NG == 1) {
+    if (ok)
+#pragma unroll 4
+      for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[s * rows + at][0]);
+  } else {
+    for (int s = threadIdx.x & 63; s < a.splits; s += 64) m = fmaxf(m, ml[s * rows + at][0]);
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  }
+  const int grp = threadIdx.x / kLanes % NG, d4 = 4 * (threadIdx.x % kLanes);
   floatx4 acc = {};
   float l = 0.0f;
-  for (int s = grp; s < a.splits; s += NG) {
-    const floatx2 v = ml[s * rows + at];
-    // a part without an allowed key has no sums (NaN scores: the sum is NaN)
-    if (v[0] == -INFINITY && v[1] == 0.0f) continue;
-    const float w = __builtin_amdgcn_exp2f(v[0] - (m == -INFINITY ? 0.0f : m));
-    l += w * v[1];
-    acc += w * *reinterpret_cast<const floatx4*>(a.part + (s * rows + at) * DP + d4);
+  if (ok)
+#pragma unroll 2
+    for (int s = grp; s < a.splits; s += NG) {
+      const floatx2 v = ml[s * rows + at];
+      // a part without an allowed key has no sums (NaN scores: the sum is NaN)
+      if (v[0] == -INFINITY && v[1] == 0.0f) continue;
+      const float w = __builtin_amdgcn_exp2f(v[0] - (m == -INFINITY ? 0.0f : m));
+      l += w * v[1];
+      acc += w * *reinterpret_cast<const floatx4*>(a.part + (s * rows + at) * DP + d4);
+    }
+  if constexpr (NG > 1) {  // one row: the groups' sums
+    __shared__ floatx4 red[NG][kLanes];
+    __shared__ float red_l[NG];
+    red[grp][d4 / 4] = acc;
+    if (d4 == 0) red_l[grp] = l;
+    __syncthreads();
+    if (grp > 0) return;
+    acc = floatx4{};
+    l = 0.0f;
+    for (int i = 0; i < NG; ++i) acc += red[i][d4 / 4], l += red_l[i];
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) red[grp][d4 + i] = acc[i];
-  if (d4 == 0) red_l[grp] = l;
-  __syncthreads();
-  l = 0.0f;
-  for (int i = 0; i < NG; ++i) l += red_l[i];
+  if (!ok) return;
+  const uint32_t bg = (uint32_t)at / a.M, row = (uint32_t)at % a.M;
+  const int g = bg % a.Hkv, b = bg / a.Hkv, qi = row / a.G, head = g * a.G + row % a.G;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  typename T::E* op = (typename T::E*)a.o + b * a.os[0] + (int64_t)qi * a.os[1] + head * a.os[2];
-  for (int d = threadIdx.x; d < a.D; d += 256) {
-    float x = 0.0f;
-    for (int i = 0; i < NG; ++i) x += red[i][d];
-    op[d] = (typename T::E)(x * inv);
-  }
-  if (a.lse && threadIdx.x == 0) a.lse[((int64_t)b * a.Hq + head) * a.Sq + qi] = log_sum(m, l);
+  uint16_t* op = (uint16_t*)a.o + b * a.os[0] + (int64_t)qi * a.os[1] + head * a.os[2] + d4;
+  const uint2 x = make_uint2(T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv));
+  if (a.vec)
+    store4<true>(op, x, min(a.D - d4, 4));
+  else
+    store4<false>(op, x, min(a.D - d4, 4));
+  if (a.lse && d4 == 0) a.lse[((int64_t)b * a.Hq + head) * a.Sq + qi] = log_sum(m, l);
 }
 
 template <class T, int DP>
@@ -437,7 +452,13 @@ void launch(const AttnArgs& a, hipStream_t s) {
     k_attn_fwd<T, DP, 2><<<n, 512, 0, s>>>(a, o);
   else
     k_attn_fwd<T, DP, 1><<<n, 256, 0, s>>>(a, o);
-  if (a.splits > 1) k_attn_join<T, DP><<<(unsigned)(a.B * a.Hkv * a.M), 256, 0, s>>>(a);
+  if (a.splits == 1) return;
+  constexpr int kGroups = 256 / (DP / 4);
+  const int64_t all = (int64_t)a.B * a.Hkv * a.M;
+  if (a.splits < kGroups && all > 2 * kCUs)
+    k_attn_join<T, DP, 1><<<(unsigned)((all + kGroups - 1) / kGroups), 256, 0, s>>>(a);
+  else
+    k_attn_join<T, DP, kGroups><<<(unsigned)all, 256, 0, s>>>(a);
 }
 
 }  // namespace
