@@ -210,7 +210,7 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, 
   }
   if (row >= a.M) return;
   if (splits > 1) {
-    store_part<DP>(acc, part + (sp * rows + at) * DP, h);
+    if (t0 < t1) store_part<DP>(acc, part + (sp * rows + at) * DP, h);
   } else {
     uint16_t* out = (uint16_t*)a.dq + b * a.dqs[0] + (int64_t)qi * a.dqs[1] + head * a.dqs[2];
     store_cols<T, DP, FAST>(acc, out, ldexpf(a.scale, -a.shift), a.D, h);
@@ -341,6 +341,7 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
 #pragma unroll
     for (int i = 0; i < ND; ++i) dk[i] = dv[i] = floatx16{};
   if (splits > 1) {
+    if (t0 >= t1) return;  // the sum reads no empty part
     const int64_t keys = (int64_t)a.B * a.Hkv * a.Sk, at = ((int64_t)b * a.Hkv + g) * a.Sk + key;
     float* p = part + 2 * (sp * keys + at) * DP;
     store_part<DP>(dk, p, h);
@@ -354,7 +355,9 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
   }
 }
 
-// Adds the parts up in order, 4 elements a thread: dq (KV = false), dk and dv.
+// Adds the parts up in order, 4 elements a thread: dq (KV = false), dk and dv.  Of a
+// batch entry's parts the first ones have tiles, the others were not written, and
+// nothing was for rows and keys past its lengths.
 template <class T, int DP, bool KV, bool VEC>
 __global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a, int splits, const float* part) {
   const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -362,13 +365,18 @@ __global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a, int splits, 
   const int64_t n = (int64_t)a.B * a.Hkv * len * (KV ? 2 : 1) * DP;
   const int d = (int)(e % DP);
   if (e >= n || d >= a.D) return;
-  floatx4 x = *reinterpret_cast<const floatx4*>(part + e);
-#pragma unroll 4
-  for (int s = 1; s < splits; ++s) x += *reinterpret_cast<const floatx4*>(part + s * n + e);
-  int64_t i = e / DP;
+  uint32_t i = (uint32_t)(e / DP);
   const bool val = KV && (i & 1);
   if (KV) i >>= 1;
   const int at = (int)(i % len), bg = (int)(i / len), g = bg % a.Hkv, b = bg / a.Hkv;
+  const int nq = clamp_len(a.q_len, b, a.Sq), nk = clamp_len(a.kv_len, b, a.Sk);
+  const int tiles = KV ? (nq + dkv_rows(DP, VEC) - 1) / dkv_rows(DP, VEC) * a.G : (nk + kBN - 1) / kBN;
+  const int per = (tiles + splits - 1) / splits;
+  int parts = tiles ? (tiles + per - 1) / per : 0;
+  if (KV ? at >= nk : at / a.G >= nq) parts = 0;
+  floatx4 x = {};
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s) x += *reinterpret_cast<const floatx4*>(part + s * n + e);
   const float f = ldexpf(val ? 1.0f : a.scale, -a.shift);
   uint16_t* out;
   if (!KV)
