@@ -134,14 +134,18 @@ __device__ __forceinline__ void finish8(const Product& p, int m, int n, float c[
 // Any sizes, strides and alignment: 64 x 64 tiles, 32 deep, a 32 x 32 part a
 // wavefront; both operands go through LDS with their contracted axis contiguous.
 // The product is formed transposed (A operand: columns of B), so that a lane's
-// result registers are neighbours in a row of C.
+// result registers are neighbours in a row of C.  A step waits for its element
+// loads, about 2 us, so few tiles of a deep product are cut into parts of the
+// depth (222 x 5690 x 101: 344 us in one part, 23 in 44 with their join).
 template <class T, bool EPI, bool AK, bool BK>
-__global__ __launch_bounds__(256) void k_product_any(const Product p) {
+__global__ __launch_bounds__(256) void k_product_any(const Product p, int splits, float* part) {
   constexpr int kT = 64, kD = 32, kRow = kD + 8;  // padded rows: 16-byte reads spread over the banks
   __shared__ alignas(16) uint16_t sa[kT * kRow], sb[kT * kRow];
-  const int tiles_n = (p.N + kT - 1) / kT;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
-  const int n0 = id % tiles_n * kT, m0 = id / tiles_n * kT;
+  const int tiles_n = (p.N + kT - 1) / kT, tiles = (p.M + kT - 1) / kT * tiles_n;
+  const int id = xcd_order(blockIdx.x, gridDim.x), sp = id / tiles;
+  const int n0 = id % tiles % tiles_n * kT, m0 = id % tiles / tiles_n * kT;
+  const int steps = (p.K + kD - 1) / kD, per = (steps + splits - 1) / splits;
+  const int k_first = min(sp * per, steps) * kD, k_end = min((sp + 1) * per, steps) * kD;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
 
   uint4 ra, rb;
@@ -163,14 +167,14 @@ __global__ __launch_bounds__(256) void k_product_any(const Product p) {
     }
   };
   floatx16 acc = {};
-  ra = fetch(p.a, AK, m0, p.M, 0);
-  rb = fetch(p.b, BK, n0, p.N, 0);
-  for (int k0 = 0; k0 < p.K; k0 += kD) {
+  ra = fetch(p.a, AK, m0, p.M, k_first);
+  rb = fetch(p.b, BK, n0, p.N, k_first);
+  for (int k0 = k_first; k0 < k_end; k0 += kD) {
     __syncthreads();
     put(sa, ra, AK);
     put(sb, rb, BK);
     __syncthreads();
-    if (k0 + kD < p.K) {
+    if (k0 + kD < k_end) {
       ra = fetch(p.a, AK, m0, p.M, k0 + kD);
       rb = fetch(p.b, BK, n0, p.N, k0 + kD);
     }
@@ -188,7 +192,11 @@ __global__ __launch_bounds__(256) void k_product_any(const Product p) {
   for (int i = 0; i < 4; ++i) {
     const int n = n0 + 32 * (wave & 1) + 8 * i + 4 * h;
     float c[4] = {acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
-    if (n < p.N) finish_any<T, EPI, 4>(p, m, n, c);
+    if (n >= p.N) continue;
+    if (splits > 1)
+      *reinterpret_cast<floatx4*>(part + ((int64_t)sp * p.M + m) * p.row + n) = floatx4{c[0], c[1], c[2], c[3]};
+    else
+      finish_any<T, EPI, 4>(p, m, n, c);
   }
 }
 
@@ -660,7 +668,8 @@ Mat lay_out(const Mat& m, char*& ws, hipStream_t s) {
 // is worth their copies: two launches and the operands' bytes against a product
 // element by element (55 TFLOP/s on 6355 x 3389 x 5488, where the copies and
 // their products take a training step at 720 TFLOP/s; the weights of few rows at a
-// fraction of the memory's rate).
+// fraction of the memory's rate).  Training steps with copies and without: 641 x 287
+// x 317 78 and 65 us, 1933 x 2123 x 82 87 and 112.
 bool worth_copies(int64_t M, int64_t N, int64_t K) {
   return std::max(N, K) <= kMaxFastStride && (M * N * K >= 1 << 27 || K * N >= 1 << 21);
 }
@@ -678,8 +687,11 @@ struct Plan {
 // tiles, two workgroups a compute unit, and where those are still too few, parts
 // of the depth of at least 4 tiles each.
 Plan plan_of(int M, int N, int K, bool fast, bool few) {
-  if (!fast) return {kAny, 1};
   auto over = [](int a, int b) { return ((int64_t)a + b - 1) / b; };
+  if (!fast) {
+    const int64_t tiles = std::max<int64_t>(1, over(M, 64) * over(N, 64));
+    return {kAny, (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCUs / tiles, over(K, 32) / 4))};
+  }
   if (few && M <= 32) {
     const int64_t wgs = over(N, 64), most = over(K, 32) / (2 * kFewWaves);
     return {kFew, (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / wgs, most))};
@@ -689,7 +701,11 @@ Plan plan_of(int M, int N, int K, bool fast, bool few) {
   const int64_t small = std::max<int64_t>(1, over(M, 128) * over(N, 128));  // M may be 0
   return {kTile128, (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCUs / small, over(K, kBK) / 4))};
 }
-int64_t plan_bytes(const Plan& pl, int64_t M, int64_t N) { return pl.splits > 1 ? pl.splits * M * chunked(N) * 4 : 0; }
+// Its parts' sums, whether the operands turn out to be aligned or not.
+int64_t plan_bytes(int M, int N, int K, bool few) {
+  const int parts = std::max(plan_of(M, N, K, true, few).splits, plan_of(M, N, K, false, few).splits);
+  return parts > 1 ? parts * (int64_t)M * chunked(N) * 4 : 0;
+}
 
 template <class T, bool EPI, bool AK, bool BK>
 void product(Product p, bool fast, float* part, hipStream_t s) {
@@ -701,7 +717,7 @@ void product(Product p, bool fast, float* part, hipStream_t s) {
   auto tiles = [&](int a, int b) { return (unsigned)(((int64_t)p.M + a - 1) / a * (((int64_t)p.N + b - 1) / b)); };
   switch (pl.kind) {
     case kAny:
-      k_product_any<T, EPI, AK, BK><<<tiles(64, 64), 256, 0, s>>>(p);
+      k_product_any<T, EPI, AK, BK><<<tiles(64, 64) * pl.splits, 256, 0, s>>>(p, pl.splits, part);
       break;
     case kFew:
       if constexpr (EPI) {
@@ -808,7 +824,7 @@ void backward(const LinearArgs& a, void* ws, hipStream_t s) {
 // The workspace follows from sizes and strides alone, whatever the pointers' alignment.
 int64_t linear_fwd_bytes(const LinearArgs& a) {
   return (copies(a, false) ? copy_bytes(x_of(a)) + copy_bytes(w_of(a)) : 0) +
-         plan_bytes(plan_of(a.M, a.N, a.K, true, true), a.M, a.N);
+         plan_bytes(a.M, a.N, a.K, true);
 }
 
 hipError_t launch_linear_fwd(const LinearArgs& a, void* ws, hipStream_t s) {
@@ -818,8 +834,7 @@ hipError_t launch_linear_fwd(const LinearArgs& a, void* ws, hipStream_t s) {
 
 int64_t linear_bwd_bytes(const LinearArgs& a) {
   const int64_t copied = copies(a, true) ? copy_bytes(x_of(a)) + copy_bytes(w_of(a)) + (a.act == kNone ? copy_bytes(dy_of(a)) : 0) : 0;
-  return dz_bytes(a) + db_bytes(a) + copied + std::max(plan_bytes(plan_of(a.M, a.K, a.N, true, false), a.M, a.K),
-                                                       plan_bytes(plan_of(a.K, a.N, a.M, true, false), a.K, a.N));
+  return dz_bytes(a) + db_bytes(a) + copied + std::max(plan_bytes(a.M, a.K, a.N, false), plan_bytes(a.K, a.N, a.M, false));
 }
 
 hipError_t launch_linear_bwd(const LinearArgs& a, void* ws, hipStream_t s) {

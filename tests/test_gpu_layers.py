@@ -422,6 +422,20 @@ def test_linear(L, case, dt):
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("case", [(222, 5690, 101), (45, 7085, 4), (57, 26, 4382), (29, 835, 62), (2000, 9, 31),
+                                  (66, 129, 127)], ids=str)
+def test_linear_odd_and_deep(L, case, dt):
+    # sizes that are not of whole chunks, one axis long: in one of the three products
+    # few tiles share a long contracted axis, in parts of which the last may be empty
+    M, K, N = case
+    g = gen_of(25)
+    x, w = normal(g, M, K, dt=dt), normal(g, K, N, dt=dt, std=K ** -0.5)
+    b, res, dy = normal(g, N, dt=dt), normal(g, M, N, dt=dt), normal(g, M, N, dt=dt)
+    check_linear(L, x, w, b, res, "silu", dy, str(case))
+    check_linear(L, x, w, None, None, "none", dy, f"{case} product alone")
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
 @pytest.mark.parametrize("case", [(3500, 136, 3600), (3584, 64, 3840), (3400, 3500, 72), (77, 3480, 3610),
                                   (3333, 129, 3601), (5, 2100, 1001), (20, 1023, 2050), (700, 1000, 301)], ids=str)
 def test_linear_large(L, case, dt):
