@@ -75,8 +75,7 @@ struct Product {
   int64_t zs;
 };
 
-// c[0..n-1] of row m, columns n0.. (W of them, at most 8): the epilogue, element
-// by element.
+// c[0..W-1] of row m, columns n0.. before N: the epilogue, element by element.
 template <class T, bool EPI, int W>
 __device__ __forceinline__ void finish_any(const Product& p, int m, int n0, float c[W]) {
   using E = typename T::E;
@@ -386,6 +385,7 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
   // the next 32 rows is on its way into LDS (each lane's own pieces) meanwhile: a
   // wavefront is alone on its SIMD and nothing else would hide its latency.
   constexpr int kRow = BN / WN + 4, kLanes = BN / WN / 8, kStep = 64 / kLanes, kSteps = 32 / kStep;
+  static_assert(BN / WN == 64, "a lane for every column");
   static_assert(NW * (32 * kRow * 4 + 2 * kSteps * 1024) <= kLds, "results and residual fit LDS");
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kRow;
   const char* res = lds + NW * 32 * kRow * 4 + wave * 2 * kSteps * 1024;
@@ -427,6 +427,32 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
       if (i + 1 < TM) load_res(i + 1);
     }
     wave_fence();
+    // An element a lane, 64 neighbours at a time (dx of 4001 x 4003 x 4005 134 us, 151 by
+    // 8 elements a lane).
+    if (!p.vec && splits == 1) {
+      using E = typename T::E;
+      const int col = n0 + wn * (BN / WN) + lane, row = m0 + wm * (BM / 2) + 32 * i;
+      const int rows = col < p.N ? min(p.M - row, 32) : 0;
+      const float add = EPI && p.bias && rows > 0 ? (float)((const E*)p.bias)[col] : 0.0f;
+#pragma unroll 1
+      for (int k = 0; k < rows; k += 8) {
+        float v[8] = {}, u[8];
+        if (EPI && p.res)  // all before the first store, which the compiler would not move them past
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (k + j < rows) v[j] = (float)((const E*)p.res)[(row + k + j) * p.rs + col];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = mine[(k + j) * kRow + lane] + add;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (k + j >= rows) break;
+          if (EPI && p.z) ((E*)p.z)[(row + k + j) * p.zs + col] = (E)u[j];
+          ((E*)p.c)[(row + k + j) * p.cs + col] = (E)(EPI ? act_value(p.act, u[j]) + v[j] : u[j]);
+        }
+      }
+      wave_fence();
+      continue;
+    }
 #pragma unroll 1
     for (int k = 0; k < kSteps; ++k) {
       const int m = first + 32 * i + k * kStep;
@@ -438,10 +464,6 @@ __global__ __launch_bounds__(128 * WN, BM == 256 ? 1 : 2) void k_product(const P
         to[0] = x, to[1] = y;
       } else {
         float c[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-        if (!p.vec) {
-          finish_any<T, EPI, 8>(p, m, n, c);
-          continue;
-        }
         const uint4 add = with_res ? *reinterpret_cast<const uint4*>(res + ((i & 1) * kSteps + k) * 1024 + 16 * lane)
                                    : make_uint4(0, 0, 0, 0);
         finish8<T, EPI>(p, m, n, c, bias, add);
