@@ -18,7 +18,10 @@ namespace pnerf {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kFwdBlocks = 16 * kCUs, kBwdBlocks = 2 * kCUs;  // workgroups, at most
+// Workgroups, at most.  The gradient's each leave a sum for dw, so they are fewer, but
+// enough for their loads to cover each other (8192 x 32 and 8192 x 8 heads of 128,
+// bf16: 79 us with 2 a compute unit, 54 with 4 or 8).
+constexpr int kFwdBlocks = 16 * kCUs, kBwdBlocks = 4 * kCUs;
 
 // 8 consecutive elements: as they are loaded, and as numbers.
 template <class E>
