@@ -379,13 +379,17 @@ int lanes(int D) {
 
 // Workgroups of both sides, in proportion to their heads: at most `most` in all
 // (the forward: what the chip holds; the backward, whose partial sums of dw each
-// cost a read: fewer).
+// cost a read: fewer), and at least one where there are heads.
 void blocks_of(const NormArgs& a, int64_t most, int b[2]) {
   const int64_t per = a.vec ? kBlock / lanes(a.D) : 4;
   int64_t want[2];
   for (int i = 0; i < 2; ++i) want[i] = ((int64_t)a.side[i].rows * a.side[i].heads + per - 1) / per;
   const int64_t all = want[0] + want[1];
-  for (int i = 0; i < 2; ++i) b[i] = (int)(all <= most ? want[i] : (want[i] * most + all - 1) / all);
+  if (all > most && want[0] && want[1]) {
+    want[0] = std::min(std::max<int64_t>(want[0] * most / all, 1), most - 1);
+    want[1] = most - want[0];
+  }
+  for (int i = 0; i < 2; ++i) b[i] = (int)std::min(want[i], most);
 }
 
 template <class E, int LR, Pairs P>
@@ -444,9 +448,13 @@ hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The workspace follows from the sizes alone: whatever the tensors' alignment, no
+// call has more workgroups than one whose heads go 4 to a workgroup.
 int64_t norm_bwd_bytes(const NormArgs& a) {
+  NormArgs any = a;
+  any.vec = 0;
   int b[2];
-  blocks_of(a, kBwdBlocks, b);
+  blocks_of(any, kBwdBlocks, b);
   return (int64_t)(b[0] + b[1]) * a.D * 4;
 }
 

@@ -619,3 +619,20 @@ def test_binding_refusals(L):
         with pytest.raises(pnerf.PnerfError) as e:
             fn()
         assert e.value.status == pnerf.ERR_INVALID_ARG
+
+
+# ---------------------------------------------------------------- more heads than workgroups
+@pytest.mark.parametrize("case", [(1025, 1025, 24, 8, 128), (1030, 1030, 28, 4, 128), (513, 513, 12, 4, 256),
+                                  (4100, 4099, 6, 2, 64), (1, 20000, 1, 1, 64), (20000, 1, 1, 3, 32)], ids=str)
+def test_norm_rotate_uneven_shares_of_the_workgroups(L, case):
+    # the gradient's workgroups are divided between queries and keys: shares that do not come out even
+    Tq, Tk, Hq, Hk, D = case
+    g = gen_of(80)
+    q, k, dq, dk = (normal(g, T, H, D, dt="bf16") for T, H in ((Tq, Hq), (Tk, Hk), (Tq, Hq), (Tk, Hk)))
+    wq, wk = normal(g, D, dt="bf16"), normal(g, D, dt="bf16")
+    table = _table(64, D)
+    pq, pk = (torch.randint(0, 64, (n,), generator=g, device="cuda", dtype=torch.int32) for n in (Tq, Tk))
+    check_norm(L, q, k, wq, wk, table, pq, pk, 1e-6, False, dq, dk, str(case))
+    odd = torch.empty(Tq * Hq * D + 1, dtype=q.dtype, device="cuda")[1:].view(Tq, Hq, D)
+    odd.copy_(q)
+    check_norm(L, odd, k, wq, wk, table, pq, pk, 1e-6, False, dq, dk, f"{case}, odd addresses")

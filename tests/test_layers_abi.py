@@ -268,3 +268,63 @@ def test_no_mfma_result_read_unpadded_after_a_branch(src, tmp_path):
     asm = out.read_text()
     assert "v_mfma" in asm and "v_pk_fma_f32" not in asm and "v_pk_mul_f32" not in asm and "v_pk_add_f32" not in asm
     assert kr.unpadded_mfma_reads_after_branches(asm) == []
+
+
+# ---------------------------------------------------------------- workspaces and their calls
+def _contiguous(p, **tensors):
+    for name, sizes in tensors.items():
+        stride, s = [], 1
+        for n in reversed(sizes):
+            s *= max(n, 1)
+            stride.append(s)
+        getattr(p, name + "_stride")[:] = tuple(reversed(stride))
+
+
+def _takes(lib, fn, p, n_tensors, workspace_of, what):
+    """The call takes as many bytes as it was said to need, wherever its tensors
+    lie (a workspace 8 bytes off stops it before anything would be launched)."""
+    n = C.c_int64(-1)
+    assert workspace_of(n) == pnerf.OK, (what, lib.pnerf_last_error())
+    for at in (PTR, PTR + 4):
+        st = fn(C.byref(p), *[at] * n_tensors, PTR + 8 if n.value else None, n.value, None)
+        says = lib.pnerf_last_error().decode()
+        assert st not in (pnerf.OK, CAPACITY), (what, at, n.value, says)
+        assert "16-byte aligned" in says if n.value else "NULL workspace" not in says, (what, at, says)
+
+
+@no_device
+@pytest.mark.parametrize("D", [32, 64, 128, 256, 100])
+def test_norm_calls_take_the_workspace_asked_for(lib, D):
+    rng = random.Random(D)
+    cases = [(T, T, h, g) for T in (1, 513, 1025, 1030, 2011, 4100, 4999) for h, g in
+             ((1, 1), (3, 1), (6, 2), (12, 4), (24, 8), (28, 4), (56, 8), (32, 8))]
+    cases += [(1001, 3003, 8, 8), (1, 100000, 1, 1), (100000, 1, 7, 1), (5000, 0, 3, 1)]
+    cases += [(rng.randint(1, 20000), rng.randint(0, 20000), rng.randint(1, 64), rng.randint(1, 16)) for _ in range(400)]
+    for Tq, Tk, Hq, Hk in cases:
+        p = norm(dtype=rng.randint(0, 2), q_rows=Tq, k_rows=Tk, q_heads=Hq, k_heads=Hk, head_dim=D, rotary_dim=0)
+        _contiguous(p, **{n: (Hq, D) for n in ("q", "q_out", "dq_out", "dq")},
+                    **{n: (Hk, D) for n in ("k", "k_out", "dk_out", "dk")})
+        _takes(lib, lib.pnerf_norm_rotate_backward, p, 8,
+               lambda n: lib.pnerf_norm_rotate_workspace(C.byref(p), C.byref(n)), (Tq, Tk, Hq, Hk, D))
+
+
+@no_device
+def test_attention_and_linear_calls_take_the_workspace_asked_for(lib):
+    rng = random.Random(7)
+
+    def size(most):
+        return rng.choice([1, rng.randint(1, 40), rng.randint(1, most), int(2 ** rng.uniform(0, most.bit_length() - 1))])
+    for _ in range(1500):
+        B, Sq, Sk, Hk, D = size(64), size(8000), size(20000), rng.randint(1, 16), rng.randint(1, 128)
+        Hq = Hk * rng.randint(1, 8)
+        p = attention(dtype=rng.randint(1, 2), batch=B, q_rows=Sq, kv_rows=Sk, q_heads=Hq, kv_heads=Hk, head_dim=D)
+        _contiguous(p, **{n: (Sq, Hq, D) for n in ("q", "o", "do", "dq")}, **{n: (Sk, Hk, D) for n in ("k", "v", "dk", "dv")})
+        for fn, back, n in ((lib.pnerf_cross_attention, 0, 5), (lib.pnerf_cross_attention_backward, 1, 9)):
+            _takes(lib, fn, p, n, lambda b: lib.pnerf_cross_attention_workspace(C.byref(p), back, C.byref(b)),
+                   (back, B, Sq, Sk, Hq, Hk, D))
+        M, N, K, pad = size(9000), size(9000), size(9000), rng.choice([0, 0, 1, 8])
+        p = linear(dtype=rng.randint(1, 2), activation=rng.randint(0, 3), m=M, n=N, k=K)
+        p.x_stride = p.dx_stride = K + pad
+        p.w_stride = p.y_stride = p.z_stride = p.dy_stride = p.dw_stride = p.residual_stride = N + pad
+        for fn, back, n in ((lib.pnerf_linear, 0, 6), (lib.pnerf_linear_backward, 1, 7)):
+            _takes(lib, fn, p, n, lambda b: lib.pnerf_linear_workspace(C.byref(p), back, C.byref(b)), (back, M, N, K, pad))
