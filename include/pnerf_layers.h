@@ -61,10 +61,11 @@ extern "C" {
  *   ds_ij = p_ij (do_i . v_j - delta_i),  dv_j = sum p_ij do_i,
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum ds_ij q_i
  * (dk, dv: summed over the rows and the query heads that share the kv head; 0
- * where the key is not allowed).  p and ds are rounded to the data type (float16:
- * times a power of two that grows with kv_rows beyond 8192, which keeps them normal).  A
- * batch entry's dk and dv are its own also where k and v are one tensor
- * broadcast over the batch.
+ * where the key is not allowed).  p and ds are rounded to the data type.  In float16
+ * they are kept times powers of two on the way: p times 2^14, ds times one that a row
+ * (dq) or a key (dk) takes from the norms of do and v, such that no ds overflows and
+ * one is a normal number down to 2^-28 of 2 max |do| max |v|.  A batch entry's dk and
+ * dv are its own also where k and v are one tensor broadcast over the batch.
  *
  * Requires 0 <= batch <= 65535, q_rows, kv_rows >= 0, kv_heads >= 1, q_heads a
  * multiple of kv_heads (at most 65535), 1 <= head_dim <= 128, finite scale > 0,

@@ -11,8 +11,20 @@
 //
 // Fragments as in the forward kernel: what the second products contract over is
 // in the registers of the first ones' results, as their B operand.
+//
+// Float16 and its range: p and ds are rounded to 16 bits as operands, and float16
+// has normal numbers from 2^-14 to 2^16 alone.  p is at most 1 and is kept times
+// 2^14.  ds may be anything: |ds_ij| <= |do_i| |v_j| + |delta_i|, and |delta_i| <= |do_i|
+// max |v|.  Both kernels hold a row (dq) or a key (dk) a lane and contract over the
+// other, so each lane keeps its ds times a power of two of its own, by which that
+// bound lies in [2^14, 2^15), and divides its sums by it: no ds overflows, and one
+// is a normal number down to 2^-28 of the bound.  The norms are made with the rows'
+// statistics and a workgroup takes the largest of its part at its start (the whole
+// gradient with it and without: 333 and 326 us for 2 x 2011 rows, 2500 keys, 16 heads of
+// 128; 70 and 63 for 2 x 1024 rows, 1200 keys, 16 heads of 64).
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_common.h"
 
@@ -23,14 +35,62 @@ constexpr int kKeys = 128;  // keys of a workgroup of the dk, dv pass: 32 a wave
 // Rows of one of its tiles.
 constexpr int dkv_rows(int width, bool fast) { return fast && width == 128 ? 32 : 64; }
 
-// (lse / ln 2 - shift, delta) of every row; (+inf, 0) where the row has no
-// allowed key or is past q_len, which makes all of its p zero.
+template <class T>
+constexpr bool kNarrow = std::is_same_v<T, F16>;  // p and ds are kept times powers of two
+template <class T>
+constexpr int kBitsP = kNarrow<T> ? 14 : 0;       // ... p times 2^kBitsP
+
+// The power of two by which a number of at most `bound` stays below 2^15.  (A delta
+// may be as small as p is, and with it the bound: the power has an end.)
+__device__ __forceinline__ int bits_within(float bound) {
+  return bound > 0.0f ? 15 - max(__builtin_amdgcn_frexp_expf(bound), -80) : 0;
+}
+// The maximum of x over the NW wavefronts of a workgroup, by way of red.
+template <int NW>
+__device__ __forceinline__ float max_of_all(float x, float* red) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = red[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) x = fmaxf(x, red[i]);
+  return x;
+}
+// The sum of squares of 8 elements.
+template <class T>
+__device__ __forceinline__ float squares(uint4 x) {
+  return T::lo(x.x) * T::lo(x.x) + T::hi(x.x) * T::hi(x.x) + T::lo(x.y) * T::lo(x.y) + T::hi(x.y) * T::hi(x.y) +
+         T::lo(x.z) * T::lo(x.z) + T::hi(x.z) * T::hi(x.z) + T::lo(x.w) * T::lo(x.w) + T::hi(x.w) * T::hi(x.w);
+}
+
+// |v| of key `at` in memory order, DP / 8 lanes a key with 8 elements each from d.
+template <class T, int DP, bool VEC>
+__device__ __forceinline__ void v_norm(const AttnArgs& a, int64_t at, int d) {
+  const int g = (int)(at % a.Hkv), bj = (int)(at / a.Hkv), j = bj % a.Sk, b = bj / a.Sk;
+  const bool ok = j < clamp_len(a.kv_len, b, a.Sk) && (!a.mask || a.mask[b * a.mask_stride + j]);
+  float sq = squares<T>(load8<VEC>((const uint16_t*)a.v + b * a.vs[0] + (int64_t)j * a.vs[1] + g * a.vs[2] + d,
+                                   ok ? min(a.D - d, 8) : 0));
+#pragma unroll
+  for (int m = DP / 16; m; m >>= 1) sq += __shfl_xor(sq, m);
+  if (d == 0) a.v_norm[((int64_t)b * a.Hkv + g) * a.Sk + j] = sqrtf(sq);
+}
+
+// (lse / ln 2 - kBitsP, delta) of every row; (+inf, 0) where the row has no
+// allowed key or is past q_len, which makes all of its p zero.  Float16: |do| too,
+// and in the grid's second row |v| of every key (0 where it may not be read).
 template <class T, int DP, bool VEC>
 __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
   constexpr int LR = DP / 8;  // lanes of a row
   const int64_t rows = (int64_t)a.B * a.Hq * a.Sq;
   const int64_t at = (int64_t)blockIdx.x * (256 / LR) + threadIdx.x / LR;
   const int d = 8 * (threadIdx.x % LR);
+  if constexpr (kNarrow<T>) {
+    if (blockIdx.y == 1) {
+      if (at < (int64_t)a.B * a.Hkv * a.Sk) v_norm<T, DP, VEC>(a, at, d);
+      return;
+    }
+  }
   float sum = 0.0f;
   if (at < rows) {
     // neighbours are the heads of one row, as they are in memory
@@ -50,9 +110,16 @@ __global__ __launch_bounds__(256) void k_attn_stat(const AttnArgs a) {
     for (int m = LR / 2; m; m >>= 1) sum += __shfl_xor(sum, m);
     if (d == 0)
       reinterpret_cast<floatx2*>(a.delta)[out] =
-          ok ? floatx2{lse * 1.4426950408889634f - (float)a.shift, sum} : floatx2{INFINITY, 0.0f};
+          ok ? floatx2{lse * 1.4426950408889634f - (float)kBitsP<T>, sum} : floatx2{INFINITY, 0.0f};
+    if constexpr (kNarrow<T>) {
+      float sq = squares<T>(y);
+#pragma unroll
+      for (int m = LR / 2; m; m >>= 1) sq += __shfl_xor(sq, m);
+      if (d == 0) a.do_norm[out] = sqrtf(sq);
+    }
   }
 }
+
 
 // dq: four wavefronts of 32 rows share the tiles of keys and values, two of them
 // in LDS (FAST; else one, by way of registers).  As in the forward kernel the row
@@ -114,6 +181,17 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, 
     load(0, t, vm_next);
     allowed = may_read((t + KS) * kBN + lane);
   }
+  int bits = 0;  // of this row's ds
+  if constexpr (kNarrow<T>) {
+    __shared__ float red[4 * KS];
+    const float* norms = a.v_norm + ((int64_t)b * a.Hkv + g) * a.Sk;
+    float v = 0.0f;
+#pragma unroll 4
+    for (int j = t0 * kBN + threadIdx.x; j < min(t1 * kBN, nk); j += 256 * KS) v = fmaxf(v, norms[j]);
+    v = max_of_all<4 * KS>(v, red);
+    if (ok) bits = bits_within(2.0f * v * a.do_norm[((int64_t)b * a.Hq + head) * a.Sq + qi]);
+    st[0] += (float)(kBitsP<T> - bits);  // p of this kernel is kept times 2^bits
+  }
   const int rounds = (t1 - t0 + KS - 1) / KS;  // the same for both groups: they share the barrier
   for (int round = 0; round < rounds; ++round, t += KS) {
     const int buf = FAST ? round & 1 : 0;
@@ -161,8 +239,8 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, 
       }
       float s0, s1;
       halves(sum, s0, s1);
-      st[1] = ldexpf(s0 + s1, -a.shift);
-      if (h == 0 && ok) *stat = st;
+      st[1] = ldexpf(s0 + s1, -bits);
+      if (h == 0 && ok) (*stat)[1] = st[1];
     }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -209,11 +287,12 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, 
       }
   }
   if (row >= a.M) return;
+  const float back = ldexpf(1.0f, -bits);
   if (splits > 1) {
-    if (t0 < t1) store_part<DP>(acc, part + (sp * rows + at) * DP, h);
+    if (t0 < t1) store_part<DP>(acc, part + (sp * rows + at) * DP, h, back);
   } else {
     uint16_t* out = (uint16_t*)a.dq + b * a.dqs[0] + (int64_t)qi * a.dqs[1] + head * a.dqs[2];
-    store_cols<T, DP, FAST>(acc, out, ldexpf(a.scale, -a.shift), a.D, h);
+    store_cols<T, DP, FAST>(acc, out, a.scale * back, a.D, h);
   }
 }
 
@@ -297,6 +376,25 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
     next();
   };
   if (FAST && t0 < t1) load(t0 & 1);
+  int bits = 0;  // of this key's ds
+  if constexpr (kNarrow<T>)
+    if (t0 < t1) {
+      // the largest |do| and |delta| of this part's rows, from its first to its last
+      __shared__ float red[2][4];
+      const int64_t head0 = ((int64_t)b * a.Hq + g * a.G) * a.Sq;
+      const int h0 = t0 / tiles_q, h1 = (t1 - 1) / tiles_q;
+      const int i0 = h0 * a.Sq + (t0 - h0 * tiles_q) * kR, i1 = h1 * a.Sq + min((t1 - h1 * tiles_q) * kR, nq);
+      float x = 0.0f, y = 0.0f;
+#pragma unroll 4
+      for (int i = i0 + tid; i < i1; i += 256) {
+        x = fmaxf(x, a.do_norm[head0 + i]);
+        y = fmaxf(y, fabsf(a.delta[2 * (head0 + i) + 1]));
+      }
+      x = max_of_all<4>(x, red[0]);
+      y = max_of_all<4>(y, red[1]);
+      if (ok) bits = bits_within(fmaf(x, a.v_norm[((int64_t)b * a.Hkv + g) * a.Sk + key], y));
+    }
+  const float up = ldexpf(1.0f, bits - kBitsP<T>);  // ds comes out times 2^kBitsP, as p does
   for (int t = t0; t < t1; ++t) {
     if (FAST) {
       wait_loads();
@@ -323,6 +421,7 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
         s[i + 1] = __builtin_amdgcn_exp2f(fmaf(s[i + 1], a.c, -st[2]));
         dp[i] = s[i] * (dp[i] - st[1]);
         dp[i + 1] = s[i + 1] * (dp[i + 1] - st[3]);
+        if (kNarrow<T>) dp[i] *= up, dp[i + 1] *= up;
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -340,18 +439,18 @@ __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a
   if (!ok)
 #pragma unroll
     for (int i = 0; i < ND; ++i) dk[i] = dv[i] = floatx16{};
+  const float back_k = ldexpf(1.0f, -bits), back_v = ldexpf(1.0f, -kBitsP<T>);
   if (splits > 1) {
     if (t0 >= t1) return;  // the sum reads no empty part
     const int64_t keys = (int64_t)a.B * a.Hkv * a.Sk, at = ((int64_t)b * a.Hkv + g) * a.Sk + key;
     float* p = part + 2 * (sp * keys + at) * DP;
-    store_part<DP>(dk, p, h);
-    store_part<DP>(dv, p + DP, h);
+    store_part<DP>(dk, p, h, back_k);
+    store_part<DP>(dv, p + DP, h, back_v);
   } else {
-    const float back = ldexpf(1.0f, -a.shift);
     store_cols<T, DP, FAST>(dk, (uint16_t*)a.dk + b * a.dks[0] + (int64_t)key * a.dks[1] + g * a.dks[2],
-                            a.scale * back, a.D, h);
+                            a.scale * back_k, a.D, h);
     store_cols<T, DP, FAST>(dv, (uint16_t*)a.dv + b * a.dvs[0] + (int64_t)key * a.dvs[1] + g * a.dvs[2],
-                            back, a.D, h);
+                            back_v, a.D, h);
   }
 }
 
@@ -377,7 +476,7 @@ __global__ __launch_bounds__(256) void k_attn_sum(const AttnArgs a, int splits, 
   floatx4 x = {};
 #pragma unroll 4
   for (int s = 0; s < parts; ++s) x += *reinterpret_cast<const floatx4*>(part + s * n + e);
-  const float f = ldexpf(val ? 1.0f : a.scale, -a.shift);
+  const float f = val ? 1.0f : a.scale;
   uint16_t* out;
   if (!KV)
     out = (uint16_t*)a.dq + b * a.dqs[0] + (int64_t)(at / a.G) * a.dqs[1] + (g * a.G + at % a.G) * a.dqs[2];
@@ -407,6 +506,9 @@ bool fast_rows(const AttnArgs& a) {
   return fits(a.qs[1]) && fits(a.dos[1]);
 }
 int64_t stat_floats(const AttnArgs& a) { return ((int64_t)2 * a.B * a.Hkv * a.M + 3) / 4 * 4; }
+int64_t norm_floats(const AttnArgs& a) {
+  return a.dtype == kF16 ? ((int64_t)a.B * a.Hkv * ((int64_t)a.M + a.Sk) + 3) / 4 * 4 : 0;
+}
 int64_t dq_floats(const AttnArgs& a) {
   const int s = dq_splits(a);
   return s > 1 ? (int64_t)s * a.B * a.Hkv * a.M * padded(a.D) : 0;
@@ -421,7 +523,8 @@ void launch(const AttnArgs& a, float* part_q, float* part_kv, hipStream_t s) {
   const int64_t rows = (int64_t)a.B * a.Hkv * a.M, keys = (int64_t)a.B * a.Hkv * a.Sk;
   if (rows) {
     const int per = 256 / (DP / 8);
-    k_attn_stat<T, DP, FAST><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(a);
+    const int64_t most = kNarrow<T> ? std::max(rows, keys) : rows;
+    k_attn_stat<T, DP, FAST><<<dim3((unsigned)((most + per - 1) / per), kNarrow<T> ? 2 : 1), 256, 0, s>>>(a);
     const int ns = dq_splits(a);
     const Order o = order_of(((int64_t)a.M + 127) / 128, a.Hkv);
     const int64_t n = workgroups(o, ns, a);
@@ -457,13 +560,15 @@ void launch_t(const AttnArgs& a, float* pq, float* pk, hipStream_t s) {
 }  // namespace
 
 int64_t attn_bwd_bytes(const AttnArgs& a) {
-  return 4 * (stat_floats(a) + dq_floats(a) + dkv_floats(a));
+  return 4 * (stat_floats(a) + norm_floats(a) + dq_floats(a) + dkv_floats(a));
 }
 
 hipError_t launch_attn_bwd(const AttnArgs& a0, void* ws, hipStream_t s) {
   AttnArgs a = a0;
   a.delta = (float*)ws;
-  float* pq = a.delta + stat_floats(a);
+  a.do_norm = a.delta + stat_floats(a);
+  a.v_norm = a.do_norm + (int64_t)a.B * a.Hkv * a.M;
+  float* pq = a.do_norm + norm_floats(a);
   float* pk = pq + dq_floats(a);
   if (a.B == 0) return hipSuccess;
   a.dtype == kF16 ? launch_t<F16>(a, pq, pk, s) : launch_t<BF16>(a, pq, pk, s);

@@ -188,13 +188,13 @@ __device__ __forceinline__ void store_cols(const floatx16* acc, uint16_t* p, flo
     }
 }
 template <int DP>
-__device__ __forceinline__ void store_part(const floatx16* acc, float* p, int h) {
+__device__ __forceinline__ void store_part(const floatx16* acc, float* p, int h, float f = 1.0f) {
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<floatx4*>(p + 32 * d + 8 * i + 4 * h) =
-          floatx4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+          floatx4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]} * f;
 }
 
 __device__ __forceinline__ float log_sum(float m, float l) {  // m in units of ln 2

@@ -137,10 +137,6 @@ pnerf_status attention_args(const pnerf_attention_params* p, AttnArgs* out, bool
     return fail(PNERF_ERR_INVALID_ARG, "kv_mask has stride %lld", (long long)a.mask_stride);
   if ((a.q_len && !aligned(a.q_len, 4)) || (a.kv_len && !aligned(a.kv_len, 4)))
     return fail(PNERF_ERR_INVALID_ARG, "q_len and kv_len must be aligned to 4 bytes");
-  // float16 p and ds of a row over very many keys would fall below the normal
-  // numbers (2^-14): a typical p is 1 / kv_rows, kept times 2^shift
-  if (backward && a.dtype == kF16)
-    for (int s = a.Sk >> 13; s; s >>= 1) ++a.shift;
   a.splits = backward ? 1 : attn_fwd_splits(a);
   *out = a;
   return PNERF_OK;

@@ -32,8 +32,8 @@ struct AttnArgs {
   const void* dout;
   void *dq, *dk, *dv;
   int64_t dos[3], dqs[3], dks[3], dvs[3];
-  float* delta;     // [B][Hkv][M]
-  int shift;        // p and ds are kept times 2^shift (float16 only)
+  float* delta;     // (lse, delta) of every row [B][Hq][Sq]
+  float *do_norm, *v_norm;  // float16: |do| of every row, |v| of every key [B][Hkv][Sk]
 };
 
 // Parts of the key axis and bytes of workspace of the forward pass.
