@@ -636,3 +636,26 @@ def test_norm_rotate_uneven_shares_of_the_workgroups(L, case):
     odd = torch.empty(Tq * Hq * D + 1, dtype=q.dtype, device="cuda")[1:].view(Tq, Hq, D)
     odd.copy_(q)
     check_norm(L, odd, k, wq, wk, table, pq, pk, 1e-6, False, dq, dk, f"{case}, odd addresses")
+
+
+# ---------------------------------------------------------------- GELU's tail
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_gelu_tail_is_relatively_exact(L, dt):
+    # far below zero GELU is small and the data type holds it as exactly as any number: the
+    # bound is relative.  2^-19 for the form and its steps, and 2^-23 z^2 for the exponent,
+    # three of whose roundings (2^-24 each) weigh z^2 / 2 there.
+    z = -torch.linspace(0.01, 5.5 if dt == "f16" else 12.5, 4000, device="cuda").to(R.DT[dt]).unique()
+    x, w = z[:, None].contiguous(), torch.ones(1, 8, dtype=z.dtype, device="cuda")
+    y, kept = L.linear(x, w, activation="gelu", return_preact=True)
+    assert torch.equal(kept[:, 0], z)
+    Z = z.double()
+    phi = 0.5 * torch.special.erfc(-Z * math.sqrt(0.5))
+    density = torch.exp(-0.5 * Z * Z) / math.sqrt(2 * math.pi)
+    e = 2.0 ** -19 + 2.0 ** -23 * Z * Z
+    R.check(y[:, 0], Z * phi, (R.U[dt] + e) * (Z * phi).abs() + R.TINY[dt], "gelu")
+    dy = torch.zeros_like(y)
+    dy[:, 0] = 1.0
+    dx, _, _ = L.linear_backward(dy, x, w, kept, activation="gelu", bias=False)
+    slope = phi + Z * density
+    # dz is rounded, and its product with 1 once more
+    R.check(dx[:, 0], slope, 2 * R.U[dt] * slope.abs() + e * (phi + (Z * density).abs()) + 2 * R.TINY[dt], "gelu'")
