@@ -843,7 +843,10 @@ void backward(const LinearArgs& a, void* ws, hipStream_t s) {
     p.a = {x.p, 1, x.stride};
     p.b = {dz.p, 1, dz.stride};
     p.c = a.dw, p.cs = a.dws;
-    product<T, false, false, false>(p, dz_ready && (copy || ready(x)), (float*)at, s);
+    // the rows past a single one are beyond the descriptor's bound only while their
+    // 32-bit offsets do not come round
+    const bool near = std::max(x.stride, dz.stride) <= kMaxFastStride;
+    product<T, false, false, false>(p, near && dz_ready && (copy || ready(x)), (float*)at, s);
   }
 }
 

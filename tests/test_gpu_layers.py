@@ -659,3 +659,23 @@ def test_gelu_tail_is_relatively_exact(L, dt):
     slope = phi + Z * density
     # dz is rounded, and its product with 1 once more
     R.check(dx[:, 0], slope, 2 * R.U[dt] * slope.abs() + e * (phi + (Z * density).abs()) + 2 * R.TINY[dt], "gelu'")
+
+
+# ---------------------------------------------------------------- one very long row
+@pytest.mark.parametrize("K,N", [(8, 1 << 26), (1 << 26, 8)])
+def test_linear_gradient_of_one_very_long_row(L, K, N):
+    # the rows that a tile has beyond the only one are zeros, however long a row is: an
+    # infinity meets no other row's zero
+    say("linear, one long row", K, N)
+    x, dy = torch.ones(1, K, dtype=torch.float16, device="cuda"), torch.ones(1, N, dtype=torch.float16, device="cuda")
+    w = torch.ones(1, N, dtype=torch.float16, device="cuda").expand(K, N)
+    long = x if K > N else dy
+    long[0, 12345], long[0, -1] = math.inf, 3.0
+    dw = torch.empty(K, N, dtype=torch.float16, device="cuda")
+    dx = torch.empty(1, K, dtype=torch.float16, device="cuda")
+    L.linear_backward(dy, x, w, bias=False, dw=dw, dx=dx)
+    want = long[0]
+    for row in (dw.t() if K > N else dw):
+        assert torch.equal(row, want)
+    del dw, dx
+    torch.cuda.empty_cache()
