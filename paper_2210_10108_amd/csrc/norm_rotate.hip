@@ -109,7 +109,12 @@ __device__ __forceinline__ void partners(const NormArgs& a, int d, const float v
   }
 }
 
-__device__ __forceinline__ float inv_rms(float mean, float eps) { return __builtin_amdgcn_rsqf(mean + eps); }
+// (The instruction takes a subnormal number for zero.)
+__device__ __forceinline__ float inv_rms(float mean, float eps) {
+  const float x = mean + eps;
+  const bool small = x < 0x1p-126f;
+  return __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x) * (small ? 0x1p32f : 1.0f);
+}
 
 // Cosines and sines of a lane's 8 elements at position pos: element i turns
 // with its partner by (c[i], s[i]), s negated for the first of a pair; (1, 0)

@@ -679,3 +679,15 @@ def test_linear_gradient_of_one_very_long_row(L, K, N):
         assert torch.equal(row, want)
     del dw, dx
     torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------- small rows without eps
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 33])
+def test_norm_rotate_small_rows_without_eps(L, D, dt):
+    # with eps = 0 a row's size does not matter; here its mean square is a subnormal
+    # number of 32 bits, exact to 2^-23 still
+    g = gen_of(90)
+    q, dq, w = normal(g, 9, 3, D, dt="f32"), normal(g, 9, 3, D, dt=dt), normal(g, D, dt=dt)
+    q = (q * 8e-20).to(R.DT[dt])
+    check_norm(L, q, None, w, None, None, None, None, 0.0, False, dq, None, f"small rows {D}")
