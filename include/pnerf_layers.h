@@ -31,7 +31,10 @@
  *    elements will do; the fast kernels want every row to start on 16 bytes
  *    (pointers and strides), as contiguous tensors with rows of a multiple of 8
  *    16-bit elements do.  (Linear layers copy large operands of other sizes and
- *    strides to such rows in the workspace.)
+ *    strides to such rows in the workspace.  The workspace follows from sizes and
+ *    strides alone: where those are of whole 16-byte chunks and only a pointer is off 16
+ *    bytes nothing is copied, and a large product runs element by element, an order
+ *    of magnitude slower.)
  *  - The same inputs give the same bits on every call (no atomics on results).
  */
 #ifndef PNERF_LAYERS_H
@@ -140,8 +143,9 @@ pnerf_status pnerf_norm_rotate_backward(const pnerf_norm_rotate_params* params, 
 /* Linear layer, weights [in][out] as the field's networks keep them:
  *   z = x W + bias,  y = act(z) + residual
  * x [m][k], W [k][n], bias [n], residual, y, z [m][n]; bias, residual and z may be
- * NULL.  z is act's argument, kept for the backward.  y may be the residual
- * itself (same pointer and stride).
+ * NULL.  z is act's argument, kept for the backward, which takes act' at it as it
+ * was rounded to the data type.  y may be the residual itself (same pointer and
+ * stride).
  * Backward, given dy:  dz = dy act'(z),  dx = dz W^T,  dW = x^T dz,  db = sum_m dz;
  * dz is rounded to the data type before the products.  The gradient of the
  * residual is dy.  z may be NULL when activation is 0; dx, dw and db may each be

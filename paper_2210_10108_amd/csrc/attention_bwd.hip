@@ -301,7 +301,7 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_dq(const AttnArgs a, 
 // (whose addresses are a plain progression) that the workgroup's wavefronts share.
 // At the wide head the sums take 128 registers and the keys 32; the values, each
 // lane's its own, wait in LDS, which leaves registers for two wavefronts a SIMD
-// (4 x 4096 rows and keys, 16 heads of 128: 1.00 to 1.05 PFLOP/s; with the values in
+// (4 x 4096 rows and keys, 16 heads of 128, bf16: 1.00 to 1.05 PFLOP/s; with the values in
 // registers and one wavefront a SIMD 0.70).  The tiles are then of 32 rows.
 template <class T, int DP, bool FAST>
 __global__ __launch_bounds__(256, FAST ? 2 : 1) void k_attn_dkv(const AttnArgs a, const Order order, int splits, float* part) {

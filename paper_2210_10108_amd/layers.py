@@ -8,7 +8,8 @@ enqueues its kernels on `stream` (default: the device's current stream) and
 returns.  Outputs and workspaces that it allocates are torch's memory of that
 stream, and inputs used on another stream than the current one are recorded on
 it, so tensors may be dropped while the work is queued; what the streams wait
-for is the caller's, as everywhere in torch.
+for is the caller's, as everywhere in torch.  No call makes an autograd graph,
+whatever requires_grad says: every operator has its *_backward function.
 """
 from __future__ import annotations
 

@@ -13,7 +13,8 @@ encoder's states are the image's patches, made of the layer operators alone:
 ProposalBlock runs it forward, for a batch of hypotheses or one at a time, and
 backward.  `python -m paper_2210_10108_amd.propose` trains it on views of a
 synthetic field and reports how far the hypotheses are from the true pose
-before and after; the proposals are what Field.render_loss_grad starts from.
+before and after.  The proposals are poses as Field.render_loss_grad takes them;
+the optimisation itself is not run here.
 """
 from __future__ import annotations
 
