@@ -536,11 +536,12 @@ def _exact_quant(s):
         for t in range(0, Sk, BLOCK):
             part = x[:, t:t + BLOCK].double() * on[:, t:t + BLOCK, None, None]
             most = part.abs().amax((1, 3))
-            power = torch.where(most > 0, torch.ceil(torch.log2(most.clamp_min(1e-300) / 448.0)), 0.0)
-            power = torch.where(torch.exp2(power) * 448.0 < most, power + 1, power)
-            blocks.append(torch.exp2(power))
+            # most = m 2^e with m in [1/2, 1), and 448 = 7/8 2^9
+            m, e = torch.frexp(most)
+            power = torch.where(most > 0, torch.where(m <= 0.875, e - 9, e - 8), 0)
+            blocks.append(torch.ldexp(torch.ones_like(most), power))
             part = part / blocks[-1][:, None, :, None]
-            step = torch.exp2(torch.floor(torch.log2(part.abs().clamp_min(2.0 ** -6))) - 3)
+            step = torch.ldexp(torch.ones_like(part), torch.frexp(part.abs().clamp_min(2.0 ** -6))[1] - 4)
             x8[:, t:t + BLOCK] = torch.round(part / step) * step
         values.append(x8)
         scales.append(torch.stack(blocks, 1))
