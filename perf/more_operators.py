@@ -357,7 +357,7 @@ def _plain_quant(s):
         x = torch.cat([x, pad], 1).view(B, blocks, BLOCK, Hkv, D)
         most = x.abs().amax((2, 4))
         m, e = torch.frexp(most / 448.0)  # m in [1/2, 1)
-        scale = torch.ldexp(torch.ones_like(most), torch.where(m == 0.5, e - 1, e))
+        scale = ((torch.where(m == 0.5, e - 1, e) + 127) << 23).view(torch.float32)  # by its bits: exact
         scale = torch.where(most == 0, torch.ones_like(scale), scale)
         x = (x / scale[:, :, None, :, None]).to(torch.float8_e4m3fn)
         return x.view(B, blocks * BLOCK, Hkv, D)[:, :Sk].contiguous(), scale
@@ -523,6 +523,11 @@ def _exact_clip(s):
     return [total, flat]
 
 
+def _power_of_two(e):
+    """2^e in 64 bits, by its bits (exp2 and ldexp round on some devices)."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
 def _exact_quant(s):
     """Scales by powers of two until the largest value fits; values to the nearest
     of e4m3's numbers (steps of 2^-9 below 2^-6, of an eighth of the power of two
@@ -539,9 +544,9 @@ def _exact_quant(s):
             # most = m 2^e with m in [1/2, 1), and 448 = 7/8 2^9
             m, e = torch.frexp(most)
             power = torch.where(most > 0, torch.where(m <= 0.875, e - 9, e - 8), 0)
-            blocks.append(torch.ldexp(torch.ones_like(most), power))
+            blocks.append(_power_of_two(power))
             part = part / blocks[-1][:, None, :, None]
-            step = torch.ldexp(torch.ones_like(part), torch.frexp(part.abs().clamp_min(2.0 ** -6))[1] - 4)
+            step = _power_of_two(torch.frexp(part.abs().clamp_min(2.0 ** -6))[1] - 4)
             x8[:, t:t + BLOCK] = torch.round(part / step) * step
         values.append(x8)
         scales.append(torch.stack(blocks, 1))
