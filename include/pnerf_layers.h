@@ -9,6 +9,14 @@
  *                           position rotation in one pass, and its gradient
  *   pnerf_linear            matrix product with bias, activation and residual,
  *                           and its gradient
+ *   pnerf_layer_norm        the norm of whole rows, with mean and bias, and its
+ *                           gradient
+ *   pnerf_rotate_axes       the position rotation where positions have several axes
+ *                           (a patch's row, column and frame), with or without the
+ *                           norm, and its gradient
+ *   pnerf_clip_gradients    the norm over all gradients of a step, and their scaling
+ *   pnerf_quantize_states   keys and values in 8 bits, a scale for each block of rows
+ *   pnerf_cross_attention_q8  attention to such states
  *
  * The conventions of pnerf.h hold: arguments are validated on the host before
  * anything is enqueued (PNERF_ERR_INVALID_ARG or PNERF_ERR_NOT_SUPPORTED, the
@@ -172,6 +180,129 @@ pnerf_status pnerf_linear(const pnerf_linear_params* params, const void* x, cons
 pnerf_status pnerf_linear_backward(const pnerf_linear_params* params, const void* x, const void* w,
                                    const void* z, const void* dy, void* dx, void* dw, void* db,
                                    void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Layer norm of every row x of `width` W elements:
+ *   y_d = (x_d - mean) r w_d + b_d,  r = 1 / sqrt(mean_d (x_d - mean)^2 + eps)
+ * y may be x itself (same pointer and stride).
+ * Backward, given dy and, if not NULL, dres (the gradient that reaches x past the
+ * norm, of a residual connection), with g_d = dy_d w_d, n_d = (x_d - mean) r:
+ *   dx_d = r (g_d - mean g - n_d mean(g n)) + dres_d
+ *   dweight_d = sum_rows dy_d n_d,  dbias_d = sum_rows dy_d
+ * dx may be dy, dres or x itself.  weight (ones) and bias (zeros) may be NULL, dweight
+ * and dbias too (not wanted).  A row is what its elements were rounded to: the mean is
+ * taken in two steps, so that a mean large beside the spread costs nothing more.  A row
+ * of equal elements has n = 0 where eps > 0, NaN where eps = 0; squares of a row's
+ * differences past float32's range make it infinite or NaN.
+ *
+ * Requires rows >= 0, 1 <= width <= 2^20, rows * width at most 2^40, finite eps >= 0;
+ * any dtype. */
+typedef struct {
+  int32_t dtype, rows, width;
+  float eps;
+  /* row strides; the last three are read by the backward only */
+  int64_t x_stride, y_stride, dy_stride, dres_stride, dx_stride;
+} pnerf_layer_norm_params;
+
+pnerf_status pnerf_layer_norm(const pnerf_layer_norm_params* params, const void* x,
+                              const void* weight, const void* bias, void* y, void* stream);
+pnerf_status pnerf_layer_norm_workspace(const pnerf_layer_norm_params* params, int64_t* bytes);
+pnerf_status pnerf_layer_norm_backward(const pnerf_layer_norm_params* params, const void* x,
+                                       const void* weight, const void* dy, const void* dres,
+                                       void* dx, void* dweight, void* dbias, void* workspace,
+                                       int64_t workspace_bytes, void* stream);
+
+/* Rotation at positions of several axes: as pnerf_norm_rotate with
+ *   c_j = table[t_a][0][j], s_j = table[t_a][1][j],  a = pair_axis[j],
+ * t_a the row's position along axis a: base.q_pos is [q_rows][axes], base.k_pos
+ * [k_rows][axes].  Every frequency an axis may want is in the columns of its pairs.
+ * A position outside [0, n_positions) gives NaN in the pairs of its axis.
+ * norm = 1: the heads are normed first, as there; norm = 0: n = x, the weights are not
+ * read, the gradient is the rotation back alone (q and k are not read and may be NULL,
+ * no weight has a gradient, no workspace is needed).
+ *
+ * Requires what pnerf_norm_rotate does, norm 0 or 1, 1 <= axes <= 4 and
+ * pair_axis[j] < axes for the rotary_dim / 2 pairs. */
+typedef struct {
+  pnerf_norm_rotate_params base;
+  int32_t norm, axes;
+  uint8_t pair_axis[128];
+} pnerf_rotate_axes_params;
+
+pnerf_status pnerf_rotate_axes(const pnerf_rotate_axes_params* params, const void* q, const void* k,
+                               void* q_out, void* k_out, void* stream);
+pnerf_status pnerf_rotate_axes_workspace(const pnerf_rotate_axes_params* params, int64_t* bytes);
+pnerf_status pnerf_rotate_axes_backward(const pnerf_rotate_axes_params* params, const void* q,
+                                        const void* k, const void* dq_out, const void* dk_out,
+                                        void* dq, void* dk, void* dq_weight, void* dk_weight,
+                                        void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The norm over all elements of `count` gradients and their scaling by it:
+ *   norm = sqrt(sum g^2),  out = c g,  c = min(1, max_norm / (norm + eps))
+ * Squares and their sum are float64; norm (device) is the result in float32, c is
+ * rounded to float32, c g to the output's type.  An output may be its gradient (same
+ * pointer and dtype; where c = 1 it is not touched), and overlaps no other gradient or
+ * output.  max_norm may be infinite: c = 1.  A NaN among the gradients makes the norm
+ * and every output NaN (max_norm infinite: the norm alone); an infinity makes the norm
+ * infinite and c = 0.
+ * `gradients` (host) is read before the call returns.
+ *
+ * Requires 0 <= count <= 65536, n >= 0, all n together at most 2^42, out_dtype the
+ * gradient's or PNERF_F32, max_norm > 0, finite eps >= 0. */
+typedef struct {
+  const void* grad; /* (device) [n] */
+  void* out;        /* (device) [n] */
+  int64_t n;
+  int32_t dtype, out_dtype;
+} pnerf_gradient;
+
+pnerf_status pnerf_clip_gradients_workspace(int32_t count, int64_t* bytes);
+pnerf_status pnerf_clip_gradients(const pnerf_gradient* gradients, int32_t count, double max_norm,
+                                  double eps, float* norm, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/* Keys and values in 8 bits.  For each block of PNERF_STATE_BLOCK rows of a head,
+ * over its allowed rows (as for pnerf_cross_attention):
+ *   scale = the least power of two, at least 2^-126, with max |x| <= 448 scale
+ *           (1 where all x are 0 or no row is allowed)
+ *   x8 = x / scale to the nearest e4m3 number (ties to the even one; no infinities:
+ *        those of x become NaN, which like NaN do not count for the scale)
+ * x8 is 0 in rows that are not allowed; what x holds there has no influence.
+ * k8, v8 are bytes [batch][kv_rows][kv_heads][head_dim], the scales float32
+ * [batch][blocks][kv_heads], blocks = kv_rows / PNERF_STATE_BLOCK rounded up.
+ *
+ * Requires of the sizes what pnerf_cross_attention does; dtype PNERF_F16 or PNERF_BF16. */
+#define PNERF_STATE_BLOCK 64
+typedef struct {
+  int32_t dtype, batch, kv_rows, kv_heads, head_dim;
+  int64_t k_stride[3], v_stride[3], k8_stride[3], v8_stride[3]; /* (batch, row, head) */
+  int64_t k_scale_stride[2], v_scale_stride[2];                 /* (batch, block) */
+  const int32_t* kv_len;   /* (device) [batch], clamped to 0..kv_rows, or NULL: all kv_rows */
+  const uint8_t* kv_mask;  /* (device) [batch][kv_rows], nonzero = allowed, or NULL */
+  int64_t kv_mask_stride;  /* between batch entries */
+} pnerf_states_params;
+
+pnerf_status pnerf_quantize_states(const pnerf_states_params* params, const void* k, const void* v,
+                                   void* k8, void* v8, float* k_scale, float* v_scale, void* stream);
+
+/* Cross attention to 8-bit states: pnerf_cross_attention with
+ *   k_j = k_scale[j / PNERF_STATE_BLOCK] k8_j,  v_j = v_scale[j / PNERF_STATE_BLOCK] v8_j
+ * as pnerf_quantize_states leaves them (attention.k_stride and v_stride are those of k8
+ * and v8; attention.dtype is that of q and o).  The scales are positive finite
+ * numbers, not only powers of two; those of one head's values within 2^96 of each
+ * other.  Keys, values and masks in places that are not allowed, and the scales of
+ * blocks without an allowed key, have no influence.  No gradient: states are kept in 8
+ * bits for proposals, not for training. */
+typedef struct {
+  pnerf_attention_params attention;
+  int64_t k_scale_stride[2], v_scale_stride[2]; /* (batch, block) */
+} pnerf_attention_q8_params;
+
+pnerf_status pnerf_cross_attention_q8_workspace(const pnerf_attention_q8_params* params, int64_t* bytes);
+/* lse (device): float32 [batch][q_heads][q_rows], or NULL. */
+pnerf_status pnerf_cross_attention_q8(const pnerf_attention_q8_params* params, const void* q,
+                                      const void* k8, const void* v8, const float* k_scale,
+                                      const float* v_scale, void* o, float* lse, void* workspace,
+                                      int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

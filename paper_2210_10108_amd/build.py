@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpnerf.so")
 SOURCES = ["api.hip", "march.hip", "encode.hip", "mlp.hip", "composite.hip", "pose.hip",
-           "layers_api.hip", "attention.hip", "attention_bwd.hip", "norm_rotate.hip", "linear.hip"]
+           "layers_api.hip", "attention.hip", "attention_bwd.hip", "norm_rotate.hip", "linear.hip",
+           "rotate_axes.hip", "attention_q8.hip", "quantize.hip", "layer_norm.hip", "clip.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

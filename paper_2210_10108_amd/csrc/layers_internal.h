@@ -34,6 +34,9 @@ struct AttnArgs {
   int64_t dos[3], dqs[3], dks[3], dvs[3];
   float* delta;     // (lse, delta) of every row [B][Hq][Sq]
   float *do_norm, *v_norm;  // float16: |do| of every row, |v| of every key [B][Hkv][Sk]
+  // 8-bit states: k, v and their strides are of bytes; scales [B][blocks][Hkv], strides of batch and block
+  const float *k_scale, *v_scale;
+  int64_t kss[2], vss[2];
 };
 
 // Parts of the key axis and bytes of workspace of the forward pass.
@@ -42,6 +45,59 @@ int64_t attn_fwd_bytes(const AttnArgs& a);
 hipError_t launch_attn_fwd(const AttnArgs& a, void* ws, hipStream_t s);
 int64_t attn_bwd_bytes(const AttnArgs& a);
 hipError_t launch_attn_bwd(const AttnArgs& a, void* ws, hipStream_t s);
+hipError_t launch_attn_q8(const AttnArgs& a, void* ws, hipStream_t s);
+
+struct QuantSide {
+  const void* x;
+  uint8_t* y;
+  float* scale;
+  int64_t xs[3], ys[3], ss[2];
+};
+struct QuantArgs {
+  int dtype, B, S, H, D;
+  int vec;  // every row of every tensor starts on 16 (outputs 8) bytes and D % 8 == 0
+  QuantSide side[2];  // keys, values
+  const int32_t* len;
+  const uint8_t* mask;
+  int64_t mask_stride;
+};
+hipError_t launch_quantize(const QuantArgs& a, hipStream_t s);
+
+struct LayerNormArgs {
+  int dtype, rows, W;
+  int vec;  // every row of every tensor starts on 16 bytes and W % 8 == 0
+  float eps;
+  const void *x, *w, *b, *dy, *dres;
+  void *y, *dx, *dw, *db;
+  int64_t xs, ys, dys, drs, dxs;
+};
+hipError_t launch_layer_norm_fwd(const LayerNormArgs& a, hipStream_t s);
+int64_t layer_norm_bwd_bytes(const LayerNormArgs& a);
+hipError_t launch_layer_norm_bwd(const LayerNormArgs& a, void* ws, hipStream_t s);
+
+// One gradient of a clipping call.
+struct ClipEntry {
+  const void* g;
+  void* out;
+  int64_t n;
+  uint32_t first;  // its first chunk among all
+  uint16_t dtype, out_dtype;
+};
+constexpr int kClipChunk = 8192;  // elements that a workgroup takes at a time
+constexpr int kClipInline = 96;   // entries that a launch carries in its arguments
+struct ClipArgs {
+  double max_norm, eps;
+  int count;        // entries; the first kClipInline of a group in e, or all in `table`
+  uint32_t chunks;
+  int parts;        // workgroups of the sum, each with its partial
+  double* part;
+  float* norm;
+  ClipEntry* table;
+  ClipEntry e[kClipInline];
+};
+int64_t clip_bytes(int64_t count);
+hipError_t launch_clip(const ClipEntry* e, int count, double max_norm, double eps, float* norm, void* ws,
+                       hipStream_t s);
 
 struct NormSide {
   int rows, heads;
@@ -56,10 +112,18 @@ struct NormArgs {
   float eps;
   const float* table;
   NormSide side[2];  // queries, keys
+  // rotation at positions of several axes (pos is then [rows][axes])
+  int axes;
+  int whole;         // the pairs of every 8 elements (of every 16 where they are interleaved) share an axis
+  int norm;          // 0: the heads are turned as they are
+  float sign;        // -1: turned back
+  uint32_t pair_axis[8];  // 2 bits a pair
 };
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s);
 int64_t norm_bwd_bytes(const NormArgs& a);
 hipError_t launch_norm_bwd(const NormArgs& a, void* ws, hipStream_t s);
+hipError_t launch_axes_fwd(const NormArgs& a, hipStream_t s);
+hipError_t launch_axes_bwd(const NormArgs& a, void* ws, hipStream_t s);  // workspace as for launch_norm_bwd
 
 struct LinearArgs {
   int dtype, act;

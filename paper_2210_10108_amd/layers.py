@@ -13,6 +13,7 @@ whatever requires_grad says: every operator has its *_backward function.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import math
 
@@ -55,7 +56,39 @@ class LinearParams(C.Structure):
                 ("dx_stride", C.c_int64), ("dw_stride", C.c_int64)]
 
 
-_P, _I64, _I32 = C.c_void_p, C.c_int64, C.c_int32
+class LayerNormParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("width", C.c_int32), ("eps", C.c_float),
+                ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("dy_stride", C.c_int64),
+                ("dres_stride", C.c_int64), ("dx_stride", C.c_int64)]
+
+
+class RotateAxesParams(C.Structure):
+    _fields_ = [("base", NormRotateParams), ("norm", C.c_int32), ("axes", C.c_int32),
+                ("pair_axis", C.c_uint8 * 128)]
+
+
+class Gradient(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32),
+                ("out_dtype", C.c_int32)]
+
+
+class StatesParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("kv_rows", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("k8_stride", C.c_int64 * 3), ("v8_stride", C.c_int64 * 3),
+                ("k_scale_stride", C.c_int64 * 2), ("v_scale_stride", C.c_int64 * 2),
+                ("kv_len", C.c_void_p), ("kv_mask", C.c_void_p), ("kv_mask_stride", C.c_int64)]
+
+
+class AttentionQ8Params(C.Structure):
+    _fields_ = [("attention", AttentionParams),
+                ("k_scale_stride", C.c_int64 * 2), ("v_scale_stride", C.c_int64 * 2)]
+
+
+STATE_BLOCK = 64  # rows of the states that share a scale
+
+_P, _I64, _I32, _F64 = C.c_void_p, C.c_int64, C.c_int32, C.c_double
 # name -> argtypes; every function declared in include/pnerf_layers.h (each returns a status)
 _SIGS = {
     "pnerf_cross_attention_workspace": [_P, _I32, _P],
@@ -67,6 +100,17 @@ _SIGS = {
     "pnerf_linear_workspace": [_P, _I32, _P],
     "pnerf_linear": [_P] * 8 + [_I64, _P],
     "pnerf_linear_backward": [_P] * 9 + [_I64, _P],
+    "pnerf_layer_norm": [_P] * 6,
+    "pnerf_layer_norm_workspace": [_P, _P],
+    "pnerf_layer_norm_backward": [_P] * 9 + [_I64, _P],
+    "pnerf_rotate_axes": [_P] * 6,
+    "pnerf_rotate_axes_workspace": [_P, _P],
+    "pnerf_rotate_axes_backward": [_P] * 10 + [_I64, _P],
+    "pnerf_clip_gradients_workspace": [_I32, _P],
+    "pnerf_clip_gradients": [_P, _I32, _F64, _F64, _P, _P, _I64, _P],
+    "pnerf_quantize_states": [_P] * 8,
+    "pnerf_cross_attention_q8_workspace": [_P, _P],
+    "pnerf_cross_attention_q8": [_P] * 9 + [_I64, _P],
 }
 
 _lib = None
@@ -184,13 +228,21 @@ def _dtypes():
 
 
 # ---------------------------------------------------------------- attention
-def _attention(call, q, k, v, q_len, kv_len, kv_mask, scale):
+def _kv_mask(call, p, kv_mask, shape):
+    import torch
+    if kv_mask.dtype not in (torch.bool, torch.uint8):
+        raise TypeError(f"kv_mask must be torch.bool or torch.uint8, got {kv_mask.dtype}")
+    p.kv_mask = call.tensor(kv_mask, "kv_mask", shape, kv_mask.dtype)
+    p.kv_mask_stride = kv_mask.stride(0)
+
+
+def _attention(call, q, k, v, q_len, kv_len, kv_mask, scale, p=None, states=None):
     import torch
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must have 4 dimensions: batch, rows, heads, head width")
     B, Sq, Hq, D = q.shape
     Sk, Hkv = k.shape[1:3]
-    p = AttentionParams()
+    p = p or AttentionParams()
     p.dtype, p.batch, p.q_rows, p.kv_rows = call.code, B, Sq, Sk
     p.q_heads, p.kv_heads, p.head_dim = Hq, Hkv, D
     p.scale = (1.0 / math.sqrt(D) if D else 1.0) if scale is None else scale
@@ -200,12 +252,9 @@ def _attention(call, q, k, v, q_len, kv_len, kv_mask, scale):
     p.q_len = call.tensor(q_len, "q_len", (B,), torch.int32, True)
     p.kv_len = call.tensor(kv_len, "kv_len", (B,), torch.int32, True)
     if kv_mask is not None:
-        if kv_mask.dtype not in (torch.bool, torch.uint8):
-            raise TypeError(f"kv_mask must be torch.bool or torch.uint8, got {kv_mask.dtype}")
-        p.kv_mask = call.tensor(kv_mask, "kv_mask", (B, Sk), kv_mask.dtype)
-        p.kv_mask_stride = kv_mask.stride(0)
+        _kv_mask(call, p, kv_mask, (B, Sk))
     kv = (B, Sk, Hkv, D)
-    return p, call.tensor(q, "q", q.shape), call.tensor(k, "k", kv), call.tensor(v, "v", kv)
+    return p, call.tensor(q, "q", q.shape), call.tensor(k, "k", kv, states), call.tensor(v, "v", kv, states)
 
 
 def cross_attention(q, k, v, q_len=None, kv_len=None, kv_mask=None, scale=None, o=None,
@@ -253,9 +302,9 @@ def cross_attention_backward(do, q, k, v, o, lse, q_len=None, kv_len=None, kv_ma
 
 
 # ---------------------------------------------------------------- norm and rotation
-def _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved):
+def _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved, p=None, axes=()):
     import torch
-    p = NormRotateParams()
+    p = p or NormRotateParams()
     p.dtype, p.eps, p.interleaved = call.code, eps, int(interleaved)
     p.head_dim = D = q.shape[-1]
     if table is not None:
@@ -269,7 +318,7 @@ def _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
     p.q_rows, p.q_heads, _ = q.shape
     p.q_stride[:] = q.stride()[:2]
     p.q_weight = call.tensor(q_weight, "q_weight", (D,), None, True)
-    p.q_pos = call.tensor(q_pos, "q_pos", q.shape[:1], torch.int32, True)
+    p.q_pos = call.tensor(q_pos, "q_pos", (*q.shape[:1], *axes), torch.int32, True)
     if k is None:
         return p, qp, None
     if k.dim() != 3 or k.shape[2] != D:
@@ -278,7 +327,7 @@ def _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps, interleaved)
     p.k_rows, p.k_heads, _ = k.shape
     p.k_stride[:] = k.stride()[:2]
     p.k_weight = call.tensor(k_weight, "k_weight", (D,), None, True)
-    p.k_pos = call.tensor(k_pos, "k_pos", k.shape[:1], torch.int32, True)
+    p.k_pos = call.tensor(k_pos, "k_pos", (*k.shape[:1], *axes), torch.int32, True)
     return p, qp, kp
 
 
@@ -396,3 +445,227 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = Tru
     ws, nb, _keep = call.workspace(x, n.value)
     call.run(_lib.pnerf_linear_backward, ref, xp, wp, zp, gp, dxp, dwp, dbp, ws, nb)
     return dx, dw, db
+
+
+# ---------------------------------------------------------------- layer norm
+def _layer_norm(call, x, weight, bias, eps):
+    if x.dim() != 2:
+        raise ValueError("x must have 2 dimensions: rows, width")
+    p = LayerNormParams()
+    p.dtype, p.eps = call.code, eps
+    p.rows, p.width = shape = x.shape
+    p.x_stride = x.stride(0)
+    wide = shape[1:]
+    return (p, call.tensor(x, "x", shape), call.tensor(weight, "weight", wide, None, True),
+            call.tensor(bias, "bias", wide, None, True))
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, y=None, stream=None):
+    """pnerf_layer_norm: (x - mean) / sqrt(var + eps) * weight + bias over the rows
+    of x [rows, W] (any W up to 2^20), weight and bias [W] or None.  y may be x.
+    Returns y."""
+    call = _Call(x, stream)
+    p, xp, wp, bp = _layer_norm(call, x, weight, bias, eps)
+    y, yp = call.out(y, x, "y", None)
+    p.y_stride = y.stride(0)
+    call.run(lib().pnerf_layer_norm, C.byref(p), xp, wp, bp, yp)
+    return y
+
+
+def layer_norm_backward(dy, x, weight=None, eps: float = 1e-5, bias: bool = True, residual_grad=None,
+                        dx=None, stream=None):
+    """pnerf_layer_norm_backward: (dx, dweight, dbias) for dy = dL/dy; dweight is
+    None where weight is, dbias without bias.  residual_grad [rows, W], the
+    gradient that reaches x past the norm, is added to dx in the same pass.  dx may
+    be dy or residual_grad."""
+    call = _Call(x, stream)
+    p, xp, wp, _ = _layer_norm(call, x, weight, None, eps)
+    gp, rp = call.tensor(dy, "dy", x.shape), call.tensor(residual_grad, "residual_grad", x.shape)
+    p.dy_stride = dy.stride(0)
+    if residual_grad is not None:
+        p.dres_stride = residual_grad.stride(0)
+    dx, dxp = call.out(dx, x, "dx", None)
+    p.dx_stride = dx.stride(0)
+    dw = dwp = db = dbp = None
+    if weight is not None:
+        dw, dwp = call.out(None, weight, "", None)
+    if bias:
+        db = call.new(x, (p.width,))
+        dbp = db.data_ptr()
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_layer_norm_workspace(ref, C.byref(n)))
+    ws, nb, _keep = call.workspace(x, n.value)
+    call.run(_lib.pnerf_layer_norm_backward, ref, xp, wp, gp, rp, dxp, dwp, dbp, ws, nb)
+    return dx, dw, db
+
+
+# ---------------------------------------------------------------- rotation with several axes
+def _axes(call, q, k, table, q_pos, k_pos, pair_axis, q_weight, k_weight, eps, interleaved):
+    p = RotateAxesParams()
+    pair_axis = bytes(pair_axis)
+    if table is None or table.dim() != 3 or len(pair_axis) != table.shape[2] or len(pair_axis) > 128:
+        raise ValueError("table must be (positions, 2, pairs) and pair_axis name the axis of each of its pairs, 128 at most")
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights without a norm: eps is None")
+    if q_pos.dim() != 2:
+        raise ValueError("positions must have 2 dimensions: rows, axes")
+    C.memmove(p.pair_axis, pair_axis, len(pair_axis))
+    p.norm, p.axes = eps is not None, q_pos.shape[1]
+    _, qp, kp = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps or 0.0, interleaved,
+                      p.base, q_pos.shape[1:])
+    return p, qp, kp
+
+
+def rotate_axes(q, k, table, q_pos, k_pos, pair_axis, q_weight=None, k_weight=None, eps=None,
+                interleaved: bool = False, q_out=None, k_out=None, stream=None):
+    """pnerf_rotate_axes.  q [Tq, Hq, D] and k [Tk, Hk, D] (or None); table float32
+    [positions, 2, pairs]; q_pos int32 [Tq, axes], k_pos int32 [Tk, axes] (axes at
+    most 4); pair_axis: the axis of each pair, bytes or numbers.  With eps the heads
+    are normed first (weights [D] or None), without they are only turned.  Returns
+    (q_out, k_out); an output may be its input."""
+    call = _Call(q, stream)
+    p, qp, kp = _axes(call, q, k, table, q_pos, k_pos, pair_axis, q_weight, k_weight, eps, interleaved)
+    q_out, qo = call.out(q_out, q, "q_out", p.base.q_out_stride)
+    ko = None
+    if k is None:
+        k_out = None
+    else:
+        k_out, ko = call.out(k_out, k, "k_out", p.base.k_out_stride)
+    call.run(lib().pnerf_rotate_axes, C.byref(p), qp, kp, qo, ko)
+    return q_out, k_out
+
+
+def rotate_axes_backward(dq_out, dk_out, q, k, table, q_pos, k_pos, pair_axis, q_weight=None,
+                         k_weight=None, eps=None, interleaved: bool = False, dq=None, dk=None, stream=None):
+    """pnerf_rotate_axes_backward: (dq, dk, dq_weight, dk_weight) for the gradients
+    of the outputs; None where there is no such operand or weight.  Without eps q
+    and k give their shapes alone.  dq may be dq_out, dk may be dk_out."""
+    call = _Call(q, stream)
+    p, qp, kp = _axes(call, q, k, table, q_pos, k_pos, pair_axis, q_weight, k_weight, eps, interleaved)
+    b = p.base
+    gq, gk, dkp, dqw, dkw, wqp, wkp = call.tensor(dq_out, "dq_out", q.shape), *(None,) * 6
+    b.dq_out_stride[:] = dq_out.stride()[:2]
+    dq, dqp = call.out(dq, q, "dq", b.dq_stride)
+    if q_weight is not None:
+        dqw, wqp = call.out(None, q_weight, "", None)
+    if k is None:
+        dk = None
+    else:
+        gk = call.tensor(dk_out, "dk_out", k.shape)
+        b.dk_out_stride[:] = dk_out.stride()[:2]
+        dk, dkp = call.out(dk, k, "dk", b.dk_stride)
+        if k_weight is not None:
+            dkw, wkp = call.out(None, k_weight, "", None)
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_rotate_axes_workspace(ref, C.byref(n)))
+    ws, nb, _keep = call.workspace(q, n.value)
+    call.run(_lib.pnerf_rotate_axes_backward, ref, qp, kp, gq, gk, dqp, dkp, wqp, wkp, ws, nb)
+    return dq, dk, dqw, dkw
+
+
+# ---------------------------------------------------------------- gradients
+def clip_gradients(grads, max_norm: float, out=None, eps: float = 1e-6, stream=None):
+    """pnerf_clip_gradients: scales all gradients by min(1, max_norm / (norm + eps)),
+    norm the square root of the sum of all their squares, and returns norm (float32,
+    0-dimensional, on the device).  grads: contiguous tensors of any shapes, float32,
+    float16 and bfloat16 side by side.  out: as many tensors of the same shapes, each
+    of its gradient's type or float32 (default: the gradients themselves).  max_norm
+    may be math.inf (the norm alone)."""
+    import torch
+    if not grads:
+        raise ValueError("no gradients")
+    call = _Call(grads[0], stream)
+    outs = grads if out is None else out
+    if len(outs) != len(grads):
+        raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
+    codes, rows, index, f32 = _dtypes(), [], call.index, torch.float32
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        # what is usual is asked for in one go: many small gradients cost the host's time
+        code, n = codes.get(g.dtype), g.numel()
+        if code is None or g.get_device() != index or not g.is_contiguous():
+            call.tensor(g, f"gradient {i}", g.shape, g.dtype if code is not None else f32, True)
+        at = o_at = g.data_ptr()
+        o_code = code
+        if o is not g:
+            same = o.dtype is g.dtype
+            if not same:
+                o_code = F32
+            if o.shape != g.shape or o.get_device() != index or not o.is_contiguous() or \
+                    not (same or o.dtype is f32):
+                call.tensor(o, f"output {i}", g.shape, g.dtype if same else f32, True)
+            o_at = o.data_ptr()
+        rows += (at, o_at, n, code | o_code << 32)
+        if call.stream is not None:
+            g.record_stream(call.stream)
+            o.record_stream(call.stream)
+    norm = call.new(grads[0], (), f32)
+    n = C.c_int64()
+    _check(lib().pnerf_clip_gradients_workspace(len(grads), C.byref(n)))
+    ws, nb, _keep = call.workspace(grads[0], n.value)
+    table = array.array("q", rows)
+    call.run(_lib.pnerf_clip_gradients, table.buffer_info()[0], len(grads), max_norm, eps, norm.data_ptr(), ws, nb)
+    return norm
+
+
+# ---------------------------------------------------------------- 8-bit states
+def quantize_states(k, v, kv_len=None, kv_mask=None, k8=None, v8=None, k_scale=None, v_scale=None,
+                    stream=None):
+    """pnerf_quantize_states.  k and v [B, Sk, Hkv, D] (float16 or bfloat16); kv_len
+    int32 [B], kv_mask bool or uint8 [B, Sk] as cross_attention takes them.  Returns
+    (k8, v8, k_scale, v_scale): float8_e4m3fn [B, Sk, Hkv, D] and float32 [B, blocks,
+    Hkv], a scale for each STATE_BLOCK rows; any of them may be passed in."""
+    import torch
+    call = _Call(k, stream)
+    if k.dim() != 4:
+        raise ValueError("k must have 4 dimensions: batch, rows, heads, head width")
+    p = StatesParams()
+    p.dtype = call.code
+    p.batch, p.kv_rows, p.kv_heads, p.head_dim = shape = k.shape
+    kp, vp = call.tensor(k, "k", shape), call.tensor(v, "v", shape)
+    p.k_stride[:], p.v_stride[:] = k.stride()[:3], v.stride()[:3]
+    scales = (shape[0], -(-shape[1] // STATE_BLOCK), shape[2])
+    p.kv_len = call.tensor(kv_len, "kv_len", shape[:1], torch.int32, True)
+    if kv_mask is not None:
+        _kv_mask(call, p, kv_mask, shape[:2])
+
+    def output(t, name, size, dtype, strides):
+        if t is None:
+            t = call.new(k, size, dtype)
+        at = call.tensor(t, name, size, dtype)
+        strides[:] = t.stride()[:-1]
+        return t, at
+    k8, k8p = output(k8, "k8", shape, torch.float8_e4m3fn, p.k8_stride)
+    v8, v8p = output(v8, "v8", shape, torch.float8_e4m3fn, p.v8_stride)
+    k_scale, ksp = output(k_scale, "k_scale", scales, torch.float32, p.k_scale_stride)
+    v_scale, vsp = output(v_scale, "v_scale", scales, torch.float32, p.v_scale_stride)
+    call.run(lib().pnerf_quantize_states, C.byref(p), kp, vp, k8p, v8p, ksp, vsp)
+    return k8, v8, k_scale, v_scale
+
+
+def cross_attention_q8(q, k8, v8, k_scale, v_scale, q_len=None, kv_len=None, kv_mask=None, scale=None,
+                       o=None, return_lse: bool = False, stream=None):
+    """pnerf_cross_attention_q8: cross_attention of q [B, Sq, Hq, D] (float16 or
+    bfloat16) to states as quantize_states gives them, k8 and v8 float8_e4m3fn
+    [B, Sk, Hkv, D], k_scale and v_scale float32 [B, blocks, Hkv].  Returns o, or
+    (o, lse)."""
+    import torch
+    call = _Call(q, stream)
+    p = AttentionQ8Params()
+    a, qp, kp, vp = _attention(call, q, k8, v8, q_len, kv_len, kv_mask, scale, p.attention, torch.float8_e4m3fn)
+    scales = (a.batch, -(-a.kv_rows // STATE_BLOCK), a.kv_heads)
+    ksp = call.tensor(k_scale, "k_scale", scales, torch.float32)
+    vsp = call.tensor(v_scale, "v_scale", scales, torch.float32)
+    p.k_scale_stride[:], p.v_scale_stride[:] = k_scale.stride()[:2], v_scale.stride()[:2]
+    o, op = call.out(o, q, "o", a.o_stride)
+    lse = lp = None
+    if return_lse:
+        lse = call.new(q, (a.batch, a.q_heads, a.q_rows), torch.float32)
+        lp = lse.data_ptr()
+    n = C.c_int64()
+    ref = C.byref(p)
+    _check(lib().pnerf_cross_attention_q8_workspace(ref, C.byref(n)))
+    ws, nb, _keep = call.workspace(q, n.value)
+    call.run(_lib.pnerf_cross_attention_q8, ref, qp, kp, vp, ksp, vsp, op, lp, ws, nb)
+    return (o, lse) if return_lse else o

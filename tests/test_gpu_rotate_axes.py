@@ -1,0 +1,220 @@
+"""The rotation at positions of several axes against its definition in 64 bits."""
+import math
+import sys
+
+import pytest
+import torch
+
+from . import layers_common as R
+from . import more_layers_common as M
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2210_10108_amd import layers
+    layers.lib()
+    return layers
+
+
+def say(*a):
+    sys.stderr.write("[gpu] " + " ".join(str(x) for x in a) + "\n")
+    sys.stderr.flush()
+
+
+def normal(gen, *shape, dt="f16", std=1.0):
+    return (torch.randn(*shape, generator=gen, device="cuda") * std).to(R.DT[dt])
+
+
+def gen_of(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def table_of(n_pos, pairs, seed=0):
+    a = torch.rand(n_pos, pairs, generator=gen_of(seed), device="cuda", dtype=torch.float64) * 6.3
+    return torch.stack([a.cos(), a.sin()], 1).float()
+
+
+def layout(kind, pairs, axes):
+    if kind == "turns":
+        return bytes(j % axes for j in range(pairs))
+    if kind == "runs":  # multiples of 8 pairs where there are enough
+        return bytes(min(j // max(8, pairs // axes // 8 * 8), axes - 1) for j in range(pairs))
+    if kind == "last":  # one axis alone, not the first
+        return bytes([axes - 1] * pairs)
+    return bytes((j * 7 + j // 3) % axes for j in range(pairs))
+
+
+def check(L, q, k, wq, wk, table, pq, pk, axis, eps, inter, dq, dk, what):
+    say("rotation", what, tuple(q.shape), q.dtype)
+    kw = dict(q_weight=wq, k_weight=wk, eps=eps, interleaved=inter)
+    out = L.rotate_axes(q, k, table, pq, pk, axis, **kw)
+    grads = L.rotate_axes_backward(dq, dk, q, k, table, pq, pk, axis, **kw)
+    for i, (x, w, pos, dy, n) in enumerate(((q, wq, pq, dq, "q"), (k, wk, pk, dk, "k"))):
+        if x is None:
+            assert out[i] is None and grads[i] is None and grads[2 + i] is None
+            continue
+        ref = M.axes_ref(x, w, table, pos, axis, eps, inter, dy)
+        R.check(out[i], *ref["y"], f"{what} {n}")
+        R.check(grads[i], *ref["dx"], f"{what} d{n}")
+        assert (grads[2 + i] is None) == (w is None)
+        if w is not None:
+            R.check(grads[2 + i], *ref["dw"], f"{what} d{n}_weight")
+    return out, grads
+
+
+CASES = [  # Tq, Tk, Hq, Hk, D, rotated, axes
+    (1, 0, 1, 1, 64, 64, 2), (64, 64, 16, 4, 128, 128, 3), (3, 5, 2, 1, 32, 16, 2), (37, 21, 6, 3, 80, 80, 2),
+    (11, 13, 3, 3, 80, 32, 1), (5, 9, 4, 2, 256, 256, 4), (129, 300, 8, 2, 128, 64, 3), (7, 3, 5, 2, 33, 10, 3),
+    (9, 2, 2, 1, 100, 100, 4), (2, 2, 1, 1, 250, 6, 2), (3, 4, 1, 2, 2, 2, 2), (1100, 700, 5, 3, 96, 96, 3)]
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("kind", ["runs", "turns", "last", "any"])
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_rotate_axes(L, case, kind, inter, dt):
+    Tq, Tk, Hq, Hk, D, Rd, axes = case
+    g = gen_of(11)
+    q, dq = normal(g, Tq, Hq, D, dt=dt), normal(g, Tq, Hq, D, dt=dt)
+    k, dk = (normal(g, Tk, Hk, D, dt=dt), normal(g, Tk, Hk, D, dt=dt)) if Tk else (None, None)
+    wq, wk = normal(g, D, dt=dt), normal(g, D, dt=dt) if Tk else None
+    table, axis = table_of(50, Rd // 2), layout(kind, Rd // 2, axes)
+    pq, pk = (torch.randint(0, 50, (n, axes), generator=g, device="cuda", dtype=torch.int32) if n else None
+              for n in (Tq, Tk))
+    check(L, q, k, None, None, table, pq, pk, axis, None, inter, dq, dk, f"{case} {kind}")
+    check(L, q, k, wq, wk, table, pq, pk, axis, 1e-5, inter, dq, dk, f"{case} {kind} normed")
+
+
+def test_one_axis_is_norm_rotate(L):
+    # the same numbers as the operator with one position a row
+    g = gen_of(12)
+    for dt in ("f32", "f16", "bf16"):
+        q, k, dq, dk = (normal(g, T, H, 128, dt=dt) for T, H in ((50, 8), (70, 2), (50, 8), (70, 2)))
+        w, table = normal(g, 128, dt=dt), table_of(99, 64)
+        pq, pk = (torch.randint(0, 99, (n, 1), generator=g, device="cuda", dtype=torch.int32) for n in (50, 70))
+        want = L.norm_rotate(q, k, w, w, table, pq[:, 0].contiguous(), pk[:, 0].contiguous())
+        want += L.norm_rotate_backward(dq, dk, q, k, w, w, table, pq[:, 0].contiguous(), pk[:, 0].contiguous())
+        args = (q, k, table, pq, pk, bytes(64))
+        got = L.rotate_axes(*args, q_weight=w, k_weight=w, eps=1e-6)
+        got += L.rotate_axes_backward(dq, dk, *args, q_weight=w, k_weight=w, eps=1e-6)
+        for a, b in zip(got, want):
+            assert float((a.double() - b.double()).norm()) <= R.U[dt] * float(b.double().norm())
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("kind", ["runs", "turns"])
+@pytest.mark.parametrize("eps", [None, 1e-6])
+def test_rotate_axes_strides_and_in_place(L, eps, kind, dt):
+    g = gen_of(13)
+    T, H, D = 19, 4, 64
+    packed = normal(g, T, 3, H, D, dt=dt)
+    q, k = packed[:, 0], packed[:, 1]
+    third = packed[:, 2].clone()
+    table, axis = table_of(30, 32), layout(kind, 32, 3)
+    pos = torch.randint(0, 30, (T, 3), generator=g, device="cuda", dtype=torch.int32)
+    dq, dk = normal(g, T, H, D, dt=dt), normal(g, T, H, D, dt=dt)
+    (wantq, wantk), (gq, gk, _, _) = check(L, q, k, None, None, table, pos, pos, axis, eps, False, dq, dk, "packed")
+    odd = torch.empty(T * H * (D + 1) + 1, dtype=q.dtype, device="cuda")[1:].view(T, H, D + 1)[..., :D]
+    odd.copy_(q)
+    check(L, odd, k, None, None, table, pos, pos, axis, eps, False, dq, dk, "odd rows")
+    got = L.rotate_axes_backward(dq, dk, q, k, table, pos, pos, axis, eps=eps, dq=dq, dk=dk)
+    assert got[0] is dq and torch.equal(dq, gq) and torch.equal(dk, gk)
+    L.rotate_axes(q, k, table, pos, pos, axis, eps=eps, q_out=q, k_out=k)
+    assert torch.equal(q, wantq) and torch.equal(k, wantk) and torch.equal(packed[:, 2], third)
+    ref = M.axes_ref(odd, None, table, pos, axis, eps, False)
+    L.rotate_axes(odd, None, table, pos, None, axis, eps=eps, q_out=odd)
+    R.check(odd, *ref["y"], "odd rows in place")
+    # positions of tokens for every head: one row broadcast
+    one = q[:1].expand(T, -1, -1)
+    check(L, one, None, None, None, table, pos, None, axis, eps, False, normal(g, T, H, D, dt=dt), None, "broadcast")
+
+
+@pytest.mark.parametrize("D", [64, 50])
+@pytest.mark.parametrize("kind", ["runs", "turns"])
+def test_rotate_axes_positions_outside_the_table(L, kind, D):
+    g = gen_of(14)
+    q = normal(g, 5, 2, D, dt="f32")
+    pairs = 16
+    table, axis = table_of(8, pairs), layout(kind, pairs, 2)
+    pos = torch.tensor([[0, 1], [8, 1], [2, -1], [-7, 99], [7, 7]], dtype=torch.int32, device="cuda")
+    y, _ = L.rotate_axes(q, None, table, pos, None, axis)
+    lost = torch.zeros(5, D, dtype=torch.bool, device="cuda")
+    for j, a in enumerate(axis):
+        out = (pos[:, a] < 0) | (pos[:, a] >= 8)
+        lost[:, j] |= out
+        lost[:, j + pairs] |= out
+    assert torch.equal(y.isnan(), lost[:, None].expand_as(y))
+    good = M.axes_ref(q, None, table, pos.clamp(0, 7), axis, None, False)["y"]
+    keep = ~lost[:, None].expand_as(y)
+    R.check(y[keep], good[0][keep], good[1][keep], "the others")
+
+
+def test_rotation_back_is_its_inverse(L):
+    g = gen_of(15)
+    q, table = normal(g, 40, 3, 64, dt="f32"), table_of(20, 32)
+    pos = torch.randint(0, 20, (40, 3), generator=g, device="cuda", dtype=torch.int32)
+    axis = layout("turns", 32, 3)
+    y, _ = L.rotate_axes(q, None, table, pos, None, axis)
+    back = L.rotate_axes_backward(y, None, q, None, table, pos, None, axis)[0]
+    # cosines and sines rounded to 32 bits, two products and a sum twice
+    assert float((back - q).abs().max()) <= 16 * R.E32 * float(q.abs().max())
+
+
+@pytest.mark.parametrize("eps", [None, 1e-6])
+def test_rotate_axes_gradient_against_differences(L, eps):
+    g = gen_of(16)
+    q, w, dq = normal(g, 5, 3, 16, dt="f32"), normal(g, 16, dt="f32"), normal(g, 5, 3, 16, dt="f32")
+    table, axis = table_of(9, 8), layout("turns", 8, 3)
+    pos = torch.randint(0, 9, (5, 3), generator=g, device="cuda", dtype=torch.int32)
+    wq = w if eps else None
+    for inter in (False, True):
+        gx, _, gw, _ = L.rotate_axes_backward(dq, None, q, None, table, pos, None, axis, q_weight=wq, eps=eps,
+                                              interleaved=inter)
+        ref = M.axes_ref(q, wq, table, pos, axis, eps, inter, dq)
+
+        def value(x, v):
+            n = x / torch.sqrt((x * x).mean(2, keepdim=True) + eps) * v if eps else x
+            y = n.clone()
+            for j, a in enumerate(axis):
+                i0, i1 = (2 * j, 2 * j + 1) if inter else (j, j + 8)
+                c, s = (table[pos[:, a].long(), i, j].double()[:, None] for i in (0, 1))
+                y[..., i0], y[..., i1] = n[..., i0] * c - n[..., i1] * s, n[..., i0] * s + n[..., i1] * c
+            return (dq.double() * y).sum()
+        for n, at, grad in (("dx", 0, gx), ("dw", 1, gw))[:2 if eps else 1]:
+            base = [q.double(), w.double()]
+            way = torch.randn(base[at].shape, generator=gen_of(30), device="cuda", dtype=torch.float64)
+            hi, lo = ([t + (s * 1e-5 * way if j == at else 0) for j, t in enumerate(base)] for s in (1, -1))
+            diff = (value(*hi) - value(*lo)) / 2e-5
+            bound = float((ref[n][1] * way.abs()).sum()) + 1e-6 * float((ref[n][0] * way).abs().sum())
+            assert abs(float((grad.double() * way).sum() - diff)) <= bound, (n, inter)
+
+
+def test_rotate_axes_refusals(L):
+    from paper_2210_10108_amd import pnerf
+    g = gen_of(17)
+    q, table = normal(g, 4, 2, 32), table_of(6, 16)
+    pos, axis = torch.zeros(4, 2, dtype=torch.int32, device="cuda"), bytes(j % 2 for j in range(16))
+    w = normal(g, 32)
+    for kind, fn in [(ValueError, lambda: L.rotate_axes(q, None, table, pos, None, axis[:15])),
+                     (ValueError, lambda: L.rotate_axes(q, None, None, pos, None, axis)),
+                     (ValueError, lambda: L.rotate_axes(q, None, table, pos[:, 0], None, axis)),
+                     (ValueError, lambda: L.rotate_axes(q, None, table, pos[:3], None, axis)),
+                     (ValueError, lambda: L.rotate_axes(q, None, table, pos, None, axis, q_weight=w)),
+                     (ValueError, lambda: L.rotate_axes(q, q, table, pos, pos[:, :1].contiguous(), axis)),
+                     (ValueError, lambda: L.rotate_axes(q[0], None, table, pos, None, axis)),
+                     (ValueError, lambda: L.rotate_axes(q, None, table, pos, None, [300] * 16)),
+                     (TypeError, lambda: L.rotate_axes(q, None, table, pos.long(), None, axis)),
+                     (TypeError, lambda: L.rotate_axes(q, q.float(), table, pos, pos, axis))]:
+        with pytest.raises(kind):
+            fn()
+    five = torch.zeros(4, 5, dtype=torch.int32, device="cuda")
+    for fn in (lambda: L.rotate_axes(q, None, table, pos, None, [2] * 16),
+               lambda: L.rotate_axes(q, None, table, five, None, axis),
+               lambda: L.rotate_axes(q, None, table, pos, None, axis, eps=-1.0),
+               lambda: L.rotate_axes(q, q, table, pos, None, axis)):
+        with pytest.raises(pnerf.PnerfError) as e:
+            fn()
+        assert e.value.status == pnerf.ERR_INVALID_ARG
+    assert math.isfinite(float(q.float().sum()))
