@@ -93,6 +93,169 @@ __device__ __forceinline__ void copy_tile8(uint4* lds, const void* p, const int6
   }
 }
 
+// The loads of tiles of 64 rows of bytes into registers by NW wavefronts, and their way
+// to LDS as 16-bit elements.  A lane takes 16-byte chunks, the same columns of rows
+// that differ by kRows from load to load; the rows of 16 neighbouring lanes are chosen
+// so that their two 16-byte writes each, the even and the odd chunk, cover all banks
+// (see swz_bits): rows 0 and 4, or 0, 4, 1 and 5 of eight.
+template <class T, int DP, int NW>
+struct ByteTile {
+  static constexpr int kChunks = DP / 16;                // of a row
+  static constexpr int kRows = 64 / kChunks * NW;        // of one load of all wavefronts
+  static constexpr int kLoads = kBN / kRows;             // of a wavefront
+  const char* base;
+  int64_t row_bytes;
+  int D, row, col;  // this lane's row of the first load, its column
+  uint4 raw[kLoads];
+  __device__ __forceinline__ ByteTile(const void* p, int64_t first, int64_t stride, int D_, int wave, int lane)
+      : base((const char*)p + first), row_bytes(stride), D(D_) {
+    const int i = lane / kChunks;
+    row = wave * (64 / kChunks) + ((i & 1) << 2 | (i & 6) >> 1 | (i & 8));
+    col = 16 * (lane % kChunks);
+  }
+  // Tile t of n_rows rows.  on: its rows that may be read; the others, and what lies
+  // past the head's width, are zeros (a row past the last is beyond the bound only
+  // where rows do not overlap).
+  __device__ __forceinline__ void load(int t, int n_rows, uint64_t on) {
+    const u32x4 d = descriptor(base + (int64_t)t * kBN * row_bytes, (int64_t)(n_rows - t * kBN - 1) * row_bytes + D);
+    const __amdgpu_buffer_rsrc_t desc = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>((uint64_t)d[1] << 32 | d[0]), 0, d[2], d[3]);
+    const uint32_t off = col < D ? (uint32_t)row * (uint32_t)row_bytes + col : kOutside;
+    const uint32_t step = kRows * (uint32_t)row_bytes;
+    const uint64_t mine = on >> row;
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const uint32_t o = on == ~0ull || (mine >> (n * kRows) & 1) ? off + n * step : kOutside;
+      raw[n] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(desc, o, 0, 0));
+    }
+  }
+  __device__ __forceinline__ void widen(uint4* lds) const {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      lds[swz<DP / 8>(row + n * kRows, col / 8)] = widen8<T>(raw[n].x, raw[n].y);
+      lds[swz<DP / 8>(row + n * kRows, col / 8 + 1)] = widen8<T>(raw[n].z, raw[n].w);
+    }
+  }
+};
+
+// Many rows: four wavefronts of 32 rows share the tiles, two of them in LDS and the
+// next in registers on its way there.  One barrier a tile.  KS = 2: as in k_attn_fwd.
+template <class T, int DP, int KS>
+__global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs a, const Order order) {
+  using Tile = ByteTile<T, DP, 4>;
+  constexpr int kPieces = kBN * DP / 8;
+  __shared__ uint4 lds[KS][2][2 * kPieces];  // keys, then values
+  const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int wave = all_waves & 3, grp = all_waves >> 2;
+  const Place at(a, order, 128, wave * 32 + (lane & 31));
+  const Scales sc(a, at.b, at.g);
+  Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, wave, lane);
+  Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, wave, lane);
+  ScaledRows<T, DP> x;
+  x.template init<true>(at.q, at.ok, a.D, h);
+  x.begin(a);
+  uint64_t vm = 0, vm_next = 0;
+  float ks = 1.0f, vs = 1.0f, ks_next = 1.0f, vs_next = 1.0f;
+  int t = at.t0 + grp;
+  auto fetch = [&](int tile) {  // the tile after the one in LDS, if there is one
+    if (tile >= at.t1) return;
+    vm_next = __ballot(at.allowed(tile * kBN + lane));
+    kt.load(tile, at.nk, vm_next);
+    vt.load(tile, at.nk, vm_next);
+    ks_next = sc.k[tile * sc.k_step], vs_next = sc.v[tile * sc.v_step];
+  };
+  auto put = [&](int buf) {
+    kt.widen(lds[grp][buf]);
+    vt.widen(lds[grp][buf] + kPieces);
+    vm = vm_next, ks = ks_next, vs = vs_next;
+  };
+  fetch(t);
+  if (t < at.t1) put(0);
+  fetch(t + KS);
+  const int rounds = (at.t1 - at.t0 + KS - 1) / KS;  // the same for both groups: they share the barrier
+  int round = 0;
+  x.run(
+      lane,
+      [&] {
+        if (round == rounds) return false;
+        const int buf = round & 1;
+        wait_reads();
+        __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
+        const bool here = t < at.t1;  // the last round may have no tile for the second group
+        const uint64_t on = vm;
+        x.scales(a, ks, vs, on);
+        t += KS;
+        if (t < at.t1) {
+          put(buf ^ 1);
+          fetch(t + KS);
+        }
+        if (!here) return false;
+        x.scores(lds[grp][buf], on, x.c, lane);
+        ++round;
+        return true;
+      },
+      [&] { return lds[grp][(round - 1) & 1] + kPieces; });
+  if constexpr (KS == 2) {
+    static_assert(kGroupsLds<DP> <= sizeof(lds), "a group's sums fit LDS");
+    if (!join_groups<T, DP>(x, lds, wave, grp, lane)) return;
+  }
+  x.close(at.ok);
+  if (at.row >= a.M) return;
+  if (a.splits > 1)
+    x.store_partial(a, at.sp, ((int64_t)at.b * a.Hkv + at.g) * a.M + at.row, h, at.t0 < at.t1);
+  else
+    x.template store<true>(a, at.b, at.qi, at.head, h);
+}
+
+// At most 32 rows of a kv head (single tokens): the bytes of the states are the time.
+// Four wavefronts with the same rows take the tiles in turn, each with its own keys
+// and values in LDS and no barrier; a tile's bytes are requested as soon as the tile
+// before has gone from the registers to LDS.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_attn_q8_few(const AttnArgs a, const Order order) {
+  using Tile = ByteTile<T, DP, 1>;
+  constexpr int kPieces = kBN * DP / 8;
+  __shared__ uint4 lds[4][2 * kPieces];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const Place at(a, order, 32, lane & 31);
+  const Scales sc(a, at.b, at.g);
+  Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, 0, lane);
+  Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, 0, lane);
+  ScaledRows<T, DP> x;
+  x.template init<true>(at.q, at.ok, a.D, h);
+  x.begin(a);
+  uint4 *sk = lds[wave], *sv = sk + kPieces;
+  uint64_t vm_next = 0;
+  float ks_next = 1.0f, vs_next = 1.0f;
+  int t = at.t0 + wave;
+  auto fetch = [&] {
+    if (t >= at.t1) return;
+    vm_next = __ballot(at.allowed(t * kBN + lane));
+    kt.load(t, at.nk, vm_next);
+    vt.load(t, at.nk, vm_next);
+    ks_next = sc.k[t * sc.k_step], vs_next = sc.v[t * sc.v_step];
+  };
+  fetch();
+  x.run(
+      lane,
+      [&] {
+        if (t >= at.t1) return false;
+        wave_fence();  // the values before have been used
+        kt.widen(sk);
+        vt.widen(sv);
+        const uint64_t vm = vm_next;
+        x.scales(a, ks_next, vs_next, vm);
+        t += 4;
+        fetch();
+        wave_fence();
+        x.scores(sk, vm, x.c, lane);
+        return true;
+      },
+      [&] { return sv; });
+  static_assert(kFewLds<DP> <= sizeof(lds), "the sums fit the tiles' LDS");
+  finish_few<T, DP>(a, at, x, lds, wave, lane, h);
+}
+
 // Any strides, alignment and head width.
 template <class T, int DP>
 __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Order order) {
@@ -133,7 +296,14 @@ void launch(const AttnArgs& a, hipStream_t s) {
   const int rows = few ? 32 : 128;
   const Order o = order_of(((int64_t)a.M + rows - 1) / rows, a.Hkv);
   const unsigned n = (unsigned)workgroups(o, a.splits, a);
-  k_attn_q8_any<T, DP><<<n, 256, 0, s>>>(a, o);
+  if (!fast_loads(a))
+    k_attn_q8_any<T, DP><<<n, 256, 0, s>>>(a, o);
+  else if (few)
+    k_attn_q8_few<T, DP><<<n, 256, 0, s>>>(a, o);
+  else if (two_groups(n, a))
+    k_attn_q8_fwd<T, DP, 2><<<n, 512, 0, s>>>(a, o);
+  else
+    k_attn_q8_fwd<T, DP, 1><<<n, 256, 0, s>>>(a, o);
   join<T, DP>(a, s);
 }
 

@@ -150,6 +150,86 @@ struct Place {
   __device__ __forceinline__ bool allowed(int j) const { return j < nk && (!mask || mask[j]); }
 };
 
+// Two groups of four wavefronts with the same rows: adds the second group's sums to
+// the first's, by way of LDS that all have done with; false in the second.
+template <int DP>
+constexpr int kGroupsLds = 4 * 64 * (DP / 8 * 16 + 8);
+template <class T, int DP>
+__device__ __forceinline__ bool join_groups(Rows<T, DP>& x, void* lds, int wave, int grp, int lane) {
+  floatx4* red = reinterpret_cast<floatx4*>(lds) + wave * (DP / 8) * 64 + lane;
+  floatx2* red_ml = reinterpret_cast<floatx2*>(reinterpret_cast<floatx4*>(lds) + 4 * (DP / 8) * 64) + wave * 64 + lane;
+  wait_reads();
+  __syncthreads();
+  if (grp == 1) {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        red[(4 * d + i) * 64] = floatx4{x.o[d][4 * i], x.o[d][4 * i + 1], x.o[d][4 * i + 2], x.o[d][4 * i + 3]};
+    *red_ml = floatx2{x.m, x.l};
+  }
+  __syncthreads();
+  if (grp == 1) return false;
+  const floatx2 ml = *red_ml;
+  const float m = fmaxf(x.m, ml[0]), base = m == -INFINITY ? 0.0f : m;
+  const float f0 = __builtin_amdgcn_exp2f(x.m - base), f1 = __builtin_amdgcn_exp2f(ml[0] - base);
+  x.m = m;
+  x.l = x.l * f0 + ml[1] * f1;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 o = red[(4 * d + i) * 64];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x.o[d][4 * i + j] = x.o[d][4 * i + j] * f0 + o[j] * f1;
+    }
+  return true;
+}
+
+// Four wavefronts with the same rows: their sums meet in LDS, and the result (or the
+// part's) goes to memory.
+template <int DP>
+constexpr int kFewLds = 4 * 32 * (DP + 4) * 4 + 4 * 64 * 4;
+template <class T, int DP>
+__device__ __forceinline__ void finish_few(const AttnArgs& a, const Place& at, Rows<T, DP>& x, void* lds, int wave, int lane, int h) {
+  // the wavefronts' sums at the largest of their maxima
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(lds);
+  floatx2* red_ml = reinterpret_cast<floatx2*>(red + 4 * 32 * (DP + 4));
+  x.close(at.ok);
+  if (h == 0) red_ml[wave * 32 + lane] = floatx2{x.m, x.l};
+  store_part<DP>(x.o, red + (wave * 32 + (lane & 31)) * (DP + 4), h);
+  __syncthreads();
+  constexpr int kLanes = DP / 4;  // of a row, 4 elements each
+  for (int r = threadIdx.x / kLanes; r < min(a.M, 32); r += 256 / kLanes) {
+    const int d = 4 * (threadIdx.x % kLanes);
+    float m = -INFINITY, l = 0.0f;
+    floatx4 o = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, red_ml[w * 32 + r][0]);
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const floatx2 v = red_ml[w * 32 + r];
+      const float f = __builtin_amdgcn_exp2f(v[0] - base);
+      l += f * v[1];
+      o += f * *reinterpret_cast<const floatx4*>(red + (w * 32 + r) * (DP + 4) + d);
+    }
+    const int64_t rows = (int64_t)a.B * a.Hkv * a.M, row = ((int64_t)at.b * a.Hkv + at.g) * a.M + r;
+    if (a.splits > 1) {
+      if (d == 0)
+        reinterpret_cast<floatx2*>(a.part + (int64_t)a.splits * rows * DP)[at.sp * rows + row] = floatx2{m, l};
+      *reinterpret_cast<floatx4*>(a.part + (at.sp * rows + row) * DP + d) = o;
+    } else {
+      const int qi = r / a.G, head = at.g * a.G + r % a.G;
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      store4<true>((uint16_t*)a.o + at.b * a.os[0] + (int64_t)qi * a.os[1] + head * a.os[2] + d,
+                   make_uint2(T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)), a.D - d);
+      if (a.lse && d == 0) a.lse[((int64_t)at.b * a.Hq + head) * a.Sq + qi] = log_sum(m, l);
+    }
+  }
+}
+
 // Joins the parts of the key axis, in a fixed order: the parts' sums meet at the
 // largest of their maxima.  A row is NG groups of DP / 4 lanes, each with every
 // NG-th part: one group where rows are many and parts fewer than a workgroup's
