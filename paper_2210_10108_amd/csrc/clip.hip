@@ -12,26 +12,58 @@
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
 
-#include "layers_internal.h"
+#include "rows_common.h"
 
 namespace pnerf {
 namespace {
 
 constexpr int kBlock = 256, kParts = 8 * kCUs;
 
+// Elements of a chunk before its first 16-byte boundary (n or less).
+template <class E>
+__device__ __forceinline__ int head_of(const E* p, int n) {
+  return min((int)((16 - ((uintptr_t)p & 15)) & 15) / (int)sizeof(E), n);
+}
+
+// The sum of squares of a thread's share of a chunk: 8 elements at a time from the
+// first 16-byte boundary on, what is before and behind them one by one.
 template <class E>
 __device__ __forceinline__ double squares(const E* g, int n) {
   double t = 0.0;
-  for (int i = threadIdx.x; i < n; i += kBlock) {
-    const double v = (double)(float)g[i];
+  const int head = head_of(g, n), groups = (n - head) / 8, tail = head + 8 * groups;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < groups; i += kBlock) {
+    float v[8];
+    load<E>(g + head + 8 * i, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t = fma((double)v[j], (double)v[j], t);
+  }
+  for (int i = threadIdx.x; i < head + n - tail; i += kBlock) {
+    const double v = (double)(float)g[i < head ? i : tail + i - head];
     t = fma(v, v, t);
   }
   return t;
 }
 
+// Where gradient and output reach a 16-byte boundary together, 8 elements at a time,
+// else one by one.  (The share of a thread is read before it is written: they may be one.)
 template <class E, class O>
 __device__ __forceinline__ void scaled(const E* g, O* out, int n, float c) {
-  for (int i = threadIdx.x; i < n; i += kBlock) out[i] = (O)((float)g[i] * c);
+  const int first = head_of(g, n);
+  const bool together = first == n || ((uintptr_t)(out + first) & 15) == 0;
+  const int head = together ? first : n, groups = (n - head) / 8, tail = head + 8 * groups;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < groups; i += kBlock) {
+    float v[8];
+    load<E>(g + head + 8 * i, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= c;
+    Elem<O>::store(out + head + 8 * i, v);
+  }
+  for (int i = threadIdx.x; i < head + n - tail; i += kBlock) {
+    const int at = i < head ? i : tail + i - head;
+    out[at] = (O)((float)g[at] * c);
+  }
 }
 
 // Sum over the workgroup, in all threads, in an order that is always the same.
