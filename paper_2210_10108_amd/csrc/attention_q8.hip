@@ -35,6 +35,28 @@ __device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi) {
   return make_uint4(a.x, a.y, b.x, b.y);
 }
 
+// Transposed read of bytes: within each 16 lanes, lane 2 r + c gives the address of row
+// r, bytes 8c .. 8c + 7; lane i receives byte i of rows 0 .. 7.
+__device__ __forceinline__ uint2 read_tr8(const char* lds) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  const i32x2 t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)lds);
+  return __builtin_bit_cast(uint2, t);
+}
+
+// Tiles of bytes in LDS: where 16-byte chunk c of row r is.  The chunks' positions are
+// xored with bits of the row such that both reads cover all banks: 16 rows at one chunk
+// (keys: a lane's 16 bytes are its share of two products), and 8 rows, 0..3 and 8..11,
+// at two adjacent ones (values, transposed).
+template <int DP>
+__device__ __forceinline__ int bytes_bits(int r) {
+  const int b1 = (r >> 1) & 1, b2 = (r >> 2) & 1, b3 = (r >> 3) & 1;
+  return DP == 128 ? b2 | b1 << 1 | b3 << 2 : b2 | b3 << 1;
+}
+template <int DP>
+__device__ __forceinline__ int bytes_swz(int r, int c) {
+  return r * DP + 16 * (c ^ bytes_bits<DP>(r));
+}
+
 // Rows whose tiles have scales.  `factor` of the scores' unit, `unit` of the sums.
 template <class T, int DP>
 struct ScaledRows : Rows<T, DP> {
@@ -45,8 +67,45 @@ struct ScaledRows : Rows<T, DP> {
   __device__ __forceinline__ void scales(const AttnArgs& a, float ks, float vs, uint64_t vm) {
     if (vm) c = fmaxf(a.c * ks, 0x1p-126f), unit_next = vs;  // (0 times a masked key's -inf would be NaN)
   }
+  // Queries in the order in which byte tiles hold the head's width (see bytes_swz).
+  __device__ __forceinline__ void init_bytes(const uint16_t* q, bool ok, int D, int h) {
+    this->template init<true>(q, false, D, h);
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      const int d = 32 * (i / 2) + 16 * h + 8 * (i % 2);
+      this->qf[i] = load8<true>(q + d, ok ? min(D - d, 8) : 0);
+    }
+  }
+  // The same as scores and add, of tiles of bytes.
+  __device__ __forceinline__ void scores_bytes(const char* sk, uint64_t vm, int lane) {
+    const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      this->s[n] = floatx16{};
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) {
+        const uint4 k = *reinterpret_cast<const uint4*>(sk + bytes_swz<DP>(32 * n + r, 2 * i + h));
+        this->s[n] = T::mma(widen8<T>(k.x, k.y), this->qf[2 * i], this->s[n]);
+        this->s[n] = T::mma(widen8<T>(k.z, k.w), this->qf[2 * i + 1], this->s[n]);
+      }
+    }
+    this->masked(vm, c, h);
+  }
+  __device__ __forceinline__ void add_bytes(const char* sv, int lane) {
+    this->weights(c);
+    const int l16 = lane & 15, r = 4 * (lane >> 5) + l16 / 2 + (l16 & 8 ? 4 : 0);  // keys 4 h + 0..3 and + 8
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {  // 16 keys each
+      const uint4 pf = pack8<T>(this->s[n / 2], 8 * (n % 2));
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        const uint2 v = read_tr8(sv + bytes_swz<DP>(16 * n + r, 2 * d + ((lane >> 4) & 1)) + 8 * (l16 & 1));
+        this->o[d] = T::mma(widen8<T>(v.x, v.y), pf, this->o[d]);
+      }
+    }
+  }
   template <class N, class V>
-  __device__ __forceinline__ void run(int lane, N next, V values) {
+  __device__ __forceinline__ void run(N next, V add_tile) {
     bool more = next();
     while (more) {
       this->rescale();
@@ -57,7 +116,7 @@ struct ScaledRows : Rows<T, DP> {
         for (int i = 0; i < DP / 32; ++i) this->o[i] *= f;
       }
       do {
-        this->add(values(), c, lane);
+        add_tile();
         more = next();
       } while (more && !this->grown() && unit_next == unit);
     }
@@ -175,7 +234,6 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
   const int rounds = (at.t1 - at.t0 + KS - 1) / KS;  // the same for both groups: they share the barrier
   int round = 0;
   x.run(
-      lane,
       [&] {
         if (round == rounds) return false;
         const int buf = round & 1;
@@ -194,7 +252,7 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
         ++round;
         return true;
       },
-      [&] { return lds[grp][(round - 1) & 1] + kPieces; });
+      [&] { x.add(lds[grp][(round - 1) & 1] + kPieces, x.c, lane); });
   if constexpr (KS == 2) {
     static_assert(kGroupsLds<DP> <= sizeof(lds), "a group's sums fit LDS");
     if (!join_groups<T, DP>(x, lds, wave, grp, lane)) return;
@@ -207,53 +265,89 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
     x.template store<true>(a, at.b, at.qi, at.head, h);
 }
 
+// The loads of tiles of 64 rows of bytes straight into LDS, by one wavefront.
+template <int DP>
+struct ByteRows {
+  static constexpr int kChunks = DP / 16, kRows = 64 / kChunks, kLoads = kBN / kRows;
+  static_assert(kRows % 8 == 0 && (DP == 64 ? kRows == 16 : true), "see off: rows of the other loads");
+  const char* base;
+  int64_t row_bytes;
+  int D;
+  uint32_t off[DP == 128 ? 2 : 1];  // this lane's chunk of the first load (of even and odd ones: bytes_bits)
+  __device__ __forceinline__ ByteRows(const void* p, int64_t first, int64_t stride, int D_, int lane)
+      : base((const char*)p + first), row_bytes(stride), D(D_) {
+#pragma unroll
+    for (int i = 0; i < (DP == 128 ? 2 : 1); ++i) {
+      const int r = lane / kChunks, c = (lane % kChunks) ^ bytes_bits<DP>(r + i * kRows);
+      off[i] = 16 * c < D ? (uint32_t)r * (uint32_t)row_bytes + 16 * c : kOutside;
+    }
+  }
+  __device__ __forceinline__ void load(uint32_t lds, int t, int n_rows, uint64_t on, int lane) const {
+    const u32x4 desc = descriptor(base + (int64_t)t * kBN * row_bytes, (int64_t)(n_rows - t * kBN - 1) * row_bytes + D);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds), step = kRows * (uint32_t)row_bytes;
+    const uint64_t mine = on >> (lane / kChunks);
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const uint32_t o = off[DP == 128 ? n % 2 : 0] + n * step;
+      load_to_lds(to + n * 1024, on == ~0ull || (mine >> (n * kRows) & 1) ? o : kOutside, desc);
+    }
+  }
+};
+
 // At most 32 rows of a kv head (single tokens): the bytes of the states are the time.
-// Four wavefronts with the same rows take the tiles in turn, each with its own keys
-// and values in LDS and no barrier; a tile's bytes are requested as soon as the tile
-// before has gone from the registers to LDS.
+// Eight wavefronts with the same rows take the tiles in turn, each with its own keys
+// and values in LDS, as bytes, and no barrier; keys are loaded again as soon as the
+// scores are there, values as soon as they have been used.  The bytes are widened on
+// the way from LDS to the products: each is read once.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_q8_few(const AttnArgs a, const Order order) {
-  using Tile = ByteTile<T, DP, 1>;
-  constexpr int kPieces = kBN * DP / 8;
-  __shared__ uint4 lds[4][2 * kPieces];
+__global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Order order) {
+  constexpr int kWaves = 8, kTile = kBN * DP;
+  __shared__ uint4 lds[(kWaves * 2 * kTile > kFewLds<DP, kWaves> ? kWaves * 2 * kTile : kFewLds<DP, kWaves>) / 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const Place at(a, order, 32, lane & 31);
   const Scales sc(a, at.b, at.g);
-  Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, 0, lane);
-  Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, 0, lane);
+  const ByteRows<DP> kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, lane);
+  const ByteRows<DP> vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, lane);
   ScaledRows<T, DP> x;
-  x.template init<true>(at.q, at.ok, a.D, h);
+  x.init_bytes(at.q, at.ok, a.D, h);
   x.begin(a);
-  uint4 *sk = lds[wave], *sv = sk + kPieces;
-  uint64_t vm_next = 0;
-  float ks_next = 1.0f, vs_next = 1.0f;
-  int t = at.t0 + wave;
-  auto fetch = [&] {
-    if (t >= at.t1) return;
+  const char *sk = (const char*)lds + wave * 2 * kTile, *sv = sk + kTile;
+  const uint32_t to_k = lds_address(sk), to_v = lds_address(sv);
+  int t = at.t0 + wave;    // of the next scores
+  uint64_t vm_next = 0;    // its keys that may be read
+  float ks = 1.0f, vs = 1.0f;
+  bool allowed = false, first = true;
+  if (t < at.t1) {
     vm_next = __ballot(at.allowed(t * kBN + lane));
-    kt.load(t, at.nk, vm_next);
-    vt.load(t, at.nk, vm_next);
-    ks_next = sc.k[t * sc.k_step], vs_next = sc.v[t * sc.v_step];
-  };
-  fetch();
+    kt.load(to_k, t, at.nk, vm_next, lane);
+    vt.load(to_v, t, at.nk, vm_next, lane);
+    allowed = at.allowed((t + kWaves) * kBN + lane);
+    ks = sc.k[t * sc.k_step], vs = sc.v[t * sc.v_step];
+  }
   x.run(
-      lane,
       [&] {
+        if (!first) {
+          wait_reads();  // the values before have been used
+          if (t < at.t1) vt.load(to_v, t, at.nk, vm_next, lane);
+        }
         if (t >= at.t1) return false;
-        wave_fence();  // the values before have been used
-        kt.widen(sk);
-        vt.widen(sv);
+        first = false;
+        wait_loads();
         const uint64_t vm = vm_next;
-        x.scales(a, ks_next, vs_next, vm);
-        t += 4;
-        fetch();
-        wave_fence();
-        x.scores(sk, vm, x.c, lane);
+        vm_next = __ballot(allowed);
+        x.scales(a, ks, vs, vm);
+        x.scores_bytes(sk, vm, lane);
+        wait_reads();
+        t += kWaves;
+        if (t < at.t1) {
+          kt.load(to_k, t, at.nk, vm_next, lane);
+          allowed = at.allowed((t + kWaves) * kBN + lane);
+          ks = sc.k[t * sc.k_step], vs = sc.v[t * sc.v_step];
+        }
         return true;
       },
-      [&] { return sv; });
-  static_assert(kFewLds<DP> <= sizeof(lds), "the sums fit the tiles' LDS");
-  finish_few<T, DP>(a, at, x, lds, wave, lane, h);
+      [&] { x.add_bytes(sv, lane); });
+  finish_few<T, DP, kWaves>(a, at, x, lds, wave, lane, h);
 }
 
 // Any strides, alignment and head width.
@@ -268,7 +362,6 @@ __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Ord
   x.begin(a);
   int t = at.t0;
   x.run(
-      lane,
       [&] {
         if (t >= at.t1) return false;
         const uint64_t vm = __ballot(at.allowed(t * kBN + lane));
@@ -281,7 +374,7 @@ __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Ord
         ++t;
         return true;
       },
-      [&] { return sv; });
+      [&] { x.add(sv, x.c, lane); });
   x.close(at.ok);
   if (at.row >= a.M) return;
   if (a.splits > 1)
@@ -299,7 +392,7 @@ void launch(const AttnArgs& a, hipStream_t s) {
   if (!fast_loads(a))
     k_attn_q8_any<T, DP><<<n, 256, 0, s>>>(a, o);
   else if (few)
-    k_attn_q8_few<T, DP><<<n, 256, 0, s>>>(a, o);
+    k_attn_q8_few<T, DP><<<n, 512, 0, s>>>(a, o);
   else if (two_groups(n, a))
     k_attn_q8_fwd<T, DP, 2><<<n, 512, 0, s>>>(a, o);
   else

@@ -37,6 +37,10 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < DP / 16; ++i) s[n] = T::mma(sk[swz<CH>(32 * n + r, 2 * i + h)], qf[i], s[n]);
     }
+    masked(vm, c, h);
+  }
+  // The scores that are there: those of keys that may not be read become -inf.
+  __device__ __forceinline__ void masked(uint64_t vm, float c, int h) {
     if (vm != ~0ull) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -65,9 +69,8 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) o[i] *= alpha;
   }
-  // Adds the tile whose scores are there.
-  __device__ __forceinline__ void add(const uint4* sv, float c, int lane) {
-    constexpr int CH = DP / 8;
+  // The scores' exponentials, and their sum.
+  __device__ __forceinline__ void weights(float c) {
     const float base = m == -INFINITY ? 0.0f : m;  // no allowed key yet
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -76,6 +79,11 @@ struct Rows {
         s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
         l += s[n][i];
       }
+  }
+  // Adds the tile whose scores are there.
+  __device__ __forceinline__ void add(const uint4* sv, float c, int lane) {
+    constexpr int CH = DP / 8;
+    weights(c);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {  // 16 keys each
       const uint4 pf = pack8<T>(s[n / 2], 8 * (n % 2));
@@ -186,30 +194,30 @@ __device__ __forceinline__ bool join_groups(Rows<T, DP>& x, void* lds, int wave,
   return true;
 }
 
-// Four wavefronts with the same rows: their sums meet in LDS, and the result (or the
+// NW wavefronts with the same rows: their sums meet in LDS, and the result (or the
 // part's) goes to memory.
-template <int DP>
-constexpr int kFewLds = 4 * 32 * (DP + 4) * 4 + 4 * 64 * 4;
-template <class T, int DP>
+template <int DP, int NW = 4>
+constexpr int kFewLds = NW * 32 * (DP + 4) * 4 + NW * 64 * 4;
+template <class T, int DP, int NW = 4>
 __device__ __forceinline__ void finish_few(const AttnArgs& a, const Place& at, Rows<T, DP>& x, void* lds, int wave, int lane, int h) {
   // the wavefronts' sums at the largest of their maxima
   __syncthreads();
   float* red = reinterpret_cast<float*>(lds);
-  floatx2* red_ml = reinterpret_cast<floatx2*>(red + 4 * 32 * (DP + 4));
+  floatx2* red_ml = reinterpret_cast<floatx2*>(red + NW * 32 * (DP + 4));
   x.close(at.ok);
   if (h == 0) red_ml[wave * 32 + lane] = floatx2{x.m, x.l};
   store_part<DP>(x.o, red + (wave * 32 + (lane & 31)) * (DP + 4), h);
   __syncthreads();
   constexpr int kLanes = DP / 4;  // of a row, 4 elements each
-  for (int r = threadIdx.x / kLanes; r < min(a.M, 32); r += 256 / kLanes) {
+  for (int r = threadIdx.x / kLanes; r < min(a.M, 32); r += 64 * NW / kLanes) {
     const int d = 4 * (threadIdx.x % kLanes);
     float m = -INFINITY, l = 0.0f;
     floatx4 o = {};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, red_ml[w * 32 + r][0]);
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, red_ml[w * 32 + r][0]);
     const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const floatx2 v = red_ml[w * 32 + r];
       const float f = __builtin_amdgcn_exp2f(v[0] - base);
       l += f * v[1];
