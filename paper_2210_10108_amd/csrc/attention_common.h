@@ -61,6 +61,7 @@ __device__ __forceinline__ int swz(int r, int c) {
 
 struct Item {
   int tile, sp, g, b;  // tile may be past the last one: nothing to do
+  Item() = default;
   __device__ __forceinline__ Item(const Order& o, int splits, int Hkv, int B) {
     if (o.tiles == 1) {
       int id = blockIdx.x;

@@ -16,6 +16,42 @@
 namespace pnerf {
 namespace {
 
+// The batch entry whose length is the rank-th longest of its 64 (in every lane; equal
+// ones in order).
+__device__ __forceinline__ int by_length(const AttnArgs& a, int rank) {
+  const int first = rank & ~63, n = min(a.B - first, 64), lane = threadIdx.x & 63;
+  const int mine = lane < n ? clamp_len(a.kv_len, first + lane, a.Sk) : -1;
+  int before = 0;
+  for (int i = 0; i < n; ++i) {
+    const int other = __builtin_amdgcn_readlane(mine, i);
+    before += other > mine || (other == mine && i < lane);
+  }
+  return first + __builtin_ctzll(__ballot(lane < n && before == (rank & 63)));
+}
+
+// The workgroup's item.  Where batch entries differ in length and the chip does not hold
+// all workgroups at once, the longest go first: one that starts late would leave the
+// others waiting for it.  Each XCD then goes through the entries with all of its heads.
+__device__ __forceinline__ Item item_of(const AttnArgs& a, const Order& o) {
+  Item item(o, a.splits, a.Hkv, a.B);
+  const int heads = a.Hkv * o.chunks / kXCDs;  // and chunks of an XCD
+  if (!a.sorted) return item;
+  if (o.tiles > 1 && a.Hkv * o.chunks % kXCDs == 0) {
+    int id = blockIdx.x / kXCDs;
+    const int t = id % o.per;
+    id /= o.per;
+    item.sp = id % a.splits;
+    id /= a.splits;
+    const int hc = blockIdx.x % kXCDs * heads + id % heads;
+    item.b = id / heads;
+    item.g = hc / o.chunks;
+    item.tile = hc % o.chunks * o.per + t;
+    if (item.tile >= o.tiles) item.tile = o.tiles;
+  }
+  item.b = by_length(a, item.b);
+  return item;
+}
+
 // 4 e4m3 numbers as two pairs of 16-bit ones.
 template <class T>
 __device__ __forceinline__ uint2 widen4(uint32_t w);
@@ -57,6 +93,28 @@ __device__ __forceinline__ int bytes_swz(int r, int c) {
   return r * DP + 16 * (c ^ bytes_bits<DP>(r));
 }
 
+// The scales of 64 tiles at a time, a lane each: a load for each tile would have to be
+// waited for, and with it the tiles that are on their way.
+struct Scales {
+  const float *k, *v;
+  int64_t k_step, v_step;
+  int last, first;  // the states' last tile; the first one held
+  float ks, vs;
+  __device__ __forceinline__ Scales(const AttnArgs& a, int b, int g)
+      : k(a.k_scale + b * a.kss[0] + g), v(a.v_scale + b * a.vss[0] + g), k_step(a.kss[1]), v_step(a.vss[1]),
+        last((a.Sk - 1) / kBN), first(-64), ks(1.0f), vs(1.0f) {}
+  // Tiles are asked for in rising order, the same one in all lanes.
+  __device__ __forceinline__ void of(int t, float& k_scale, float& v_scale) {
+    if (t >= first + 64) {
+      first = t;
+      const int mine = min(t + (int)(threadIdx.x & 63), last);
+      ks = k[mine * k_step], vs = v[mine * v_step];
+    }
+    k_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), t - first));
+    v_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), t - first));
+  }
+};
+
 // Rows whose tiles have scales.  `factor` of the scores' unit, `unit` of the sums.
 template <class T, int DP>
 struct ScaledRows : Rows<T, DP> {
@@ -64,7 +122,9 @@ struct ScaledRows : Rows<T, DP> {
 
   __device__ __forceinline__ void begin(const AttnArgs& a) { c = a.c, unit = unit_next = 1.0f; }
   // The scales of the next tile; one without an allowed key has none that count.
-  __device__ __forceinline__ void scales(const AttnArgs& a, float ks, float vs, uint64_t vm) {
+  __device__ __forceinline__ void scales(const AttnArgs& a, Scales& sc, int t, uint64_t vm) {
+    float ks, vs;
+    sc.of(t, ks, vs);
     if (vm) c = fmaxf(a.c * ks, 0x1p-126f), unit_next = vs;  // (0 times a masked key's -inf would be NaN)
   }
   // Queries in the order in which byte tiles hold the head's width (see bytes_swz).
@@ -123,14 +183,6 @@ struct ScaledRows : Rows<T, DP> {
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) this->o[i] *= unit;
   }
-};
-
-// A tile's scales (index of the tile below the number of blocks).
-struct Scales {
-  const float *k, *v;
-  int64_t k_step, v_step;
-  __device__ __forceinline__ Scales(const AttnArgs& a, int b, int g)
-      : k(a.k_scale + b * a.kss[0] + g), v(a.v_scale + b * a.vss[0] + g), k_step(a.kss[1]), v_step(a.vss[1]) {}
 };
 
 // A tile by way of registers, element by element, 256 threads.
@@ -206,27 +258,27 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
   __shared__ uint4 lds[KS][2][2 * kPieces];  // keys, then values
   const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int wave = all_waves & 3, grp = all_waves >> 2;
-  const Place at(a, order, 128, wave * 32 + (lane & 31));
-  const Scales sc(a, at.b, at.g);
+  const Place at(a, item_of(a, order), 128, wave * 32 + (lane & 31));
+  Scales sc(a, at.b, at.g);
   Tile kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, wave, lane);
   Tile vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, wave, lane);
   ScaledRows<T, DP> x;
   x.template init<true>(at.q, at.ok, a.D, h);
   x.begin(a);
   uint64_t vm = 0, vm_next = 0;
-  float ks = 1.0f, vs = 1.0f, ks_next = 1.0f, vs_next = 1.0f;
   int t = at.t0 + grp;
+  uint32_t mask = at.mask_at(t * kBN + lane);  // of key `lane` of the tile to be fetched next
   auto fetch = [&](int tile) {  // the tile after the one in LDS, if there is one
     if (tile >= at.t1) return;
-    vm_next = __ballot(at.allowed(tile * kBN + lane));
+    vm_next = at.allowed_of(mask, tile * kBN + lane);
+    mask = at.mask_at((tile + KS) * kBN + lane);
     kt.load(tile, at.nk, vm_next);
     vt.load(tile, at.nk, vm_next);
-    ks_next = sc.k[tile * sc.k_step], vs_next = sc.v[tile * sc.v_step];
   };
   auto put = [&](int buf) {
     kt.widen(lds[grp][buf]);
     vt.widen(lds[grp][buf] + kPieces);
-    vm = vm_next, ks = ks_next, vs = vs_next;
+    vm = vm_next;
   };
   fetch(t);
   if (t < at.t1) put(0);
@@ -241,7 +293,7 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
         __builtin_amdgcn_s_barrier();  // this tile is there, and the one before has been read
         const bool here = t < at.t1;  // the last round may have no tile for the second group
         const uint64_t on = vm;
-        x.scales(a, ks, vs, on);
+        if (here) x.scales(a, sc, t, on);
         t += KS;
         if (t < at.t1) {
           put(buf ^ 1);
@@ -304,8 +356,8 @@ __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Ord
   constexpr int kWaves = 8, kTile = kBN * DP;
   __shared__ uint4 lds[(kWaves * 2 * kTile > kFewLds<DP, kWaves> ? kWaves * 2 * kTile : kFewLds<DP, kWaves>) / 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const Place at(a, order, 32, lane & 31);
-  const Scales sc(a, at.b, at.g);
+  const Place at(a, item_of(a, order), 32, lane & 31);
+  Scales sc(a, at.b, at.g);
   const ByteRows<DP> kt(a.k, at.b * a.ks[0] + at.g * a.ks[2], a.ks[1], a.D, lane);
   const ByteRows<DP> vt(a.v, at.b * a.vs[0] + at.g * a.vs[2], a.vs[1], a.D, lane);
   ScaledRows<T, DP> x;
@@ -315,14 +367,13 @@ __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Ord
   const uint32_t to_k = lds_address(sk), to_v = lds_address(sv);
   int t = at.t0 + wave;    // of the next scores
   uint64_t vm_next = 0;    // its keys that may be read
-  float ks = 1.0f, vs = 1.0f;
-  bool allowed = false, first = true;
+  uint32_t mask = 1;
+  bool first = true;
   if (t < at.t1) {
     vm_next = __ballot(at.allowed(t * kBN + lane));
+    mask = at.mask_at((t + kWaves) * kBN + lane);
     kt.load(to_k, t, at.nk, vm_next, lane);
     vt.load(to_v, t, at.nk, vm_next, lane);
-    allowed = at.allowed((t + kWaves) * kBN + lane);
-    ks = sc.k[t * sc.k_step], vs = sc.v[t * sc.v_step];
   }
   x.run(
       [&] {
@@ -334,16 +385,15 @@ __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Ord
         first = false;
         wait_loads();
         const uint64_t vm = vm_next;
-        vm_next = __ballot(allowed);
-        x.scales(a, ks, vs, vm);
+        vm_next = at.allowed_of(mask, (t + kWaves) * kBN + lane);
+        x.scales(a, sc, t, vm);
         x.scores_bytes(sk, vm, lane);
         wait_reads();
         t += kWaves;
         if (t < at.t1) {
+          mask = at.mask_at((t + kWaves) * kBN + lane);
           kt.load(to_k, t, at.nk, vm_next, lane);
-          allowed = at.allowed((t + kWaves) * kBN + lane);
-          ks = sc.k[t * sc.k_step], vs = sc.v[t * sc.v_step];
-        }
+              }
         return true;
       },
       [&] { x.add_bytes(sv, lane); });
@@ -355,8 +405,8 @@ template <class T, int DP>
 __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Order order) {
   __shared__ uint4 sk[kBN * DP / 8], sv[kBN * DP / 8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const Place at(a, order, 128, wave * 32 + (lane & 31));
-  const Scales sc(a, at.b, at.g);
+  const Place at(a, item_of(a, order), 128, wave * 32 + (lane & 31));
+  Scales sc(a, at.b, at.g);
   ScaledRows<T, DP> x;
   x.template init<false>(at.q, at.ok, a.D, h);
   x.begin(a);
@@ -368,7 +418,7 @@ __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Ord
         __syncthreads();
         copy_tile8<T, DP>(sk, a.k, a.ks, at.b, at.g, a.D, t, vm);
         copy_tile8<T, DP>(sv, a.v, a.vs, at.b, at.g, a.D, t, vm);
-        x.scales(a, sc.k[t * sc.k_step], sc.v[t * sc.v_step], vm);
+        x.scales(a, sc, t, vm);
         __syncthreads();
         x.scores(sk, vm, x.c, lane);
         ++t;
@@ -384,11 +434,12 @@ __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Ord
 }
 
 template <class T, int DP>
-void launch(const AttnArgs& a, hipStream_t s) {
+void launch(AttnArgs a, hipStream_t s) {
   const bool few = a.M <= 32;
   const int rows = few ? 32 : 128;
   const Order o = order_of(((int64_t)a.M + rows - 1) / rows, a.Hkv);
   const unsigned n = (unsigned)workgroups(o, a.splits, a);
+  a.sorted = a.kv_len && a.B > 1 && n > kCUs;
   if (!fast_loads(a))
     k_attn_q8_any<T, DP><<<n, 256, 0, s>>>(a, o);
   else if (few)

@@ -139,8 +139,9 @@ struct Place {
   bool ok;
   const uint16_t* q;
   const uint8_t* mask;
-  __device__ __forceinline__ Place(const AttnArgs& a, const Order& order, int rows_wg, int row_in) {
-    const Item item(order, a.splits, a.Hkv, a.B);
+  __device__ __forceinline__ Place(const AttnArgs& a, const Order& order, int rows_wg, int row_in)
+      : Place(a, Item(order, a.splits, a.Hkv, a.B), rows_wg, row_in) {}
+  __device__ __forceinline__ Place(const AttnArgs& a, const Item& item, int rows_wg, int row_in) {
     const int mt = item.tile;  // past the last: every row is, too
     sp = item.sp, g = item.g, b = item.b;
     row = mt * rows_wg + row_in;
@@ -156,6 +157,10 @@ struct Place {
     mask = a.mask ? a.mask + b * a.mask_stride : nullptr;
   }
   __device__ __forceinline__ bool allowed(int j) const { return j < nk && (!mask || mask[j]); }
+  // The same in two steps: what the mask says, which may still be on its way (nothing
+  // looks at it here), and the answer.
+  __device__ __forceinline__ uint32_t mask_at(int j) const { return mask && j < nk ? mask[j] : 1u; }
+  __device__ __forceinline__ uint64_t allowed_of(uint32_t m, int j) const { return __ballot(j < nk && m != 0); }
 };
 
 // Two groups of four wavefronts with the same rows: adds the second group's sums to

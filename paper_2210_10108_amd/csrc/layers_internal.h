@@ -37,6 +37,7 @@ struct AttnArgs {
   // 8-bit states: k, v and their strides are of bytes; scales [B][blocks][Hkv], strides of batch and block
   const float *k_scale, *v_scale;
   int64_t kss[2], vss[2];
+  int sorted;  // longest batch entries first
 };
 
 // Parts of the key axis and bytes of workspace of the forward pass.
