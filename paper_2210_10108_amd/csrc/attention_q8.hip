@@ -45,8 +45,7 @@ __device__ __forceinline__ Item item_of(const AttnArgs& a, const Order& o) {
     const int hc = blockIdx.x % kXCDs * heads + id % heads;
     item.b = id / heads;
     item.g = hc / o.chunks;
-    item.tile = hc % o.chunks * o.per + t;
-    if (item.tile >= o.tiles) item.tile = o.tiles;
+    item.tile = min(t * o.chunks + hc % o.chunks, o.tiles);  // in turn: short entries fill no chunk first
   }
   item.b = by_length(a, item.b);
   return item;
@@ -136,12 +135,37 @@ struct ScaledRows : Rows<T, DP> {
       this->qf[i] = load8<true>(q + d, ok ? min(D - d, 8) : 0);
     }
   }
+  // What the scores of 32 keys start from: 0, and -inf at those that may not be read,
+  // whose rows in LDS are zeros.  (A register holds two keys, one a half wavefront.)
+  __device__ __forceinline__ static floatx16 start(uint32_t keys) {
+    floatx16 s = {};
+    if (keys != ~0u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = 8 * (i / 4) + i % 4;
+        const uint32_t lo = (int32_t)(keys << (31 - k)) >> 31, hi = (int32_t)(keys << (27 - k)) >> 31;
+        s[i] = __builtin_amdgcn_inverse_ballot_w64((uint64_t)hi << 32 | lo) ? 0.0f : -INFINITY;
+      }
+    return s;
+  }
+  __device__ __forceinline__ void scores(const uint4* sk, uint64_t vm, int lane) {
+    constexpr int CH = DP / 8;
+    const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      this->s[n] = start((uint32_t)(vm >> (32 * n)));
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i)
+        this->s[n] = T::mma(sk[swz<CH>(32 * n + r, 2 * i + h)], this->qf[i], this->s[n]);
+    }
+    this->raise(c);
+  }
   // The same as scores and add, of tiles of bytes.
   __device__ __forceinline__ void scores_bytes(const char* sk, uint64_t vm, int lane) {
     const int r = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      this->s[n] = floatx16{};
+      this->s[n] = start((uint32_t)(vm >> (32 * n)));
 #pragma unroll
       for (int i = 0; i < DP / 32; ++i) {
         const uint4 k = *reinterpret_cast<const uint4*>(sk + bytes_swz<DP>(32 * n + r, 2 * i + h));
@@ -149,7 +173,7 @@ struct ScaledRows : Rows<T, DP> {
         this->s[n] = T::mma(widen8<T>(k.z, k.w), this->qf[2 * i + 1], this->s[n]);
       }
     }
-    this->masked(vm, c, h);
+    this->raise(c);
   }
   __device__ __forceinline__ void add_bytes(const char* sv, int lane) {
     this->weights(c);
@@ -300,7 +324,7 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
           fetch(t + KS);
         }
         if (!here) return false;
-        x.scores(lds[grp][buf], on, x.c, lane);
+        x.scores(lds[grp][buf], on, lane);
         ++round;
         return true;
       },
@@ -420,7 +444,7 @@ __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Ord
         copy_tile8<T, DP>(sv, a.v, a.vs, at.b, at.g, a.D, t, vm);
         x.scales(a, sc, t, vm);
         __syncthreads();
-        x.scores(sk, vm, x.c, lane);
+        x.scores(sk, vm, lane);
         ++t;
         return true;
       },

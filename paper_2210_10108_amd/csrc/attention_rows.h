@@ -37,10 +37,6 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < DP / 16; ++i) s[n] = T::mma(sk[swz<CH>(32 * n + r, 2 * i + h)], qf[i], s[n]);
     }
-    masked(vm, c, h);
-  }
-  // The scores that are there: those of keys that may not be read become -inf.
-  __device__ __forceinline__ void masked(uint64_t vm, float c, int h) {
     if (vm != ~0ull) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -50,6 +46,10 @@ struct Rows {
           if (!((w >> (8 * (i / 4) + i % 4)) & 1)) s[n][i] = -INFINITY;
       }
     }
+    raise(c);
+  }
+  // `top` of the scores that are there.
+  __device__ __forceinline__ void raise(float c) {
     float mx = -INFINITY;
 #pragma unroll
     for (int n = 0; n < 2; ++n)
