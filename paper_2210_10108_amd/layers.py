@@ -580,32 +580,35 @@ def clip_gradients(grads, max_norm: float, out=None, eps: float = 1e-6, stream=N
     outs = grads if out is None else out
     if len(outs) != len(grads):
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
-    codes, rows, index, f32 = _dtypes(), [], call.index, torch.float32
-    for i, (g, o) in enumerate(zip(grads, outs)):
-        # what is usual is asked for in one go: many small gradients cost the host's time
-        code, n = codes.get(g.dtype), g.numel()
-        if code is None or g.get_device() != index or not g.is_contiguous():
-            call.tensor(g, f"gradient {i}", g.shape, g.dtype if code is not None else f32, True)
-        at = o_at = g.data_ptr()
-        o_code = code
-        if o is not g:
-            same = o.dtype is g.dtype
-            if not same:
-                o_code = F32
-            if o.shape != g.shape or o.get_device() != index or not o.is_contiguous() or \
-                    not (same or o.dtype is f32):
-                call.tensor(o, f"output {i}", g.shape, g.dtype if same else f32, True)
-            o_at = o.data_ptr()
-        rows += (at, o_at, n, code | o_code << 32)
-        if call.stream is not None:
-            g.record_stream(call.stream)
-            o.record_stream(call.stream)
+    # Many small gradients cost the host's time, so each property is asked for in a row
+    # over all of them, and told apart tensor by tensor only where one is not as usual.
+    T, f32, index = torch.Tensor, torch.float32, call.index
+    types = [g.dtype for g in grads]
+    good = set(types) <= _dtypes().keys() and all(map(T.is_contiguous, grads)) and \
+        set(map(T.get_device, grads)) == {index}
+    out_types = types
+    if outs is not grads:
+        out_types = [o.dtype for o in outs]
+        good = good and all(map(T.is_contiguous, outs)) and set(map(T.get_device, outs)) == {index} and \
+            all([a is b or a is f32 for a, b in zip(out_types, types)]) and \
+            [o.shape for o in outs] == [g.shape for g in grads]
+    if not good:
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            call.tensor(g, f"gradient {i}", g.shape, g.dtype if g.dtype in _dtypes() else f32, True)
+            call.tensor(o, f"output {i}", g.shape, g.dtype if o.dtype is g.dtype else f32, True)
+    if call.stream is not None:
+        for t in (*grads, *outs):
+            t.record_stream(call.stream)
+    at = list(map(T.data_ptr, grads))
+    codes = _dtypes()
+    pairs = [codes[a] | codes[b] << 32 for a, b in zip(types, out_types)]
+    out_at = at if outs is grads else list(map(T.data_ptr, outs))
+    rows = array.array("q", [x for row in zip(at, out_at, map(T.numel, grads), pairs) for x in row])
     norm = call.new(grads[0], (), f32)
     n = C.c_int64()
     _check(lib().pnerf_clip_gradients_workspace(len(grads), C.byref(n)))
     ws, nb, _keep = call.workspace(grads[0], n.value)
-    table = array.array("q", rows)
-    call.run(_lib.pnerf_clip_gradients, table.buffer_info()[0], len(grads), max_norm, eps, norm.data_ptr(), ws, nb)
+    call.run(_lib.pnerf_clip_gradients, rows.buffer_info()[0], len(grads), max_norm, eps, norm.data_ptr(), ws, nb)
     return norm
 
 
