@@ -570,9 +570,9 @@ def clip_gradients(grads, max_norm: float, out=None, eps: float = 1e-6, stream=N
     """pnerf_clip_gradients: scales all gradients by min(1, max_norm / (norm + eps)),
     norm the square root of the sum of all their squares, and returns norm (float32,
     0-dimensional, on the device).  grads: contiguous tensors of any shapes, float32,
-    float16 and bfloat16 side by side.  out: as many tensors of the same shapes, each
-    of its gradient's type or float32 (default: the gradients themselves).  max_norm
-    may be math.inf (the norm alone)."""
+    float16 and bfloat16 side by side.  out: as many contiguous tensors of as many
+    elements, each of its gradient's type or float32 (default: the gradients
+    themselves).  max_norm may be math.inf (the norm alone)."""
     import torch
     if not grads:
         raise ValueError("no gradients")
@@ -582,33 +582,33 @@ def clip_gradients(grads, max_norm: float, out=None, eps: float = 1e-6, stream=N
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
     # Many small gradients cost the host's time, so each property is asked for in a row
     # over all of them, and told apart tensor by tensor only where one is not as usual.
-    T, f32, index = torch.Tensor, torch.float32, call.index
-    types = [g.dtype for g in grads]
-    good = set(types) <= _dtypes().keys() and all(map(T.is_contiguous, grads)) and \
-        set(map(T.get_device, grads)) == {index}
-    out_types = types
+    T, f32, codes, count = torch.Tensor, torch.float32, _dtypes(), len(grads)
+    types = out_types = [g.dtype for g in grads]
+    sizes = array.array("q", map(T.numel, grads))
+    good = set(types) <= codes.keys() and all(map(T.is_contiguous, grads)) and \
+        set(map(T.get_device, grads)) == {call.index}
     if outs is not grads:
         out_types = [o.dtype for o in outs]
-        good = good and all(map(T.is_contiguous, outs)) and set(map(T.get_device, outs)) == {index} and \
-            all([a is b or a is f32 for a, b in zip(out_types, types)]) and \
-            [o.shape for o in outs] == [g.shape for g in grads]
+        good = good and all(map(T.is_contiguous, outs)) and set(map(T.get_device, outs)) == {call.index} and \
+            (out_types == types or all([a is b or a is f32 for a, b in zip(out_types, types)])) and \
+            array.array("q", map(T.numel, outs)) == sizes
     if not good:
         for i, (g, o) in enumerate(zip(grads, outs)):
-            call.tensor(g, f"gradient {i}", g.shape, g.dtype if g.dtype in _dtypes() else f32, True)
+            call.tensor(g, f"gradient {i}", g.shape, g.dtype if g.dtype in codes else f32, True)
             call.tensor(o, f"output {i}", g.shape, g.dtype if o.dtype is g.dtype else f32, True)
     if call.stream is not None:
         for t in (*grads, *outs):
             t.record_stream(call.stream)
-    at = list(map(T.data_ptr, grads))
-    codes = _dtypes()
-    pairs = [codes[a] | codes[b] << 32 for a, b in zip(types, out_types)]
-    out_at = at if outs is grads else list(map(T.data_ptr, outs))
-    rows = array.array("q", [x for row in zip(at, out_at, map(T.numel, grads), pairs) for x in row])
+    rows = array.array("q", bytes(32 * count))
+    rows[0::4] = at = array.array("q", map(T.data_ptr, grads))
+    rows[1::4] = at if outs is grads else array.array("q", map(T.data_ptr, outs))
+    rows[2::4] = sizes
+    rows[3::4] = array.array("q", [codes[a] | codes[b] << 32 for a, b in zip(types, out_types)])
     norm = call.new(grads[0], (), f32)
     n = C.c_int64()
-    _check(lib().pnerf_clip_gradients_workspace(len(grads), C.byref(n)))
+    _check(lib().pnerf_clip_gradients_workspace(count, C.byref(n)))
     ws, nb, _keep = call.workspace(grads[0], n.value)
-    call.run(_lib.pnerf_clip_gradients, rows.buffer_info()[0], len(grads), max_norm, eps, norm.data_ptr(), ws, nb)
+    call.run(_lib.pnerf_clip_gradients, rows.buffer_info()[0], count, max_norm, eps, norm.data_ptr(), ws, nb)
     return norm
 
 
@@ -636,7 +636,9 @@ def quantize_states(k, v, kv_len=None, kv_mask=None, k8=None, v8=None, k_scale=N
     def output(t, name, size, dtype, strides):
         if t is None:
             t = call.new(k, size, dtype)
-        at = call.tensor(t, name, size, dtype)
+            at = t.data_ptr()
+        else:
+            at = call.tensor(t, name, size, dtype)
         strides[:] = t.stride()[:-1]
         return t, at
     k8, k8p = output(k8, "k8", shape, torch.float8_e4m3fn, p.k8_stride)
