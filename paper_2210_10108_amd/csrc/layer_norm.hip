@@ -56,27 +56,79 @@ struct RowSums {
   }
 };
 
+// Eight elements from or to an address that is aligned to its elements alone (the
+// hardware takes it in one access as well), and n < 8 of them.
+template <class E>
+struct Odd {
+  struct __attribute__((packed, aligned(sizeof(E)))) Eight {
+    uint32_t w[2 * sizeof(E)];
+  };
+  static __device__ __forceinline__ typename Elem<E>::Raw raw(const E* p, int n) {
+    typename Elem<E>::Raw r;
+    if (n >= 8) {
+      const Eight x = *reinterpret_cast<const Eight*>(p);
+      __builtin_memcpy(&r, &x, sizeof(r));
+      return r;
+    }
+    alignas(16) E e[8] = {};
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < n) e[j] = p[j];
+    __builtin_memcpy(&r, e, sizeof(r));
+    return r;
+  }
+  static __device__ __forceinline__ void store(E* p, const float (&v)[8], int n) {
+    if (n >= 8) {
+      alignas(16) E e[8];
+      Elem<E>::store(e, v);
+      Eight x;
+      __builtin_memcpy(&x, e, sizeof(x));
+      *reinterpret_cast<Eight*>(p) = x;
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < n) p[j] = (E)v[j];
+  }
+};
+// The n (1 or more) elements of a row from p on, at most 8.  ODD: any width and
+// alignment; otherwise n >= 8 and p is on 16 bytes.
+template <class E, bool ODD>
+__device__ __forceinline__ typename Elem<E>::Raw raw8(const void* p, int64_t at, int n) {
+  if (ODD) return Odd<E>::raw((const E*)p + at, n);
+  return Elem<E>::raw((const E*)p + at);
+}
+template <class E, bool ODD>
+__device__ __forceinline__ void store8(void* p, int64_t at, const float (&v)[8], int n) {
+  if (ODD)
+    Odd<E>::store((E*)p + at, v, n);
+  else
+    Elem<E>::store((E*)p + at, v);
+}
+
 // NV groups of 8 elements of a row as they are loaded.
-template <class E, int TPR, int NV>
+template <class E, int TPR, int NV, bool ODD>
 struct Group {
   typename Elem<E>::Raw raw[NV];
   __device__ __forceinline__ void load(const void* p, int64_t at, int W) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int d = 8 * ((int)(threadIdx.x % TPR) + v * TPR);
-      if (d < W) raw[v] = Elem<E>::raw((const E*)p + at + d);
+      if (d < W) raw[v] = raw8<E, ODD>(p, at + d, W - d);
     }
   }
 };
 
-template <class E, int TPR, int NV>
+template <class E, int TPR, int NV, bool ODD>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm(const LayerNormArgs a) {
   constexpr int kRows = Shape<TPR>::kRows;
   __shared__ float lds[TPR > 64 ? TPR / 8 : 1];
   RowSums<TPR> sums(lds);
   const int group = threadIdx.x / TPR;
   const float inv = 1.0f / a.W;
-  Group<E, TPR, NV> x = {}, w = {}, b = {};
+  // elements of the row from j of group k on (0 or less: none is there; 8 at a time but for ODD)
+  auto left = [&](int k, int j) { return a.W - 8 * ((int)(threadIdx.x % TPR) + k * TPR) - (ODD ? j : 0); };
+  Group<E, TPR, NV, ODD> x = {}, w = {}, b = {};
   if (a.w) w.load(a.w, 0, a.W);
   if (a.b) b.load(a.b, 0, a.W);
   int64_t row = (int64_t)blockIdx.x * kRows + group;
@@ -88,17 +140,16 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm(const Layer
     for (int k = 0; k < NV; ++k) {
       Elem<E>::unpack(x.raw[k], v[k]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[0] += 8 * ((int)(threadIdx.x % TPR) + k * TPR) < a.W ? v[k][j] : 0.0f;
+      for (int j = 0; j < 8; ++j) t[0] += left(k, j) > 0 ? v[k][j] : 0.0f;
     }
     if (row + step < a.rows) x.load(a.x, (row + step) * a.xs, a.W);
     sums.sum(t);
     const float m = t[0] * inv;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const bool on = 8 * ((int)(threadIdx.x % TPR) + k * TPR) < a.W;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        v[k][j] = on ? v[k][j] - m : 0.0f;
+        v[k][j] = left(k, j) > 0 ? v[k][j] - m : 0.0f;
         u[0] += v[k][j], u[1] += v[k][j] * v[k][j];
       }
     }
@@ -117,20 +168,21 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm(const Layer
         const float n = (v[k][j] - c) * r;
         v[k][j] = (a.w ? n * wk[j] : n) + (a.b ? bk[j] : 0.0f);
       }
-      Elem<E>::store((E*)a.y + row * a.ys + d, v[k]);
+      store8<E, ODD>(a.y, row * a.ys + d, v[k], a.W - d);
     }
   }
 }
 
 // Each workgroup leaves its sums of dw and db, [workgroup][2][W].
-template <class E, int TPR, int NV>
+template <class E, int TPR, int NV, bool ODD>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const LayerNormArgs a, float* part) {
   constexpr int kRows = Shape<TPR>::kRows;
   __shared__ float lds[TPR > 64 ? TPR / 8 : 1];
   RowSums<TPR> sums(lds);
   const int group = threadIdx.x / TPR;
   const float inv = 1.0f / a.W;
-  Group<E, TPR, NV> x = {}, dy = {}, res = {}, w = {};
+  auto left = [&](int k, int j) { return a.W - 8 * ((int)(threadIdx.x % TPR) + k * TPR) - (ODD ? j : 0); };
+  Group<E, TPR, NV, ODD> x = {}, dy = {}, res = {}, w = {};
   if (a.w) w.load(a.w, 0, a.W);
   int64_t row = (int64_t)blockIdx.x * kRows + group;
   const int64_t step = (int64_t)gridDim.x * kRows;
@@ -146,11 +198,11 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const L
     const bool in = row < a.rows;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const bool on = in && 8 * ((int)(threadIdx.x % TPR) + k * TPR) < a.W;
       Elem<E>::unpack(x.raw[k], v[k]);
       Elem<E>::unpack(dy.raw[k], g[k]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
+        const bool on = in && left(k, j) > 0;
         t[0] += on ? v[k][j] : 0.0f;
         g[k][j] = on ? g[k][j] : 0.0f;
       }
@@ -161,12 +213,11 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const L
     const float m = t[0] * inv;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const bool on = in && 8 * ((int)(threadIdx.x % TPR) + k * TPR) < a.W;
       float wk[8];
       Elem<E>::unpack(w.raw[k], wk);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        v[k][j] = on ? v[k][j] - m : 0.0f;
+        v[k][j] = in && left(k, j) > 0 ? v[k][j] - m : 0.0f;
         const float gw = a.w ? g[k][j] * wk[j] : g[k][j];
         u[0] += v[k][j], u[1] += v[k][j] * v[k][j];
         u[2] += gw, u[3] += gw * v[k][j];
@@ -190,7 +241,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const L
         db[k][j] += g[k][j];
         v[k][j] = r * ((a.w ? g[k][j] * wk[j] : g[k][j]) - s1 - n * s2) + (a.dres ? rk[j] : 0.0f);
       }
-      Elem<E>::store((E*)a.dx + row * a.dxs + d, v[k]);
+      store8<E, ODD>(a.dx, row * a.dxs + d, v[k], a.W - d);
     }
   }
   if (!a.dw && !a.db) return;
@@ -200,8 +251,8 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const L
     for (int k = 0; k < NV; ++k) {
       const int d = 8 * ((int)threadIdx.x + k * TPR);
       if (d >= a.W) continue;
-      Elem<float>::store(part + d, dw[k]);
-      Elem<float>::store(part + a.W + d, db[k]);
+      store8<float, ODD>(part, d, dw[k], a.W - d);
+      store8<float, ODD>(part, a.W + d, db[k], a.W - d);
     }
   } else {  // the rows' sums meet in LDS, those of dw and then those of db
     __shared__ float all[kRows][TPR * NV * 8];
@@ -222,110 +273,132 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const L
   }
 }
 
-// N values of a row from element d on, as numbers: one load of 8, or one element.
-template <class E, int N>
-__device__ __forceinline__ void values(const void* p, int64_t at, float (&v)[N]) {
-  if constexpr (N == 8)
-    load<E>((const E*)p + at, v);
-  else
-    v[0] = (float)((const E*)p)[at];
-}
-template <class E, int N>
-__device__ __forceinline__ void put(void* p, int64_t at, const float (&v)[N]) {
-  if constexpr (N == 8)
-    Elem<E>::store((E*)p + at, v);
-  else
-    ((E*)p)[at] = (E)v[0];
-}
-
-// Any width: a workgroup a row, read again for each step.  N = 8: rows wider than the
-// registers hold, by 16-byte accesses; N = 1: any stride and alignment, element by element.
-template <class E, int N>
-__global__ __launch_bounds__(kBlock) void k_layer_norm_any(const LayerNormArgs a) {
+// Rows wider than the registers hold: a workgroup a row, which is read again for each
+// step (from a cache, mostly).
+template <class E>
+__global__ __launch_bounds__(kBlock) void k_layer_norm_wide(const LayerNormArgs a) {
   __shared__ float lds[kBlock / 8];
   RowSums<kBlock> sums(lds);
   const float inv = 1.0f / a.W;
+  auto values = [&](const void* p, int64_t at, int d, float (&v)[8]) {
+    Elem<E>::unpack(raw8<E, true>(p, at + d, a.W - d), v);
+  };
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const int64_t x = row * a.xs;
-    float t[1] = {0.0f}, u[2] = {0.0f, 0.0f}, v[N];
-    for (int d = N * threadIdx.x; d < a.W; d += N * kBlock) {
-      values<E, N>(a.x, x + d, v);
+    float t[1] = {0.0f}, u[2] = {0.0f, 0.0f}, v[8];
+    for (int d = 8 * threadIdx.x; d < a.W; d += 8 * kBlock) {
+      values(a.x, x, d, v);
 #pragma unroll
-      for (int j = 0; j < N; ++j) t[0] += v[j];
+      for (int j = 0; j < 8; ++j) t[0] += v[j];
     }
     sums.sum(t);
     const float m = t[0] * inv;
-    for (int d = N * threadIdx.x; d < a.W; d += N * kBlock) {
-      values<E, N>(a.x, x + d, v);
+    for (int d = 8 * threadIdx.x; d < a.W; d += 8 * kBlock) {
+      values(a.x, x, d, v);
 #pragma unroll
-      for (int j = 0; j < N; ++j) u[0] += v[j] - m, u[1] += (v[j] - m) * (v[j] - m);
+      for (int j = 0; j < 8; ++j) {
+        const float e = d + j < a.W ? v[j] - m : 0.0f;
+        u[0] += e, u[1] += e * e;
+      }
     }
     sums.sum(u);
     const float c = u[0] * inv, r = inv_rms(fmaxf(u[1] * inv - c * c, 0.0f), a.eps);
-    for (int d = N * threadIdx.x; d < a.W; d += N * kBlock) {
-      float w[N], b[N];
-      values<E, N>(a.x, x + d, v);
-      if (a.w) values<E, N>(a.w, d, w);
-      if (a.b) values<E, N>(a.b, d, b);
+    for (int d = 8 * threadIdx.x; d < a.W; d += 8 * kBlock) {
+      float w[8], b[8];
+      values(a.x, x, d, v);
+      if (a.w) values(a.w, 0, d, w);
+      if (a.b) values(a.b, 0, d, b);
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
+      for (int j = 0; j < 8; ++j) {
         const float n = (v[j] - m - c) * r;
         v[j] = (a.w ? n * w[j] : n) + (a.b ? b[j] : 0.0f);
       }
-      put<E, N>(a.y, row * a.ys + d, v);
+      store8<E, true>(a.y, row * a.ys + d, v, a.W - d);
     }
   }
 }
 
-// Each workgroup leaves its sums of dw and db, [workgroup][2][W].
-template <class E, int N>
-__global__ __launch_bounds__(kBlock) void k_layer_norm_bwd_any(const LayerNormArgs a, float* part) {
-  __shared__ float lds[kBlock / 8];
-  RowSums<kBlock> sums(lds);
+// The same for the gradient.  The sums of dw and db are in registers, NV groups of 8
+// columns a thread, where those hold them; NV = 0: in the workgroup's place in memory,
+// where every row adds to them.
+template <class E, int NV>
+__global__ __launch_bounds__(1024) void k_layer_norm_bwd_wide(const LayerNormArgs a, float* part) {
+  constexpr int T = 1024;
+  __shared__ float lds[T / 8];
+  RowSums<T> sums(lds);
   const float inv = 1.0f / a.W;
-  const bool wanted = a.dw || a.db;
   float* mine = part + (int64_t)blockIdx.x * 2 * a.W;
+  float dw[NV ? NV : 1][8] = {}, db[NV ? NV : 1][8] = {};
+  auto values = [&](const void* p, int64_t at, int d, float (&v)[8]) {
+    Elem<E>::unpack(raw8<E, true>(p, at + d, a.W - d), v);
+  };
+  auto groups = [&](auto f) {  // f(d, k) for this thread's groups
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (const int d = 8 * ((int)threadIdx.x + k * T); d < a.W) f(d, k);
+    } else {
+      for (int d = 8 * threadIdx.x; d < a.W; d += 8 * T) f(d, 0);
+    }
+  };
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const int64_t x = row * a.xs, dy = row * a.dys;
-    float t[1] = {0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[N], g[N], w[N];
-    for (int d = N * threadIdx.x; d < a.W; d += N * kBlock) {
-      values<E, N>(a.x, x + d, v);
+    float t[1] = {0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    groups([&](int d, int) {
+      float v[8];
+      values(a.x, x, d, v);
 #pragma unroll
-      for (int j = 0; j < N; ++j) t[0] += v[j];
-    }
+      for (int j = 0; j < 8; ++j) t[0] += v[j];
+    });
     sums.sum(t);
     const float m = t[0] * inv;
-    for (int d = N * threadIdx.x; d < a.W; d += N * kBlock) {
-      values<E, N>(a.x, x + d, v);
-      values<E, N>(a.dy, dy + d, g);
-      if (a.w) values<E, N>(a.w, d, w);
+    groups([&](int d, int) {
+      float v[8], g[8], w[8];
+      values(a.x, x, d, v);
+      values(a.dy, dy, d, g);
+      if (a.w) values(a.w, 0, d, w);
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float e = v[j] - m, gw = a.w ? g[j] * w[j] : g[j];
+      for (int j = 0; j < 8; ++j) {
+        const float e = d + j < a.W ? v[j] - m : 0.0f, gw = a.w ? g[j] * w[j] : g[j];
         u[0] += e, u[1] += e * e, u[2] += gw, u[3] += gw * e;
       }
-    }
+    });
     sums.sum(u);
     const float c = u[0] * inv, r = inv_rms(fmaxf(u[1] * inv - c * c, 0.0f), a.eps);
     const float s1 = u[2] * inv, s2 = r * (u[3] * inv - c * s1);
-    const bool first = row == (int)blockIdx.x;
-    for (int d = N * threadIdx.x; d < a.W; d += N * kBlock) {
-      float rd[N], dw[N] = {}, db[N] = {};
-      values<E, N>(a.x, x + d, v);
-      values<E, N>(a.dy, dy + d, g);
-      if (a.w) values<E, N>(a.w, d, w);
-      if (a.dres) values<E, N>(a.dres, row * a.drs + d, rd);
-      if (wanted && !first) values<float, N>(mine, d, dw), values<float, N>(mine, a.W + d, db);
+    groups([&](int d, int k) {
+      float v[8], g[8], w[8], rd[8];
+      values(a.x, x, d, v);
+      values(a.dy, dy, d, g);
+      if (a.w) values(a.w, 0, d, w);
+      if (a.dres) values(a.dres, row * a.drs, d, rd);
+      if (NV == 0) {
+        const bool first = row == (int)blockIdx.x;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
+        for (int j = 0; j < 8; ++j) dw[0][j] = db[0][j] = 0.0f;
+        if (!first) {
+          Elem<float>::unpack(raw8<float, true>(mine, d, a.W - d), dw[0]);
+          Elem<float>::unpack(raw8<float, true>(mine, a.W + d, a.W - d), db[0]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
         const float n = (v[j] - m - c) * r;
-        dw[j] += g[j] * n, db[j] += g[j];
+        dw[k][j] += g[j] * n, db[k][j] += g[j];
         v[j] = r * ((a.w ? g[j] * w[j] : g[j]) - s1 - n * s2) + (a.dres ? rd[j] : 0.0f);
       }
-      put<E, N>(a.dx, row * a.dxs + d, v);
-      if (wanted) put<float, N>(mine, d, dw), put<float, N>(mine, a.W + d, db);
-    }
+      store8<E, true>(a.dx, row * a.dxs + d, v, a.W - d);
+      if (NV == 0) {
+        store8<float, true>(mine, d, dw[0], a.W - d);
+        store8<float, true>(mine, a.W + d, db[0], a.W - d);
+      }
+    });
   }
+  if (NV > 0 && (a.dw || a.db))
+    groups([&](int d, int k) {
+      store8<float, true>(mine, d, dw[k], a.W - d);
+      store8<float, true>(mine, a.W + d, db[k], a.W - d);
+    });
 }
 
 // dw and db: the workgroups' sums added up in order, 16 columns a workgroup, 64 sums at a time.
@@ -357,67 +430,56 @@ template <class E, int TPR, int NV>
 void forward(const LayerNormArgs& a, hipStream_t s) {
   constexpr int kRows = Shape<TPR>::kRows;
   const int n = (int)std::min<int64_t>(((int64_t)a.rows + kRows - 1) / kRows, 16 * kCUs);
-  k_layer_norm<E, TPR, NV><<<n, Shape<TPR>::kThreads, 0, s>>>(a);
+  (a.vec ? k_layer_norm<E, TPR, NV, false> : k_layer_norm<E, TPR, NV, true>)<<<n, Shape<TPR>::kThreads, 0, s>>>(a);
 }
 template <class E>
 void forward(const LayerNormArgs& a, hipStream_t s) {
   const int W = a.W;
-  if (!a.vec || W > 16384)
-    (a.vec ? k_layer_norm_any<E, 8> : k_layer_norm_any<E, 1>)<<<std::min(a.rows, 16 * kCUs), kBlock, 0, s>>>(a);
-  else if (W <= 32)
-    forward<E, 4, 1>(a, s);
-  else if (W <= 64)
-    forward<E, 8, 1>(a, s);
-  else if (W <= 128)
-    forward<E, 16, 1>(a, s);
-  else if (W <= 256)
-    forward<E, 32, 1>(a, s);
-  else if (W <= 512)
-    forward<E, 64, 1>(a, s);
-  else if (W <= 1024)
-    forward<E, 64, 2>(a, s);
-  else if (W <= 2048)
-    forward<E, 256, 1>(a, s);
-  else if (W <= 4096)
-    forward<E, 256, 2>(a, s);
-  else if (W <= 8192)
-    forward<E, 256, 4>(a, s);
-  else
-    forward<E, 1024, 2>(a, s);
+  if (W <= 32) return forward<E, 4, 1>(a, s);
+  if (W <= 64) return forward<E, 8, 1>(a, s);
+  if (W <= 128) return forward<E, 16, 1>(a, s);
+  if (W <= 256) return forward<E, 32, 1>(a, s);
+  if (W <= 512) return forward<E, 64, 1>(a, s);
+  if (W <= 1024) return forward<E, 64, 2>(a, s);
+  if (W <= 2048) return forward<E, 256, 1>(a, s);
+  if (W <= 4096) return forward<E, 256, 2>(a, s);
+  if (W <= 8192) return forward<E, 256, 4>(a, s);
+  if (W <= 16384) return forward<E, 1024, 2>(a, s);
+  k_layer_norm_wide<E><<<std::min(a.rows, 16 * kCUs), kBlock, 0, s>>>(a);
 }
 
 template <class E, int TPR, int NV>
 int backward(const LayerNormArgs& a, float* part, hipStream_t s) {
   const int n = bwd_blocks(a, Shape<TPR>::kRows);
-  if (n) k_layer_norm_bwd<E, TPR, NV><<<n, Shape<TPR>::kThreads, 0, s>>>(a, part);
+  if (n) (a.vec ? k_layer_norm_bwd<E, TPR, NV, false> : k_layer_norm_bwd<E, TPR, NV, true>)<<<n, Shape<TPR>::kThreads, 0, s>>>(a, part);
   return n;
+}
+template <class E, int NV>
+int backward_wide(const LayerNormArgs& a, float* part, hipStream_t s) {
+  const int n = bwd_blocks(a, 1);
+  if (n) k_layer_norm_bwd_wide<E, NV><<<n, 1024, 0, s>>>(a, part);
+  return n;
+}
+// Workgroups that ran, each with its sums.
+template <class E>
+int backward_rows(const LayerNormArgs& a, float* part, hipStream_t s) {
+  const int W = a.W;
+  if (W <= 32) return backward<E, 4, 1>(a, part, s);
+  if (W <= 64) return backward<E, 8, 1>(a, part, s);
+  if (W <= 128) return backward<E, 16, 1>(a, part, s);
+  if (W <= 256) return backward<E, 32, 1>(a, part, s);
+  if (W <= 512) return backward<E, 64, 1>(a, part, s);
+  if (W <= 1024) return backward<E, 64, 2>(a, part, s);
+  if (W <= 2048) return backward<E, 256, 1>(a, part, s);
+  if (W <= 4096) return backward<E, 256, 2>(a, part, s);
+  if (W <= 8192) return backward<E, 512, 2>(a, part, s);
+  if (W <= 16384) return backward_wide<E, 2>(a, part, s);
+  return backward_wide<E, 0>(a, part, s);
 }
 template <class E>
 void backward(const LayerNormArgs& a, float* part, hipStream_t s) {
-  const int W = a.W;
-  int n;
-  if (!a.vec || W > 8192) {
-    n = bwd_blocks(a, 1);
-    if (n) (a.vec ? k_layer_norm_bwd_any<E, 8> : k_layer_norm_bwd_any<E, 1>)<<<n, kBlock, 0, s>>>(a, part);
-  } else if (W <= 32)
-    n = backward<E, 4, 1>(a, part, s);
-  else if (W <= 64)
-    n = backward<E, 8, 1>(a, part, s);
-  else if (W <= 128)
-    n = backward<E, 16, 1>(a, part, s);
-  else if (W <= 256)
-    n = backward<E, 32, 1>(a, part, s);
-  else if (W <= 512)
-    n = backward<E, 64, 1>(a, part, s);
-  else if (W <= 1024)
-    n = backward<E, 64, 2>(a, part, s);
-  else if (W <= 2048)
-    n = backward<E, 256, 1>(a, part, s);
-  else if (W <= 4096)
-    n = backward<E, 256, 2>(a, part, s);
-  else
-    n = backward<E, 512, 2>(a, part, s);
-  if (a.dw || a.db) k_layer_norm_dw<E><<<(2 * W + 15) / 16, 1024, 0, s>>>(a, n, part);
+  const int n = backward_rows<E>(a, part, s);
+  if (a.dw || a.db) k_layer_norm_dw<E><<<(2 * a.W + 15) / 16, 1024, 0, s>>>(a, n, part);
 }
 
 }  // namespace
