@@ -7,70 +7,143 @@
 // A stream, bound by memory.  Where the pairs of a lane's 8 elements share an axis
 // (kWhole: runs of pairs in multiples of 8, of 4 where pairs lie side by side) its
 // cosines and sines are four 16-byte loads from one row of the table, as with a single
-// axis.  Otherwise (kMixed: axes in turn) they are loaded one by one.
+// axis.  Otherwise (kMixed: axes in turn) a workgroup looks its rows' up together.
 #define PNERF_LAYERS_DEVICE
 #include "norm_common.h"
 
 namespace pnerf {
 namespace {
 
-// Which position a lane's pairs turn by.
+// Workgroups that look angles up in advance: no more than run at once (31 us with twice as
+// many, 29 with half, where these take 28).
+constexpr int kMixedBlocks = 8 * kCUs;
+
+// Which positions a lane's pairs turn by.
 enum Axes {
   kWhole,  // that of one axis, which the lane's pairs share
-  kMixed   // each pair its own: cosines and sines are loaded one by one
-};
-// The axes of a lane's pairs, 2 bits each, and the positions of its row that it needs.
-template <Axes X, Pairs P>
-struct Positions {
-  uint32_t bits;
-  int pos[X == kMixed ? 4 : 1];
-  __device__ __forceinline__ Positions(const NormArgs& a, int d) : bits(0) {
-    pos[0] = 0;
-    if (d >= a.R) return;
-    const int j = P == kInside ? d / 2 : d < a.R / 2 ? d : d - a.R / 2;
-    bits = a.pair_axis[j / 16] >> (2 * (j % 16));
-  }
-  __device__ __forceinline__ void fetch(const NormArgs& a, const int32_t* p, int row) {
-    if (X == kWhole) pos[0] = p[(int64_t)row * a.axes + (bits & 3)];
-    if (X == kMixed)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < a.axes) pos[i] = p[(int64_t)row * a.axes + i];
-  }
-  __device__ __forceinline__ int of(int i) const {  // of the lane's pair i
-    const uint32_t x = bits >> (2 * i);
-    return x & 2 ? (x & 1 ? pos[3] : pos[2]) : (x & 1 ? pos[1] : pos[0]);
-  }
+  kMixed   // each pair its own
 };
 
-// The same with an axis for each pair.
-template <Pairs P, Axes X>
-__device__ __forceinline__ void angles(const NormArgs& a, const Positions<X, P>& at, int d, float c[8], float s[8]) {
-  if constexpr (X != kMixed) {
-    angles<P>(a, at.pos[0], d, c, s);
-  } else {
-    const int half = a.R / 2;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = 1.0f, s[i] = 0.0f;
+// The cosines and sines of a lane's pairs, where they share an axis: one row of the table.
+template <Axes X, Pairs P, int LR>
+struct Angles {
+  int axis, pos;
+  __device__ __forceinline__ Angles(const NormArgs& a, const NormSide& x, int blk, int blocks, float*) : axis(0), pos(0) {
+    const int d = 8 * (threadIdx.x % LR);
     if (d >= a.R) return;
-    const int j = P == kInside ? d / 2 : d < half ? d : d - half;
+    const int j = P == kInside ? d / 2 : d < a.R / 2 ? d : d - a.R / 2;
+    axis = a.pair_axis[j / 16] >> (2 * (j % 16)) & 3;
+  }
+  __device__ __forceinline__ void start(const NormArgs&) {}
+  // Called where the row's data are requested.
+  __device__ __forceinline__ void fetch(const NormArgs& a, const NormSide& x, int row) {
+    pos = x.pos[(int64_t)row * a.axes + axis];
+  }
+  __device__ __forceinline__ void of(const NormArgs& a, int, int d, float c[8], float s[8]) { angles<P>(a, pos, d, c, s); }
+};
+
+// Where each pair has its own, a workgroup's heads are neighbours, mostly of one row: the
+// angles of its rows are looked up once a pair and shared through LDS.  (A lane that
+// looks up its own, 16 four-byte loads: 67 us where this takes 28, and shared axes 21, for
+// 8192 rows of 16 and of 8 bfloat16 heads of 128.)  They are requested one step ahead of
+// their use, the positions two.
+template <Pairs P, int LR>
+struct Angles<kMixed, P, LR> {
+  static constexpr int kGroups = kBlock / LR, kPairs = 4 * LR, kLoads = 4;  // rows of a load: kGroups / 4
+  const NormSide& x;
+  float* stage;  // [2][kGroups][R]
+  Walk now, next, later;  // the workgroup's first head: of this step, the next two
+  int j, axis, first, buf;
+  bool mine;
+  int pos[kLoads];
+  float c[kLoads], s[kLoads];
+  __device__ __forceinline__ Angles(const NormArgs& a, const NormSide& x_, int blk, int blocks, float* lds)
+      : x(x_), stage(lds), now(x_, (int64_t)blk * kGroups, (int64_t)blocks * kGroups), next(now), later(now),
+        j(threadIdx.x % kPairs), axis(0), first(threadIdx.x / kPairs), buf(1), mine(j < a.R / 2) {
+    if (mine) axis = a.pair_axis[j / 16] >> (2 * (j % 16)) & 3;
+    next.next();
+    later.next(), later.next();
+  }
+  // Rows of a step.
+  __device__ __forceinline__ static int rows(const Walk& w) {
+    return w.on() ? (w.head + (int)min(w.left, (int64_t)kGroups) - 1) / w.heads + 1 : 0;
+  }
+  __device__ __forceinline__ void positions(const NormArgs& a, const Walk& w) {
+    const int n = rows(w);
 #pragma unroll
-    for (int i = 0; i < (P == kInside ? 4 : 8); ++i) {
-      const int pos = at.of(i);
-      const bool in = pos >= 0 && pos < a.n_pos;
-      const float* t = a.table + (int64_t)(in ? pos : 0) * a.R + j + i;
-      const float cc = in ? t[0] : __builtin_nanf(""), ss = in ? t[half] : __builtin_nanf("");
-      if (P == kInside)
-        c[2 * i] = c[2 * i + 1] = cc, s[2 * i] = -ss, s[2 * i + 1] = ss;
-      else
-        c[i] = cc, s[i] = d < half ? -ss : ss;
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = first + i * (kGroups / 4);
+      if (mine && r < n) pos[i] = x.pos[(int64_t)(w.row + r) * a.axes + axis];
     }
   }
+  __device__ __forceinline__ void look_up(const NormArgs& a, const Walk& w) {
+    const int n = rows(w);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (!mine || first + i * (kGroups / 4) >= n) continue;
+      const bool in = pos[i] >= 0 && pos[i] < a.n_pos;
+      const float* t = a.table + (int64_t)(in ? pos[i] : 0) * a.R + j;
+      c[i] = in ? t[0] : __builtin_nanf("");
+      s[i] = in ? t[a.R / 2] : __builtin_nanf("");
+    }
+  }
+  __device__ __forceinline__ void start(const NormArgs& a) {
+    positions(a, now);
+    look_up(a, now);
+    positions(a, next);
+  }
+  __device__ __forceinline__ void fetch(const NormArgs&, const NormSide&, int) {}
+  // For this step, which every wavefront of the workgroup makes; row: the lane's.
+  __device__ __forceinline__ void of(const NormArgs& a, int row, int d, float cs[8], float sn[8]) {
+    buf ^= 1;
+    float* to = stage + buf * kGroups * a.R;
+    const int n = rows(now), row0 = now.row;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = first + i * (kGroups / 4);
+      if (mine && r < n) to[r * a.R + j] = c[i], to[r * a.R + a.R / 2 + j] = s[i];
+    }
+    look_up(a, next);
+    positions(a, later);
+    now = next, next = later;
+    later.next();
+    __syncthreads();
+    const int half = a.R / 2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) cs[i] = 1.0f, sn[i] = 0.0f;
+    if (d >= a.R) return;
+    const float* t = to + (row - row0) * a.R;
+    if (P == kInside) {
+      const floatx4 cc = *reinterpret_cast<const floatx4*>(t + d / 2), ss = *reinterpret_cast<const floatx4*>(t + half + d / 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        cs[2 * i] = cs[2 * i + 1] = cc[i];
+        sn[2 * i] = -ss[i], sn[2 * i + 1] = ss[i];
+      }
+    } else {
+      const int k = d < half ? d : d - half;
+      float v[8];
+      load<float>(t + k, cs);
+      load<float>(t + half + k, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sn[i] = d < half ? -v[i] : v[i];
+    }
+  }
+};
+template <Axes X>
+constexpr int kStage = X == kMixed ? 2 * 8 * kBlock : 1;  // floats: 8 a lane, twice
+
+// Holds the compiler to have these values here: waited for after the next step's loads
+// were issued, they would be waited for together with those.
+__device__ __forceinline__ void arrived(float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(v[i]));
 }
 
 template <class E, int LR, Pairs P, Axes X>
 __global__ __launch_bounds__(kBlock) void k_axes_fwd(const NormArgs a, int blocks0, int blocks1) {
   constexpr int NG = kBlock / LR;
+  __shared__ __attribute__((aligned(16))) float stage[kStage<X>];
   const bool second = (int)blockIdx.x >= blocks0;
   const NormSide& x = second ? a.side[1] : a.side[0];
   const int blk = second ? blockIdx.x - blocks0 : blockIdx.x, blocks = second ? blocks1 : blocks0;
@@ -82,20 +155,28 @@ __global__ __launch_bounds__(kBlock) void k_axes_fwd(const NormArgs a, int block
   if (col && x.w) load<E>((const E*)x.w + d, w);
   const float inv_d = 1.0f / a.D;
   Walk at(x, (int64_t)blk * NG + threadIdx.x / LR, (int64_t)blocks * NG);
+  int64_t left = (int64_t)x.rows * x.heads - (int64_t)blk * NG;  // of the workgroup's first head
+  Angles<X, P, LR> angle(a, x, blk, blocks, stage);
+  if (a.R) angle.start(a);
   typename Elem<E>::Raw raw = {};
-  Positions<X, P> pos(a, d);
   auto fetch = [&] {
     if (!at.on() || !col) return;
     raw = Elem<E>::raw((const E*)x.x + at.row * x.xs[0] + at.head * x.xs[1] + d);
-    if (a.R) pos.fetch(a, x.pos, at.row);
+    if (a.R) angle.fetch(a, x, at.row);
   };
   fetch();
-  // every lane of a wavefront makes the same number of rounds: the exchanges need them all
-  while (__any(at.on())) {
+  // every wavefront makes the same number of rounds: the exchanges and barriers need them all
+  for (; left > 0; left -= (int64_t)blocks * NG) {
     float v[8], p[8], c[8], s[8];
     const bool here = at.on() && col;
     Elem<E>::unpack(raw, v);
-    angles<P, X>(a, pos, here ? d : a.R, c, s);
+    arrived(v);
+    if (a.R) {
+      angle.of(a, at.row, here ? d : a.R, c, s);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = 1.0f, s[j] = 0.0f;
+    }
     E* y = (E*)x.y + at.row * x.ys[0] + at.head * x.ys[1] + d;
     at.next();
     fetch();
@@ -107,11 +188,9 @@ __global__ __launch_bounds__(kBlock) void k_axes_fwd(const NormArgs a, int block
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= r * w[j];
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] *= a.sign;
     partners<P, LR>(a, d, v, p);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * c[j] + p[j] * s[j];
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * c[j] + p[j] * (a.sign * s[j]);
     if (here) Elem<E>::store(y, v);
   }
 }
@@ -121,6 +200,7 @@ template <class E, int LR, Pairs P, Axes X>
 __global__ __launch_bounds__(kBlock) void k_axes_bwd(const NormArgs a, int blocks0, int blocks1, float* part) {
   constexpr int NG = kBlock / LR;
   __shared__ float red[NG][8 * LR];
+  __shared__ __attribute__((aligned(16))) float stage[kStage<X>];
   const bool second = (int)blockIdx.x >= blocks0;
   const NormSide& x = second ? a.side[1] : a.side[0];
   const int blk = second ? blockIdx.x - blocks0 : blockIdx.x, blocks = second ? blocks1 : blocks0;
@@ -132,21 +212,30 @@ __global__ __launch_bounds__(kBlock) void k_axes_bwd(const NormArgs a, int block
   if (col && x.w) load<E>((const E*)x.w + d, w);
   const float inv_d = 1.0f / a.D;
   Walk at(x, (int64_t)blk * NG + grp, (int64_t)blocks * NG);
+  int64_t left = (int64_t)x.rows * x.heads - (int64_t)blk * NG;
+  Angles<X, P, LR> angle(a, x, blk, blocks, stage);
+  if (a.R) angle.start(a);
   typename Elem<E>::Raw raw_x = {}, raw_g = {};
-  Positions<X, P> pos(a, d);
   auto fetch = [&] {
     if (!at.on() || !col) return;
     raw_x = Elem<E>::raw((const E*)x.x + at.row * x.xs[0] + at.head * x.xs[1] + d);
     raw_g = Elem<E>::raw((const E*)x.dy + at.row * x.dys[0] + at.head * x.dys[1] + d);
-    if (a.R) pos.fetch(a, x.pos, at.row);
+    if (a.R) angle.fetch(a, x, at.row);
   };
   fetch();
-  while (__any(at.on())) {
+  for (; left > 0; left -= (int64_t)blocks * NG) {
     float v[8], g[8], p[8], c[8], s[8];
     const bool here = at.on() && col;
     Elem<E>::unpack(raw_x, v);
     Elem<E>::unpack(raw_g, g);
-    angles<P, X>(a, pos, here ? d : a.R, c, s);
+    arrived(v);
+    arrived(g);
+    if (a.R) {
+      angle.of(a, at.row, here ? d : a.R, c, s);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = 1.0f, s[j] = 0.0f;
+    }
     E* dx = (E*)x.dx + at.row * x.dxs[0] + at.head * x.dxs[1] + d;
     at.next();
     fetch();
@@ -273,7 +362,7 @@ void launch_lr(const NormArgs& a, bool bwd, float* part, int n, const int b[2], 
 template <class E>
 void launch_e(const NormArgs& a, bool bwd, float* part, hipStream_t s) {
   int b[2];
-  blocks_of(a, bwd ? kBwdBlocks : kFwdBlocks, b);
+  blocks_of(a, bwd ? kBwdBlocks : a.whole || !a.vec ? kFwdBlocks : kMixedBlocks, b);
   const int n = b[0] + b[1];
   if (n == 0) return;
   if (!a.vec) {
