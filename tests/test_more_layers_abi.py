@@ -250,7 +250,7 @@ def test_binding_wants_device_tensors():
 # ---------------------------------------------------------------- the compiler's word
 # kernel (mangled-name fragment) -> minimum waves per SIMD
 BUDGET = {
-    "rotate_axes.hip": {"k_axes_fwd": 6, "k_axes_bwd": 4, "k_axes_any": 4},
+    "rotate_axes.hip": {"k_axes_fwd": 4, "k_axes_bwd": 4, "k_axes_any": 4},
     "layer_norm.hip": {"k_layer_norm": 2},
     "clip.hip": {"k_clip": 6},
     "quantize.hip": {"k_quantize": 6},
