@@ -401,28 +401,35 @@ __global__ __launch_bounds__(1024) void k_layer_norm_bwd_wide(const LayerNormArg
     });
 }
 
-// dw and db: the workgroups' sums added up in order, 16 columns a workgroup, 64 sums at a time.
+// dw and db: the workgroups' sums added up in order, kCols columns a workgroup, kSums sums
+// at a time.
+constexpr int kCols = 32, kSums = 32;
 template <class E>
-__global__ __launch_bounds__(1024) void k_layer_norm_dw(const LayerNormArgs a, int n, const float* part) {
-  __shared__ float red[64][17];
-  const int col = blockIdx.x * 16 + threadIdx.x % 16, r = threadIdx.x / 16;  // of dw, then of db
+__global__ __launch_bounds__(kCols * kSums) void k_layer_norm_dw(const LayerNormArgs a, int n, const float* part) {
+  __shared__ float red[kSums][kCols + 1];
+  const int c = threadIdx.x % kCols, r = threadIdx.x / kCols;
+  const int64_t col = (int64_t)blockIdx.x * kCols + c;  // of dw, then of db
   float t = 0.0f;
   if (col < 2 * a.W)
-#pragma unroll 4
-    for (int i = r; i < n; i += 64) t += part[(int64_t)i * 2 * a.W + col];
-  red[r][threadIdx.x % 16] = t;
+#pragma unroll 8
+    for (int i = r; i < n; i += kSums) t += part[(int64_t)i * 2 * a.W + col];
+  red[r][c] = t;
   __syncthreads();
   if (r != 0 || col >= 2 * a.W) return;
   E* out = (E*)(col < a.W ? a.dw : a.db);
   if (!out) return;
   t = 0.0f;
-  for (int i = 0; i < 64; ++i) t += red[i][threadIdx.x];
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) t += red[i][c];
   out[col < a.W ? col : col - a.W] = (E)t;
 }
 
-// Workgroups of the gradient: each leaves its sums, so they are bounded.
-int bwd_blocks(const LayerNormArgs& a, int rows_wg) {
-  const int64_t most = std::max<int64_t>(kCUs, std::min<int64_t>(4 * kCUs, ((int64_t)1 << 21) / a.W));
+// Workgroups of the gradient: each leaves its sums, so they are bounded; and no more
+// than run at once, `per_cu` a compute unit by their registers (16384 x 1024, bf16: 25 us
+// with 2 or 3, 28 with 4; 8192 x 3000, f32: 57 with 2, 69 with the 699 that the sums allow.
+// 16381 x 2048, bf16, forward and backward: 82 us with 4, 87 with 2).
+int bwd_blocks(const LayerNormArgs& a, int rows_wg, int per_cu) {
+  const int64_t most = std::max<int64_t>(kCUs, std::min<int64_t>(per_cu * kCUs, ((int64_t)1 << 21) / a.W));
   return (int)std::min<int64_t>(((int64_t)a.rows + rows_wg - 1) / rows_wg, most);
 }
 
@@ -450,13 +457,14 @@ void forward(const LayerNormArgs& a, hipStream_t s) {
 
 template <class E, int TPR, int NV>
 int backward(const LayerNormArgs& a, float* part, hipStream_t s) {
-  const int n = bwd_blocks(a, Shape<TPR>::kRows);
+  constexpr int kPerCu = NV == 2 ? (sizeof(E) == 4 ? 2 : 3) : 4;
+  const int n = bwd_blocks(a, Shape<TPR>::kRows, kPerCu);
   if (n) (a.vec ? k_layer_norm_bwd<E, TPR, NV, false> : k_layer_norm_bwd<E, TPR, NV, true>)<<<n, Shape<TPR>::kThreads, 0, s>>>(a, part);
   return n;
 }
 template <class E, int NV>
 int backward_wide(const LayerNormArgs& a, float* part, hipStream_t s) {
-  const int n = bwd_blocks(a, 1);
+  const int n = bwd_blocks(a, 1, 1);
   if (n) k_layer_norm_bwd_wide<E, NV><<<n, 1024, 0, s>>>(a, part);
   return n;
 }
@@ -479,7 +487,7 @@ int backward_rows(const LayerNormArgs& a, float* part, hipStream_t s) {
 template <class E>
 void backward(const LayerNormArgs& a, float* part, hipStream_t s) {
   const int n = backward_rows<E>(a, part, s);
-  if (a.dw || a.db) k_layer_norm_dw<E><<<(2 * a.W + 15) / 16, 1024, 0, s>>>(a, n, part);
+  if (a.dw || a.db) k_layer_norm_dw<E><<<(2 * a.W + kCols - 1) / kCols, kCols * kSums, 0, s>>>(a, n, part);
 }
 
 }  // namespace
@@ -493,7 +501,7 @@ hipError_t launch_layer_norm_fwd(const LayerNormArgs& a, hipStream_t s) {
 }
 
 // (From the sizes alone: no call has more workgroups than one with a row each.)
-int64_t layer_norm_bwd_bytes(const LayerNormArgs& a) { return (int64_t)bwd_blocks(a, 1) * 2 * a.W * 4; }
+int64_t layer_norm_bwd_bytes(const LayerNormArgs& a) { return (int64_t)bwd_blocks(a, 1, 4) * 2 * a.W * 4; }
 
 hipError_t launch_layer_norm_bwd(const LayerNormArgs& a, void* ws, hipStream_t s) {
   if (a.dtype == kF32) backward<float>(a, (float*)ws, s);
