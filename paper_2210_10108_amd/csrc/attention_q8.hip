@@ -229,25 +229,21 @@ __device__ __forceinline__ void copy_tile8(uint4* lds, const void* p, const int6
 }
 
 // The loads of tiles of 64 rows of bytes into registers by NW wavefronts, and their way
-// to LDS as 16-bit elements.  A lane takes 16-byte chunks, the same columns of rows
-// that differ by kRows from load to load; the rows of 16 neighbouring lanes are chosen
-// so that their two 16-byte writes each, the even and the odd chunk, cover all banks
-// (see swz_bits): rows 0 and 4, or 0, 4, 1 and 5 of eight.
+// to LDS as 16-bit elements.  A lane takes 8 bytes, 16 when they are widened: 8
+// neighbouring lanes then write 8 neighbouring chunks, which cover all banks.  (Of 16
+// bytes a lane they would write every other chunk: half of all LDS cycles were conflicts.)
 template <class T, int DP, int NW>
 struct ByteTile {
-  static constexpr int kChunks = DP / 16;                // of a row
+  static constexpr int kChunks = DP / 8;                 // of a row
   static constexpr int kRows = 64 / kChunks * NW;        // of one load of all wavefronts
   static constexpr int kLoads = kBN / kRows;             // of a wavefront
   const char* base;
   int64_t row_bytes;
-  int D, row, col;  // this lane's row of the first load, its column
-  uint4 raw[kLoads];
+  int D, row, chunk;  // this lane's row of the first load, its chunk
+  uint2 raw[kLoads];
   __device__ __forceinline__ ByteTile(const void* p, int64_t first, int64_t stride, int D_, int wave, int lane)
-      : base((const char*)p + first), row_bytes(stride), D(D_) {
-    const int i = lane / kChunks;
-    row = wave * (64 / kChunks) + ((i & 1) << 2 | (i & 6) >> 1 | (i & 8));
-    col = 16 * (lane % kChunks);
-  }
+      : base((const char*)p + first), row_bytes(stride), D(D_), row(wave * (64 / kChunks) + lane / kChunks),
+        chunk(lane % kChunks) {}
   // Tile t of n_rows rows.  on: its rows that may be read; the others, and what lies
   // past the head's width, are zeros (a row past the last is beyond the bound only
   // where rows do not overlap).
@@ -255,26 +251,27 @@ struct ByteTile {
     const u32x4 d = descriptor(base + (int64_t)t * kBN * row_bytes, (int64_t)(n_rows - t * kBN - 1) * row_bytes + D);
     const __amdgpu_buffer_rsrc_t desc = __builtin_amdgcn_make_buffer_rsrc(
         reinterpret_cast<void*>((uint64_t)d[1] << 32 | d[0]), 0, d[2], d[3]);
-    const uint32_t off = col < D ? (uint32_t)row * (uint32_t)row_bytes + col : kOutside;
+    const uint32_t off = 8 * chunk < D ? (uint32_t)row * (uint32_t)row_bytes + 8 * chunk : kOutside;
     const uint32_t step = kRows * (uint32_t)row_bytes;
     const uint64_t mine = on >> row;
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       const uint32_t o = on == ~0ull || (mine >> (n * kRows) & 1) ? off + n * step : kOutside;
-      raw[n] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(desc, o, 0, 0));
+      raw[n] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(desc, o, 0, 0));
     }
   }
   __device__ __forceinline__ void widen(uint4* lds) const {
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      lds[swz<DP / 8>(row + n * kRows, col / 8)] = widen8<T>(raw[n].x, raw[n].y);
-      lds[swz<DP / 8>(row + n * kRows, col / 8 + 1)] = widen8<T>(raw[n].z, raw[n].w);
-    }
+    for (int n = 0; n < kLoads; ++n) lds[swz<DP / 8>(row + n * kRows, chunk)] = widen8<T>(raw[n].x, raw[n].y);
   }
 };
 
 // Many rows: four wavefronts of 32 rows share the tiles, two of them in LDS and the
 // next in registers on its way there.  One barrier a tile.  KS = 2: as in k_attn_fwd.
+// Matrix products, exponentials and LDS reads bound it, as with 16-bit states, and the
+// widening on top (2 x 4096 rows, 8192 keys, 32 heads of 128 over 8, bf16: 1195 us or 0.92
+// PFLOP/s, 16-bit states 1065).  Widening the next tile beside the scores' products, in one
+// stretch of code with them, spills and takes 1440 where the 16-bit form takes 1203.
 template <class T, int DP, int KS>
 __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs a, const Order order) {
   using Tile = ByteTile<T, DP, 4>;
@@ -374,7 +371,9 @@ struct ByteRows {
 // Eight wavefronts with the same rows take the tiles in turn, each with its own keys
 // and values in LDS, as bytes, and no barrier; keys are loaded again as soon as the
 // scores are there, values as soon as they have been used.  The bytes are widened on
-// the way from LDS to the products: each is read once.
+// the way from LDS to the products: each is read once.  (One token over 131109 rows, 32
+// heads of 128 over 8: 60 us or 4.5 TB/s and the join's 5; 64 ragged entries of up to 2500
+// rows, 16 heads over 4: 27 us, 42 with four wavefronts and tiles widened through registers.)
 template <class T, int DP>
 __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Order order) {
   constexpr int kWaves = 8, kTile = kBN * DP;

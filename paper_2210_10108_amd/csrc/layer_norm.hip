@@ -2,6 +2,10 @@
 //   dx = r (g - mean g - n mean(g n)) + dres,  dw = sum_rows dy n,  db = sum_rows dy
 // with g = dy w, n = (x - mean) r, r = 1 / sqrt(var + eps).
 //
+// A stream, bound by memory: x in and y out, x, dy (and dres) in and dx out (16384 x 1024
+// bf16: 13.4 us or 5.0 TB/s forward, 25 us or 4.0 TB/s backward with its sums; 8192 x 3000
+// f32: 5.2 and 6.2 TB/s; a copy reaches 5.2).
+//
 // Sums are float32.  A row's mean is taken in two steps, m = mean x and then c =
 // mean(x - m), and var = mean (x - m)^2 - c^2: rows whose mean is large beside their
 // spread lose nothing but what x itself was rounded to, and the gradient makes its
@@ -433,6 +437,11 @@ int bwd_blocks(const LayerNormArgs& a, int rows_wg, int per_cu) {
   return (int)std::min<int64_t>(((int64_t)a.rows + rows_wg - 1) / rows_wg, most);
 }
 
+// Threads of a row: the fewest that hold it in one group each up to a wavefront, two
+// groups of a wavefront up to 1024 (16384 x 1024, bf16: 13.5 us, backward 25; a workgroup
+// of 256 with barriers, half of it idle: 17.4 and 35), then a workgroup, with few groups a
+// thread rather than many threads (8192 x 3000, bf16: two groups of 256 threads 19 and 40
+// us, one of 512 21 and 48; 8192 x 8192: four groups of 256 42 us, one of 1024 68).
 template <class E, int TPR, int NV>
 void forward(const LayerNormArgs& a, hipStream_t s) {
   constexpr int kRows = Shape<TPR>::kRows;

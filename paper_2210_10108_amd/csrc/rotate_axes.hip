@@ -4,7 +4,8 @@
 // axis.  The gradient of a rotation alone is the rotation back, the forward kernel with
 // the sines negated.
 //
-// A stream, bound by memory.  Where the pairs of a lane's 8 elements share an axis
+// A stream, bound by memory (16382 rows of 16 and of 8 bf16 heads of 128: 45 us or 4.5
+// TB/s).  Where the pairs of a lane's 8 elements share an axis
 // (kWhole: runs of pairs in multiples of 8, of 4 where pairs lie side by side) its
 // cosines and sines are four 16-byte loads from one row of the table, as with a single
 // axis.  Otherwise (kMixed: axes in turn) a workgroup looks its rows' up together.
