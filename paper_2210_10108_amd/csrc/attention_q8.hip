@@ -114,17 +114,32 @@ struct Scales {
   }
 };
 
-// Rows whose tiles have scales.  `factor` of the scores' unit, `unit` of the sums.
+// Rows whose tiles have scales: c of the scores, and the value scale's ratio to `unit`,
+// in which the sums are kept.  The ratio is a factor of p, by way of its exponent, where
+// its data type holds that: in float16 from 1 to 2^7 (p is at most 2^8, and what it
+// loses below 2^-14 must not grow), in bfloat16, which has float32's range, from 2^-60 to
+// 2^60.  For a tile outside, the unit changes and the sums are rescaled.
 template <class T, int DP>
 struct ScaledRows : Rows<T, DP> {
+  static constexpr bool kNarrow = __is_same(T, F16);
+  static constexpr float kLeast = kNarrow ? 1.0f : 0x1p-60f, kMost = kNarrow ? 0x1p7f : 0x1p60f;
   float c, unit, unit_next;
+  float shift, back;  // log2 of the ratio, its inverse
 
-  __device__ __forceinline__ void begin(const AttnArgs& a) { c = a.c, unit = unit_next = 1.0f; }
+  __device__ __forceinline__ void begin(const AttnArgs& a) {
+    c = a.c, unit = unit_next = 0.0f;
+    shift = 0.0f, back = 1.0f;
+  }
   // The scales of the next tile; one without an allowed key has none that count.
   __device__ __forceinline__ void scales(const AttnArgs& a, Scales& sc, int t, uint64_t vm) {
+    if (!vm) return;
     float ks, vs;
     sc.of(t, ks, vs);
-    if (vm) c = fmaxf(a.c * ks, 0x1p-126f), unit_next = vs;  // (0 times a masked key's -inf would be NaN)
+    c = fmaxf(a.c * ks, 0x1p-126f);  // (0 times a masked key's -inf would be NaN)
+    if (!(vs >= unit * kLeast && vs <= unit * kMost)) unit_next = kNarrow ? vs * 0x1p-3f : vs;
+    const float ratio = vs / unit_next;
+    shift = __builtin_amdgcn_logf(ratio);
+    back = __builtin_amdgcn_rcpf(ratio);
   }
   // Queries in the order in which byte tiles hold the head's width (see bytes_swz).
   __device__ __forceinline__ void init_bytes(const uint16_t* q, bool ok, int D, int h) {
@@ -160,6 +175,29 @@ struct ScaledRows : Rows<T, DP> {
     }
     this->raise(c);
   }
+  // The scores' exponentials times the ratio, and their sum.
+  __device__ __forceinline__ void weights() {
+    const float base = (this->m == -INFINITY ? 0.0f : this->m) - shift;  // -inf: no allowed key yet
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        this->s[n][i] = __builtin_amdgcn_exp2f(fmaf(this->s[n][i], c, -base));
+        sum += this->s[n][i];
+      }
+    this->l = fmaf(sum, back, this->l);
+  }
+  __device__ __forceinline__ void add(const uint4* sv, int lane) {
+    weights();
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {  // 16 keys each
+      const uint4 pf = pack8<T>(this->s[n / 2], 8 * (n % 2));
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+        this->o[d] = T::mma(tr_frag<DP / 8>(sv, 16 * n, 32 * d, lane), pf, this->o[d]);
+    }
+  }
   // The same as scores and add, of tiles of bytes.
   __device__ __forceinline__ void scores_bytes(const char* sk, uint64_t vm, int lane) {
     const int r = lane & 31, h = lane >> 5;
@@ -176,7 +214,7 @@ struct ScaledRows : Rows<T, DP> {
     this->raise(c);
   }
   __device__ __forceinline__ void add_bytes(const char* sv, int lane) {
-    this->weights(c);
+    weights();
     const int l16 = lane & 15, r = 4 * (lane >> 5) + l16 / 2 + (l16 & 8 ? 4 : 0);  // keys 4 h + 0..3 and + 8
 #pragma unroll
     for (int n = 0; n < 4; ++n) {  // 16 keys each
@@ -192,13 +230,14 @@ struct ScaledRows : Rows<T, DP> {
   __device__ __forceinline__ void run(N next, V add_tile) {
     bool more = next();
     while (more) {
-      this->rescale();
-      if (unit_next != unit) {
-        const float f = unit / unit_next;
-        unit = unit_next;
+      // to the new maximum and unit: l by the first, the sums by both
+      const float alpha = __builtin_amdgcn_exp2f(this->m - (this->top == -INFINITY ? 0.0f : this->top));
+      const float f = unit == unit_next || unit == 0.0f ? alpha : alpha * (unit / unit_next);
+      this->m = this->top;
+      unit = unit_next;
+      this->l *= alpha;
 #pragma unroll
-        for (int i = 0; i < DP / 32; ++i) this->o[i] *= f;
-      }
+      for (int i = 0; i < DP / 32; ++i) this->o[i] *= f;
       do {
         add_tile();
         more = next();
@@ -325,7 +364,7 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
         ++round;
         return true;
       },
-      [&] { x.add(lds[grp][(round - 1) & 1] + kPieces, x.c, lane); });
+      [&] { x.add(lds[grp][(round - 1) & 1] + kPieces, lane); });
   if constexpr (KS == 2) {
     static_assert(kGroupsLds<DP> <= sizeof(lds), "a group's sums fit LDS");
     if (!join_groups<T, DP>(x, lds, wave, grp, lane)) return;
@@ -447,7 +486,7 @@ __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Ord
         ++t;
         return true;
       },
-      [&] { x.add(sv, x.c, lane); });
+      [&] { x.add(sv, lane); });
   x.close(at.ok);
   if (at.row >= a.M) return;
   if (a.splits > 1)
