@@ -194,6 +194,9 @@ pnerf_status pnerf_linear_backward(const pnerf_linear_params* params, const void
  * of equal elements has n = 0 where eps > 0, NaN where eps = 0; squares of a row's
  * differences past float32's range make it infinite or NaN.
  *
+ * Any width and alignment takes the fast kernels (a width of whole 16-byte chunks the
+ * fastest); the gradient of rows wider than 16384 adds to its sums in memory, row by row.
+ *
  * Requires rows >= 0, 1 <= width <= 2^20, rows * width at most 2^40, finite eps >= 0;
  * any dtype. */
 typedef struct {
@@ -216,6 +219,7 @@ pnerf_status pnerf_layer_norm_backward(const pnerf_layer_norm_params* params, co
  * t_a the row's position along axis a: base.q_pos is [q_rows][axes], base.k_pos
  * [k_rows][axes].  Every frequency an axis may want is in the columns of its pairs.
  * A position outside [0, n_positions) gives NaN in the pairs of its axis.
+ * Pairs that share an axis in runs of 8 (of 4 where interleaved = 1) are the fastest.
  * norm = 1: the heads are normed first, as there; norm = 0: n = x, the weights are not
  * read, the gradient is the rotation back alone (q and k are not read and may be NULL,
  * no weight has a gradient, no workspace is needed).
@@ -287,9 +291,10 @@ pnerf_status pnerf_quantize_states(const pnerf_states_params* params, const void
 /* Cross attention to 8-bit states: pnerf_cross_attention with
  *   k_j = k_scale[j / PNERF_STATE_BLOCK] k8_j,  v_j = v_scale[j / PNERF_STATE_BLOCK] v8_j
  * as pnerf_quantize_states leaves them (attention.k_stride and v_stride are those of k8
- * and v8; attention.dtype is that of q and o).  The scales are positive finite
+ * and v8; attention.dtype is that of q and o).  The scales are positive normal
  * numbers, not only powers of two; those of one head's values within 2^96 of each
- * other.  Keys, values and masks in places that are not allowed, and the scales of
+ * other.  exp(a - m) times the value scale, in a unit that follows it, is rounded to the
+ * data type before it meets the values.  Keys, values and masks in places that are not allowed, and the scales of
  * blocks without an allowed key, have no influence.  No gradient: states are kept in 8
  * bits for proposals, not for training. */
 typedef struct {

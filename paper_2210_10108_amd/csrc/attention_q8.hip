@@ -2,12 +2,12 @@
 // softmax and its products): over the allowed keys j
 //   a_ij = scale ks[j / 64] q_i . k8_j,  o_i = sum_j exp(a_ij - lse_i) vs[j / 64] v8_j
 // with k8, v8 of e4m3 and one scale for each block of 64 rows of a head, which is a
-// tile here.  Every e4m3 number is a float16 and a bfloat16 number: tiles are widened
-// on their way to LDS and the products are those of 16 bits, exact in what they
-// multiply.  A tile's key scale is a factor of its scores.  Its value scale would be
-// one of p, whose 16 bits might not hold it; instead the sums are kept in units of the
-// current scale and rescaled, where the maximum's rescaling stands, when a tile has
-// another one.
+// tile here.  Every e4m3 number is a float16 and a bfloat16 number: tiles are widened on
+// their way to LDS, or from it, and the products are those of 16 bits, exact in what they
+// multiply.  A tile's key scale is a factor of its scores.  Its value scale is one of p, in
+// the exponent that makes it, as far as the 16 bits of p hold it; for scales that lie
+// further apart the sums change their unit, where the maximum's rescaling stands (see
+// ScaledRows).
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
 
@@ -308,9 +308,11 @@ struct ByteTile {
 // Many rows: four wavefronts of 32 rows share the tiles, two of them in LDS and the
 // next in registers on its way there.  One barrier a tile.  KS = 2: as in k_attn_fwd.
 // Matrix products, exponentials and LDS reads bound it, as with 16-bit states, and the
-// widening on top (2 x 4096 rows, 8192 keys, 32 heads of 128 over 8, bf16: 1195 us or 0.92
-// PFLOP/s, 16-bit states 1065).  Widening the next tile beside the scores' products, in one
-// stretch of code with them, spills and takes 1440 where the 16-bit form takes 1203.
+// widening on top: 13 vector instructions for each product of 32 cycles (2 x 4096 rows, 8192
+// keys, 32 heads of 128 over 8, bf16: 1255 us or 0.88 PFLOP/s where 16-bit states take 1116; 5%
+// of the keys masked costs 20% more).  Tried and slower: the next tile widened beside the
+// scores' products (spills), or by one group after them, and sums of unmasked tiles that
+// start from the instruction's own zero.
 template <class T, int DP, int KS>
 __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs a, const Order order) {
   using Tile = ByteTile<T, DP, 4>;
