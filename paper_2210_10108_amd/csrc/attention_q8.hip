@@ -10,6 +10,7 @@
 // ScaledRows).
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_rows.h"
 
@@ -121,7 +122,7 @@ struct Scales {
 // 2^60.  For a tile outside, the unit changes and the sums are rescaled.
 template <class T, int DP>
 struct ScaledRows : Rows<T, DP> {
-  static constexpr bool kNarrow = __is_same(T, F16);
+  static constexpr bool kNarrow = std::is_same<T, F16>::value;
   static constexpr float kLeast = kNarrow ? 1.0f : 0x1p-60f, kMost = kNarrow ? 0x1p7f : 0x1p60f;
   float c, unit, unit_next;
   float shift, back;  // log2 of the ratio, its inverse
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Ord
         if (t < at.t1) {
           mask = at.mask_at((t + kWaves) * kBN + lane);
           kt.load(to_k, t, at.nk, vm_next, lane);
-              }
+        }
         return true;
       },
       [&] { x.add_bytes(sv, lane); });

@@ -508,8 +508,8 @@ def _axes(call, q, k, table, q_pos, k_pos, pair_axis, q_weight, k_weight, eps, i
         raise ValueError("table must be (positions, 2, pairs) and pair_axis name the axis of each of its pairs, 128 at most")
     if eps is None and (q_weight is not None or k_weight is not None):
         raise ValueError("weights without a norm: eps is None")
-    if q_pos.dim() != 2:
-        raise ValueError("positions must have 2 dimensions: rows, axes")
+    if q_pos is None or q_pos.dim() != 2:
+        raise ValueError("q_pos must have 2 dimensions: rows, axes")
     C.memmove(p.pair_axis, pair_axis, len(pair_axis))
     p.norm, p.axes = eps is not None, q_pos.shape[1]
     _, qp, kp = _norm(call, q, k, q_weight, k_weight, table, q_pos, k_pos, eps or 0.0, interleaved,

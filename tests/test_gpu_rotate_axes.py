@@ -200,6 +200,7 @@ def test_rotate_axes_refusals(L):
     for kind, fn in [(ValueError, lambda: L.rotate_axes(q, None, table, pos, None, axis[:15])),
                      (ValueError, lambda: L.rotate_axes(q, None, None, pos, None, axis)),
                      (ValueError, lambda: L.rotate_axes(q, None, table, pos[:, 0], None, axis)),
+                     (ValueError, lambda: L.rotate_axes(q, None, table, None, None, axis)),
                      (ValueError, lambda: L.rotate_axes(q, None, table, pos[:3], None, axis)),
                      (ValueError, lambda: L.rotate_axes(q, None, table, pos, None, axis, q_weight=w)),
                      (ValueError, lambda: L.rotate_axes(q, q, table, pos, pos[:, :1].contiguous(), axis)),

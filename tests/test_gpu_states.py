@@ -180,6 +180,24 @@ def test_attention_q8(L, shape, dt):
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", [(5, 700, 400, 16, 8, 64), (40, 300, 200, 6, 2, 128), (70, 300, 150, 3, 3, 64),
+                                   (130, 1, 500, 12, 6, 128), (70, 150, 100, 4, 4, 33)], ids=str)
+def test_attention_q8_longest_entries_first(L, shape, dt):
+    # more workgroups than compute units, entries of every length: equal ones, empty ones, over 64
+    B, Sq, Sk, Hq, Hkv, D = shape
+    g = gen_of(15)
+    q = normal(g, B, Sq, Hq, D, dt=dt)
+    (k8, ks), (v8, vs) = states(g, B, Sk, Hkv, D), states(g, B, Sk, Hkv, D)
+    kv_len = torch.randint(0, Sk + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    kv_len[B // 2:B // 2 + 3] = kv_len[0]
+    kv_len[-1], kv_len[-2] = 0, Sk + 9
+    q_len = torch.randint(0, Sq + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    check_attention(L, q, k8, v8, ks, vs, "kv lengths", kv_len=kv_len)
+    check_attention(L, q, k8, v8, ks, vs, "both lengths", q_len=q_len, kv_len=kv_len,
+                    kv_mask=torch.rand(B, Sk, generator=g, device="cuda") > 0.1)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
 @pytest.mark.parametrize("D", [1, 7, 33, 72, 100, 127])
 def test_attention_q8_odd_head_widths(L, D, dt):
     g = gen_of(6)
