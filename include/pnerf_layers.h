@@ -191,10 +191,9 @@ pnerf_status pnerf_linear_backward(const pnerf_linear_params* params, const void
  * dx may be dy, dres or x itself.  weight (ones) and bias (zeros) may be NULL, dweight
  * and dbias too (not wanted).  A row is what its elements were rounded to: the mean is
  * taken in two steps, so that a mean large beside the spread costs nothing more.  A row
- * of equal elements has n = 0, to rounding, where eps > 0; where eps = 0 its n is not
- * defined (NaN or any number).  Where the sum of a
- * row's squared differences passes float32's range (differences of some 10^19 / sqrt(W))
- * r is 0, as it is for a variance that is infinite.
+ * of equal elements has n = 0 exactly where eps > 0; where eps = 0 its n is NaN.  Where
+ * the sum of a row's squared differences passes float32's range (differences of some
+ * 10^19 / sqrt(W)) r and n are 0.  An infinity or NaN makes n NaN in all of its row.
  * Any width and alignment takes the fast kernels (a width of whole 16-byte chunks the
  * fastest); the gradient of rows wider than 16384 adds to its sums in memory, row by row.
  *

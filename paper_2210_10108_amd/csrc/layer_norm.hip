@@ -3,13 +3,14 @@
 // with g = dy w, n = (x - mean) r, r = 1 / sqrt(var + eps).
 //
 // A stream, bound by memory: x in and y out, x, dy (and dres) in and dx out (16384 x 1024
-// bf16: 13.4 us or 5.0 TB/s forward, 25 us or 4.0 TB/s backward with its sums; 8192 x 3000
+// bf16: 13.8 us or 4.9 TB/s forward, 25 us or 4.0 TB/s backward with its sums; 8192 x 3000
 // f32: 5.2 and 6.2 TB/s; a copy reaches 5.2).
 //
-// Sums are float32.  A row's mean is taken in two steps, m = mean x and then c =
-// mean(x - m), and var = mean (x - m)^2 - c^2: rows whose mean is large beside their
-// spread lose nothing but what x itself was rounded to, and the gradient makes its
-// statistics again from the row that it reads anyway.
+// Sums are float32.  A row's mean is taken in two steps, m = x_0 + mean(x - x_0) and then
+// c = mean(x - m), and var = mean (x - m)^2 - c^2: rows whose mean is large beside their
+// spread lose nothing but what x itself was rounded to, equal elements give 0 exactly at
+// any size, and the gradient makes its statistics again from the row that it reads anyway.
+// Where the sum of squares passes float32's range, r and n are 0.
 #define PNERF_LAYERS_DEVICE
 #include <algorithm>
 
@@ -110,10 +111,45 @@ __device__ __forceinline__ void store8(void* p, int64_t at, const float (&v)[8],
     Elem<E>::store((E*)p + at, v);
 }
 
-// NV groups of 8 elements of a row as they are loaded.
+// Statistics of a row: c = mean d and r, from the sums of d = x - m and d^2.  Where those
+// pass float32's range (far) c and r are 0, and n is the sum of 0 x in all places: 0, or
+// NaN where the row itself holds one or an infinity.
+struct Stats {
+  float c, r;
+  bool far;
+  __device__ __forceinline__ Stats(float sum, float squares, float inv, float eps)
+      : c(sum * inv), far(!(squares < INFINITY)) {
+    r = inv_rms(fmaxf(squares * inv - c * c, 0.0f), eps);
+    if (far) c = r = 0.0f;
+  }
+};
+
+// The sum of 0 x over a row (NULL: 0), which is read again for it.
+template <class E, int TPR>
+__device__ __forceinline__ float zeros_of(RowSums<TPR>& sums, const E* row, int W) {
+  float z[1] = {0.0f};
+  if (row)
+#pragma unroll 1
+    for (int d = threadIdx.x % TPR; d < W; d += TPR) z[0] += 0.0f * (float)row[d];
+  sums.sum(z);
+  return z[0];
+}
+
+// NV groups of 8 elements of a row as they are loaded; zeros past its end.
 template <class E, int TPR, int NV, bool ODD>
 struct Group {
   typename Elem<E>::Raw raw[NV];
+  E head;  // the row's first element, where other wavefronts have it
+  __device__ __forceinline__ void load_row(const void* p, int64_t at, int W) {
+    load(p, at, W);
+    if (TPR > 64) head = ((const E*)p)[at];
+  }
+  // The first element; v: of this thread's first group.
+  __device__ __forceinline__ float first(float v) const {
+    if (TPR > 64) return (float)head;
+    if (TPR == 64) return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+    return __shfl(v, (int)(threadIdx.x & 63) / TPR * TPR);
+  }
   __device__ __forceinline__ void load(const void* p, int64_t at, int W) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -123,6 +159,14 @@ struct Group {
   }
 };
 
+template <int NV>
+__device__ __forceinline__ void fill(float (&v)[NV][8], float x) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[k][j] = x;
+}
+
 template <class E, int TPR, int NV, bool ODD>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm(const LayerNormArgs a) {
   constexpr int kRows = Shape<TPR>::kRows;
@@ -130,35 +174,40 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm(const Layer
   RowSums<TPR> sums(lds);
   const int group = threadIdx.x / TPR;
   const float inv = 1.0f / a.W;
-  // elements of the row from j of group k on (0 or less: none is there; 8 at a time but for ODD)
-  auto left = [&](int k, int j) { return a.W - 8 * ((int)(threadIdx.x % TPR) + k * TPR) - (ODD ? j : 0); };
+  // x where the row has an element j of group k, 0 past its end (groups are whole but for ODD)
+  auto here = [&](int k, int j, float x) { return 8 * ((int)(threadIdx.x % TPR) + k * TPR) + (ODD ? j : 0) < a.W ? x : 0.0f; };
   Group<E, TPR, NV, ODD> x = {}, w = {}, b = {};
   if (a.w) w.load(a.w, 0, a.W);
   if (a.b) b.load(a.b, 0, a.W);
   int64_t row = (int64_t)blockIdx.x * kRows + group;
   const int64_t step = (int64_t)gridDim.x * kRows;
-  if (row < a.rows) x.load(a.x, row * a.xs, a.W);
+  if (row < a.rows) x.load_row(a.x, row * a.xs, a.W);
   for (; row - group < a.rows; row += step) {
     float v[NV][8], t[1] = {0.0f}, u[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      Elem<E>::unpack(x.raw[k], v[k]);
+    for (int k = 0; k < NV; ++k) Elem<E>::unpack(x.raw[k], v[k]);
+    const float x0 = x.first(v[0][0]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[0] += left(k, j) > 0 ? v[k][j] : 0.0f;
-    }
-    if (row + step < a.rows) x.load(a.x, (row + step) * a.xs, a.W);
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[0] += v[k][j] - here(k, j, x0);
+    if (row + step < a.rows) x.load_row(a.x, (row + step) * a.xs, a.W);
     sums.sum(t);
-    const float m = t[0] * inv;
+    const float m = x0 + t[0] * inv;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        v[k][j] = left(k, j) > 0 ? v[k][j] - m : 0.0f;
+        v[k][j] -= here(k, j, m);
         u[0] += v[k][j], u[1] += v[k][j] * v[k][j];
       }
     }
     sums.sum(u);
-    const float c = u[0] * inv, r = inv_rms(fmaxf(u[1] * inv - c * c, 0.0f), a.eps);
+    const Stats st(u[0], u[1], inv, a.eps);
+    if (__any(st.far)) {
+      const float n = zeros_of(sums, row < a.rows ? (const E*)a.x + row * a.xs : nullptr, a.W);
+      if (st.far) fill(v, n);
+    }
     if (row >= a.rows) continue;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -169,7 +218,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm(const Layer
       Elem<E>::unpack(b.raw[k], bk);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float n = (v[k][j] - c) * r;
+        const float n = (v[k][j] - st.c) * st.r;
         v[k][j] = (a.w ? n * wk[j] : n) + (a.b ? bk[j] : 0.0f);
       }
       store8<E, ODD>(a.y, row * a.ys + d, v[k], a.W - d);
@@ -185,14 +234,14 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const L
   RowSums<TPR> sums(lds);
   const int group = threadIdx.x / TPR;
   const float inv = 1.0f / a.W;
-  auto left = [&](int k, int j) { return a.W - 8 * ((int)(threadIdx.x % TPR) + k * TPR) - (ODD ? j : 0); };
+  auto here = [&](int k, int j, float x) { return 8 * ((int)(threadIdx.x % TPR) + k * TPR) + (ODD ? j : 0) < a.W ? x : 0.0f; };
   Group<E, TPR, NV, ODD> x = {}, dy = {}, res = {}, w = {};
   if (a.w) w.load(a.w, 0, a.W);
   int64_t row = (int64_t)blockIdx.x * kRows + group;
   const int64_t step = (int64_t)gridDim.x * kRows;
   auto fetch = [&](int64_t at) {
     if (at >= a.rows) return;
-    x.load(a.x, at * a.xs, a.W);
+    x.load_row(a.x, at * a.xs, a.W);
     dy.load(a.dy, at * a.dys, a.W);
   };
   fetch(row);
@@ -204,33 +253,37 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void k_layer_norm_bwd(const L
     for (int k = 0; k < NV; ++k) {
       Elem<E>::unpack(x.raw[k], v[k]);
       Elem<E>::unpack(dy.raw[k], g[k]);
+    }
+    const float x0 = x.first(v[0][0]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool on = in && left(k, j) > 0;
-        t[0] += on ? v[k][j] : 0.0f;
-        g[k][j] = on ? g[k][j] : 0.0f;
-      }
+    for (int k = 0; k < NV; ++k) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[0] += v[k][j] - here(k, j, x0);
     }
     if (a.dres && in) res.load(a.dres, row * a.drs, a.W);
     fetch(row + step);
     sums.sum(t);
-    const float m = t[0] * inv;
+    const float m = x0 + t[0] * inv;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float wk[8];
       Elem<E>::unpack(w.raw[k], wk);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        v[k][j] = in && left(k, j) > 0 ? v[k][j] - m : 0.0f;
+        v[k][j] -= here(k, j, m);
         const float gw = a.w ? g[k][j] * wk[j] : g[k][j];
         u[0] += v[k][j], u[1] += v[k][j] * v[k][j];
         u[2] += gw, u[3] += gw * v[k][j];
       }
     }
     sums.sum(u);
-    const float c = u[0] * inv, r = inv_rms(fmaxf(u[1] * inv - c * c, 0.0f), a.eps);
-    const float s1 = u[2] * inv, s2 = r * (u[3] * inv - c * s1);
-    if (!in) continue;
+    const Stats st(u[0], u[1], inv, a.eps);
+    const float c = st.c, r = st.r, s1 = u[2] * inv, s2 = st.far ? 0.0f : r * (u[3] * inv - c * s1);
+    if (__any(st.far)) {
+      const float n = zeros_of(sums, in ? (const E*)a.x + row * a.xs : nullptr, a.W);
+      if (st.far) fill(v, n);
+    }
+    if (!in) continue;  // (what the sums of such a row are does not matter)
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int d = 8 * ((int)(threadIdx.x % TPR) + k * TPR);
@@ -289,14 +342,15 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_wide(const LayerNormArgs 
   };
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const int64_t x = row * a.xs;
-    float t[1] = {0.0f}, u[2] = {0.0f, 0.0f}, v[8];
+    const float x0 = (float)((const E*)a.x)[x];
+    float t[2] = {0.0f, 0.0f}, u[2] = {0.0f, 0.0f}, v[8];
     for (int d = 8 * threadIdx.x; d < a.W; d += 8 * kBlock) {
       values(a.x, x, d, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[0] += v[j];
+      for (int j = 0; j < 8; ++j) t[0] += d + j < a.W ? v[j] - x0 : 0.0f, t[1] += 0.0f * v[j];
     }
     sums.sum(t);
-    const float m = t[0] * inv;
+    const float m = x0 + t[0] * inv;
     for (int d = 8 * threadIdx.x; d < a.W; d += 8 * kBlock) {
       values(a.x, x, d, v);
 #pragma unroll
@@ -306,7 +360,7 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_wide(const LayerNormArgs 
       }
     }
     sums.sum(u);
-    const float c = u[0] * inv, r = inv_rms(fmaxf(u[1] * inv - c * c, 0.0f), a.eps);
+    const Stats st(u[0], u[1], inv, a.eps);
     for (int d = 8 * threadIdx.x; d < a.W; d += 8 * kBlock) {
       float w[8], b[8];
       values(a.x, x, d, v);
@@ -314,7 +368,7 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_wide(const LayerNormArgs 
       if (a.b) values(a.b, 0, d, b);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float n = (v[j] - m - c) * r;
+        const float n = st.far ? t[1] : (v[j] - m - st.c) * st.r;
         v[j] = (a.w ? n * w[j] : n) + (a.b ? b[j] : 0.0f);
       }
       store8<E, true>(a.y, row * a.ys + d, v, a.W - d);
@@ -347,15 +401,16 @@ __global__ __launch_bounds__(1024) void k_layer_norm_bwd_wide(const LayerNormArg
   };
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const int64_t x = row * a.xs, dy = row * a.dys;
-    float t[1] = {0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float x0 = (float)((const E*)a.x)[x];
+    float t[2] = {0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     groups([&](int d, int) {
       float v[8];
       values(a.x, x, d, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[0] += v[j];
+      for (int j = 0; j < 8; ++j) t[0] += d + j < a.W ? v[j] - x0 : 0.0f, t[1] += 0.0f * v[j];
     });
     sums.sum(t);
-    const float m = t[0] * inv;
+    const float m = x0 + t[0] * inv;
     groups([&](int d, int) {
       float v[8], g[8], w[8];
       values(a.x, x, d, v);
@@ -368,8 +423,8 @@ __global__ __launch_bounds__(1024) void k_layer_norm_bwd_wide(const LayerNormArg
       }
     });
     sums.sum(u);
-    const float c = u[0] * inv, r = inv_rms(fmaxf(u[1] * inv - c * c, 0.0f), a.eps);
-    const float s1 = u[2] * inv, s2 = r * (u[3] * inv - c * s1);
+    const Stats st(u[0], u[1], inv, a.eps);
+    const float c = st.c, r = st.r, s1 = u[2] * inv, s2 = st.far ? 0.0f : r * (u[3] * inv - c * s1);
     groups([&](int d, int k) {
       float v[8], g[8], w[8], rd[8];
       values(a.x, x, d, v);
@@ -387,7 +442,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_bwd_wide(const LayerNormArg
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float n = (v[j] - m - c) * r;
+        const float n = st.far ? t[1] : (v[j] - m - c) * r;
         dw[k][j] += g[j] * n, db[k][j] += g[j];
         v[j] = r * ((a.w ? g[j] * w[j] : g[j]) - s1 - n * s2) + (a.dres ? rd[j] : 0.0f);
       }
