@@ -503,7 +503,8 @@ def layer_norm_backward(dy, x, weight=None, eps: float = 1e-5, bias: bool = True
 # ---------------------------------------------------------------- rotation with several axes
 def _axes(call, q, k, table, q_pos, k_pos, pair_axis, q_weight, k_weight, eps, interleaved):
     p = RotateAxesParams()
-    pair_axis = bytes(pair_axis)
+    if not isinstance(pair_axis, bytes):
+        pair_axis = bytes(list(pair_axis))  # (of a number, bytes() would make as many zeros)
     if table is None or table.dim() != 3 or len(pair_axis) != table.shape[2] or len(pair_axis) > 128:
         raise ValueError("table must be (positions, 2, pairs) and pair_axis name the axis of each of its pairs, 128 at most")
     if eps is None and (q_weight is not None or k_weight is not None):

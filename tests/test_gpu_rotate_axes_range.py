@@ -1,7 +1,9 @@
 """The rotation at positions of several axes: components that are no finite numbers
-past the rotated part of a head, in every form of the kernels."""
+past the rotated part of a head, in every form of the kernels; the forms in which the
+pairs' axes are given."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -82,3 +84,18 @@ def test_norm_of_heads_that_hold_no_numbers(L, D, rotated, kind, inter, dt):
         heads = torch.ones(T, H, dtype=torch.bool, device="cuda")
         heads[4, 1] = False
         assert torch.equal(dx[heads], wdx[heads]) and torch.equal(want, L.rotate_axes(make(x), None, *args, **kw)[0])
+
+
+def test_axes_of_pairs_as_bytes_or_numbers(L):
+    g = gen_of(3)
+    q, table = normal(g, 5, 2, 32), table_of(9, 16)
+    pos = torch.randint(0, 9, (5, 3), generator=g, device="cuda", dtype=torch.int32)
+    axis = [j % 3 for j in range(16)]
+    want = L.rotate_axes(q, None, table, pos, None, bytes(axis))[0]
+    for form in (axis, tuple(axis), bytearray(axis), iter(axis), np.array(axis), np.array(axis, dtype=np.int8),
+                 torch.tensor(axis), torch.tensor(axis, dtype=torch.uint8)):
+        assert torch.equal(L.rotate_axes(q, None, table, pos, None, form)[0], want)
+    # a number is not the axes of that many pairs
+    for bad in (16, np.int64(16), torch.tensor(16)):
+        with pytest.raises(TypeError):
+            L.rotate_axes(q, None, table, pos, None, bad)
