@@ -295,7 +295,8 @@ pnerf_status pnerf_quantize_states(const pnerf_states_params* params, const void
  * numbers, not only powers of two; those of one head's values within 2^96 of each
  * other.  exp(a - m) times the value scale, in a unit that follows it, is rounded to the
  * data type before it meets the values.  Keys, values and masks in places that are not allowed, and the scales of
- * blocks without an allowed key, have no influence.  No gradient: states are kept in 8
+ * blocks without an allowed key, have no influence.  A query with an infinity or NaN has
+ * NaN for o and lse where a key is allowed, 0 and -inf where none is.  No gradient: states are kept in 8
  * bits for proposals, not for training. */
 typedef struct {
   pnerf_attention_params attention;

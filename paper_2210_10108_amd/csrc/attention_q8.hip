@@ -126,10 +126,31 @@ struct ScaledRows : Rows<T, DP> {
   static constexpr float kLeast = kNarrow ? 1.0f : 0x1p-60f, kMost = kNarrow ? 0x1p7f : 0x1p60f;
   float c, unit, unit_next;
   float shift, back;  // log2 of the ratio, its inverse
+  bool bad;           // the query holds an infinity or NaN
 
   __device__ __forceinline__ void begin(const AttnArgs& a) {
     c = a.c, unit = unit_next = 0.0f;
     shift = 0.0f, back = 1.0f;
+  }
+  // A query with an infinity or NaN is taken as zeros: with it, the zeros that stand for
+  // keys that may not be read would give NaN.  Its row's sum becomes NaN in the end if there
+  // is an allowed key.  (To be called when other loads are on their way, too: it waits for
+  // the queries.)
+  __device__ __forceinline__ void clean() {
+    // an exponent of ones carries into its number's sign bit
+    constexpr uint32_t kExp = kNarrow ? 0x7C007C00u : 0x7F807F80u, kOne = kNarrow ? 0x04000400u : 0x00800080u;
+    uint32_t carry = 0;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      const uint4 w = this->qf[i];
+      carry |= ((w.x & kExp) + kOne) | ((w.y & kExp) + kOne) | ((w.z & kExp) + kOne) | ((w.w & kExp) + kOne);
+    }
+    const uint64_t here = __ballot((carry & 0x80008000u) != 0);  // a row is in lanes r and r + 32
+    const uint32_t rows = (uint32_t)here | (uint32_t)(here >> 32);
+    bad = rows >> (threadIdx.x & 31) & 1;
+    if (rows)
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i) this->qf[i] = bad ? make_uint4(0, 0, 0, 0) : this->qf[i];
   }
   // The scales of the next tile; one without an allowed key has none that count.
   __device__ __forceinline__ void scales(const AttnArgs& a, Scales& sc, int t, uint64_t vm) {
@@ -246,6 +267,7 @@ struct ScaledRows : Rows<T, DP> {
     }
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) this->o[i] *= unit;
+    if (bad && this->l != 0.0f) this->l = __builtin_nanf("");
   }
 };
 
@@ -346,6 +368,7 @@ __global__ __launch_bounds__(256 * KS, 3 - KS) void k_attn_q8_fwd(const AttnArgs
   fetch(t);
   if (t < at.t1) put(0);
   fetch(t + KS);
+  x.clean();
   const int rounds = (at.t1 - at.t0 + KS - 1) / KS;  // the same for both groups: they share the barrier
   int round = 0;
   x.run(
@@ -440,6 +463,7 @@ __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Ord
     kt.load(to_k, t, at.nk, vm_next, lane);
     vt.load(to_v, t, at.nk, vm_next, lane);
   }
+  x.clean();
   x.run(
       [&] {
         if (!first) {
@@ -475,6 +499,7 @@ __global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Ord
   ScaledRows<T, DP> x;
   x.template init<false>(at.q, at.ok, a.D, h);
   x.begin(a);
+  x.clean();
   int t = at.t0;
   x.run(
       [&] {
