@@ -291,13 +291,14 @@ pnerf_status pnerf_quantize_states(const pnerf_states_params* params, const void
 /* Cross attention to 8-bit states: pnerf_cross_attention with
  *   k_j = k_scale[j / PNERF_STATE_BLOCK] k8_j,  v_j = v_scale[j / PNERF_STATE_BLOCK] v8_j
  * as pnerf_quantize_states leaves them (attention.k_stride and v_stride are those of k8
- * and v8; attention.dtype is that of q and o).  The scales are positive normal
- * numbers, not only powers of two; those of one head's values within 2^96 of each
- * other.  exp(a - m) times the value scale, in a unit that follows it, is rounded to the
- * data type before it meets the values.  Keys, values and masks in places that are not allowed, and the scales of
- * blocks without an allowed key, have no influence.  A query with an infinity or NaN has
- * NaN for o and lse where a key is allowed, 0 and -inf where none is.  No gradient: states are kept in 8
- * bits for proposals, not for training. */
+ * and v8; attention.dtype is that of q and o).  The scales are any positive normal
+ * numbers, not only powers of two.  exp(a - m) times the value scale, in a unit that
+ * follows it, is rounded to the data type before it meets the values.  What a block adds
+ * is lost beside a row's result 2^50 times as large, and where its exp(a - lse) is below
+ * 2^-118.  Keys, values and masks in places that are not allowed, and the scales of blocks
+ * without an allowed key, have no influence.  A query with an infinity or NaN has NaN for
+ * o and lse where a key is allowed, 0 and -inf where none is.  No gradient: states are
+ * kept in 8 bits for proposals, not for training. */
 typedef struct {
   pnerf_attention_params attention;
   int64_t k_scale_stride[2], v_scale_stride[2]; /* (batch, block) */

@@ -115,23 +115,22 @@ struct Scales {
   }
 };
 
-// Rows whose tiles have scales: c of the scores, and the value scale's ratio to `unit`,
-// in which the sums are kept.  The ratio is a factor of p, by way of its exponent, where
-// its data type holds that: in float16 from 1 to 2^7 (p is at most 2^8, and what it
-// loses below 2^-14 must not grow), in bfloat16, which has float32's range, from 2^-60 to
-// 2^60.  For a tile outside, the unit changes and the sums are rescaled.
+// Rows whose tiles have scales: c of the scores, and the value scale, whose ratio to 2^e,
+// the unit in which a row's sums are kept, is a factor of p, by way of its exponent.  p's
+// data type has to hold that: in float16 ratios from 1 to 2^7 (p is at most 2^8, and what
+// it loses below 2^-14 must not grow), in bfloat16, which has float32's range, from 2^-60
+// to 2^60.  For a tile outside, the unit follows the scale and the sums are rescaled, as
+// far as they stay numbers that count: scales may be any positive normal ones.
 template <class T, int DP>
 struct ScaledRows : Rows<T, DP> {
   static constexpr bool kNarrow = std::is_same<T, F16>::value;
-  static constexpr float kLeast = kNarrow ? 1.0f : 0x1p-60f, kMost = kNarrow ? 0x1p7f : 0x1p60f;
-  float c, unit, unit_next;
-  float shift, back;  // log2 of the ratio, its inverse
-  bool bad;           // the query holds an infinity or NaN
+  static constexpr float kLeast = kNarrow ? 0.0f : -60.0f, kMost = kNarrow ? 7.0f : 60.0f;
+  static constexpr float kStart = kNarrow ? 3.0f : 0.0f;  // log2 of the ratio that a new unit begins with
+  float c, e;
+  float vk, vl;  // log2 of the tile's value scale: its whole part, the rest
+  bool bad;      // the query holds an infinity or NaN
 
-  __device__ __forceinline__ void begin(const AttnArgs& a) {
-    c = a.c, unit = unit_next = 0.0f;
-    shift = 0.0f, back = 1.0f;
-  }
+  __device__ __forceinline__ void begin(const AttnArgs& a) { c = a.c, e = 1e4f, vk = vl = 0.0f; }
   // A query with an infinity or NaN is taken as zeros: with it, the zeros that stand for
   // keys that may not be read would give NaN.  Its row's sum becomes NaN in the end if there
   // is an allowed key.  (To be called when other loads are on their way, too: it waits for
@@ -158,10 +157,50 @@ struct ScaledRows : Rows<T, DP> {
     float ks, vs;
     sc.of(t, ks, vs);
     c = fmaxf(a.c * ks, 0x1p-126f);  // (0 times a masked key's -inf would be NaN)
-    if (!(vs >= unit * kLeast && vs <= unit * kMost)) unit_next = kNarrow ? vs * 0x1p-3f : vs;
-    const float ratio = vs / unit_next;
-    shift = __builtin_amdgcn_logf(ratio);
-    back = __builtin_amdgcn_rcpf(ratio);
+    const uint32_t bits = __float_as_uint(vs);
+    vk = (float)((int)(bits >> 23) - 127);
+    vl = __builtin_amdgcn_logf(__uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u));
+  }
+  __device__ __forceinline__ bool outside() const {
+    const float r = vl + (vk - e);
+    return r < kLeast || r > kMost;
+  }
+  // log2 of the ratio.  It is less than kLeast only where sums of 2^100 make what the tile
+  // adds nothing (see unit); p itself, of which l is the sum, stays a number.
+  __device__ __forceinline__ float shift() const { return fmaxf(vl + (vk - e), -60.0f); }
+  // The largest of a lane's sums.
+  __device__ __forceinline__ float largest() const {
+    float x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x = fmaxf(x, fabsf(this->o[i][j]));
+    return x;
+  }
+  // The sums times 2^n.
+  __device__ __forceinline__ void move(int n) {
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) this->o[i][j] = __builtin_amdgcn_ldexpf(this->o[i][j], n);
+  }
+  // The unit to use from here on, given that the new maximum leaves 2^d of the sums.
+  __device__ __forceinline__ float unit(float d) const {
+    float to = outside() ? vk - kStart : e;
+    if (!__any(to != e)) return to;
+    // Down, as far as the row's largest sum stays below 2^101: beside it the tile, of less
+    // than 2^50 in that unit, is nothing.  Up, as far as that sum stays above 2^-91, where
+    // nothing is lost, or is nothing beside the tile, whose largest weight keeps 2^8 then.
+    float most = -INFINITY, x, y;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) most = fmaxf(most, this->s[i / 16][i % 16]);
+    halves(largest(), x, y);
+    const float at = ceilf(e + d + __builtin_amdgcn_logf(fmaxf(x, y)));  // -inf: nothing yet
+    halves(most, x, y);
+    const float weight = ceilf(c * fmaxf(x, y) - this->top + vk + vl);
+    if (to < e) to = fmaxf(to, at - 100.0f);
+    if (to > e && at > -INFINITY) to = fminf(to, fmaxf(at + 90.0f, weight - 8.0f));
+    return to;
   }
   // Queries in the order in which byte tiles hold the head's width (see bytes_swz).
   __device__ __forceinline__ void init_bytes(const uint16_t* q, bool ok, int D, int h) {
@@ -199,7 +238,7 @@ struct ScaledRows : Rows<T, DP> {
   }
   // The scores' exponentials times the ratio, and their sum.
   __device__ __forceinline__ void weights() {
-    const float base = (this->m == -INFINITY ? 0.0f : this->m) - shift;  // -inf: no allowed key yet
+    const float sh = shift(), base = (this->m == -INFINITY ? 0.0f : this->m) - sh;  // -inf: no allowed key yet
     float sum = 0.0f;
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -208,7 +247,7 @@ struct ScaledRows : Rows<T, DP> {
         this->s[n][i] = __builtin_amdgcn_exp2f(fmaf(this->s[n][i], c, -base));
         sum += this->s[n][i];
       }
-    this->l = fmaf(sum, back, this->l);
+    this->l = fmaf(sum, __builtin_amdgcn_exp2f(-sh), this->l);
   }
   __device__ __forceinline__ void add(const uint4* sv, int lane) {
     weights();
@@ -253,20 +292,33 @@ struct ScaledRows : Rows<T, DP> {
     bool more = next();
     while (more) {
       // to the new maximum and unit: l by the first, the sums by both
-      const float alpha = __builtin_amdgcn_exp2f(this->m - (this->top == -INFINITY ? 0.0f : this->top));
-      const float f = unit == unit_next || unit == 0.0f ? alpha : alpha * (unit / unit_next);
+      const float d = this->m - (this->top == -INFINITY ? 0.0f : this->top), to = unit(d);
+      const float alpha = __builtin_amdgcn_exp2f(d);
       this->m = this->top;
-      unit = unit_next;
       this->l *= alpha;
 #pragma unroll
-      for (int i = 0; i < DP / 32; ++i) this->o[i] *= f;
+      for (int i = 0; i < DP / 32; ++i) this->o[i] *= alpha;
+      if (__any(to != e)) move((int)(e - to));  // (2^(e - to) alone may be no number)
+      e = to;
       do {
         add_tile();
         more = next();
-      } while (more && !this->grown() && unit_next == unit);
+      } while (more && !this->grown() && !__any(outside()));
     }
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i) this->o[i] *= unit;
+    // Sums in the unit 1.  Where those would pass float32's range (the results, which l
+    // divides them by, need not) they and l are 2^-n of what they were, and m, of which
+    // they are multiples by exp2, is n more.
+    int n = 0;
+    if (__any(e > 16.0f)) {
+      float x, y;
+      halves(largest(), x, y);
+      const bool far = (int)e + __builtin_amdgcn_frexp_expf(fmaxf(x, y)) > 100;
+      halves(this->l, x, y);
+      if (far) n = 16 + __builtin_amdgcn_frexp_expf(x + y);
+      this->m += (float)n;
+      this->l = __builtin_amdgcn_ldexpf(this->l, -n);
+    }
+    move((int)e - n);
     if (bad && this->l != 0.0f) this->l = __builtin_nanf("");
   }
 };
@@ -491,7 +543,7 @@ __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Ord
 
 // Any strides, alignment and head width.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_q8_any(const AttnArgs a, const Order order) {
+__global__ __launch_bounds__(256, 2) void k_attn_q8_any(const AttnArgs a, const Order order) {
   __shared__ uint4 sk[kBN * DP / 8], sv[kBN * DP / 8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
   const Place at(a, item_of(a, order), 128, wave * 32 + (lane & 31));

@@ -1,12 +1,14 @@
 """Attention to 8-bit states at the end of the numbers' range: queries that hold
-infinities or NaN."""
+infinities or NaN, and scales of every size."""
 import math
 
 import pytest
 import torch
 
+from . import layers_common as R
+from . import more_layers_common as M
 from .test_gpu_layers import gen_of, normal, say
-from .test_gpu_states import states
+from .test_gpu_states import F8, states
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +52,82 @@ def test_queries_that_are_no_numbers(L, D, Sq, dt):
         assert torch.equal(lse.transpose(1, 2)[rest], clean[1].transpose(1, 2)[rest])
         # the row itself, with keys: no number
         assert bool(o[2:, row, 1:3].isnan().all()) and bool(lse[2:, 1:3, row].isnan().all()), junk
+
+
+def check_scales(L, q, k8, v8, ks, vs, what, **masks):
+    """As test_gpu_states' check, but with a bound that does not grow with the largest
+    value, which may have no weight: p is rounded relative to itself (u), in float16 to
+    2^-25 of the value at least (or less: the weights are below 2^8 in the row's unit,
+    2^-25 in which is 2^-33 of the largest), and what a block adds is lost only beside sums
+    2^50 times as large.  An exponential below 2^-126 is no 32-bit number, and a part of the
+    keys is joined by one of its largest p, which p reach 2^8 times of: weights below 2^-118
+    may be lost."""
+    say("scales", what, tuple(q.shape), q.dtype)
+    ref = R.attention_ref(q, M.widened(k8, ks), M.widened(v8, vs), **masks)
+    o, lse = L.cross_attention_q8(q, k8, v8, ks, vs, return_lse=True, **masks)
+    B, Sq, Hq, D = q.shape
+    G = Hq // k8.shape[2]
+    K, V = (M.widened(*t).repeat_interleave(G, 2) for t in ((k8, ks), (v8, vs)))
+    A = torch.einsum("bihd,bjhd->bhij", q.double(), K) * D ** -0.5
+    on = M.allowed(B, k8.shape[1], masks.get("kv_len"), masks.get("kv_mask"), q.device)
+    A = A.masked_fill(~on[:, None, None, :], -math.inf)
+    P = torch.softmax(A, 3)
+    V = V * on[:, :, None, None]
+    terms = torch.einsum("bhij,bjhd->bihd", P, V.abs())
+    terms_lost = torch.einsum("bhij,bjhd->bihd", torch.where(P < 2.0 ** -118, P, 0.0), V.abs())
+    e = 2 * ref["lse"][1].amax() + R.EF
+    u, tiny = R.U[R.name_of(q.dtype)], R.TINY[R.name_of(q.dtype)]
+    bound = (2 * u + 2 * e) * terms + 2.0 ** -50 * terms.amax(3, keepdim=True) + terms_lost + 2 * tiny
+    if q.dtype == torch.float16:
+        bound += 2.0 ** -24 * V.abs().sum(1)[:, None]
+    R.check(o, ref["o"][0], bound, what + " o")
+    R.check(lse, *ref["lse"], what + " lse")
+
+
+@pytest.mark.parametrize("Sq", [1, 40, 300])
+@pytest.mark.parametrize("D", [64, 128, 100])
+def test_states_of_blocks_far_apart_quantized(L, D, Sq):
+    # bfloat16 states whose blocks are of every size that the type has, in both orders and in
+    # turn; weights alike, or all on the small blocks, or all on the large ones
+    B, Sk, Hq, Hkv = 2, 64 * 7 + 9, 4, 2
+    g = gen_of(2)
+    q, k, v = (normal(g, B, S, H, D, dt="bf16") for S, H in ((Sq, Hq), (Sk, Hkv), (Sk, Hkv)))
+    q[..., 0] = 16.0
+    block = torch.arange(Sk, device="cuda") // 64
+    for large in (1.0, 1e36):
+        for small in (1e-37, 1e-30, 1e-20):
+            for name, first in (("falling", block < 3), ("rising", block >= 3), ("in turn", block % 2 == 0),
+                                ("one", block == 4), ("all but one", block != 4)):
+                x = (v.float() * torch.where(first, large, small)[None, :, None, None]).bfloat16()
+                for way in (0.0, 20.0, -20.0, 60.0, -60.0):  # scores apart by 32 |way| / sqrt(D)
+                    y = k.clone()
+                    y[..., 0] = torch.where(first, way, -way)[None, :, None]
+                    check_scales(L, q, *L.quantize_states(y, x), f"{large} {small} {name} {way}")
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("Sq", [1, 40, 300])
+@pytest.mark.parametrize("seed", range(6))
+def test_scales_of_every_size(L, seed, Sq, dt):
+    # any positive normal scales, block by block, and scores that move the weight between them
+    B, Sk, Hq, Hkv, D = 2, 64 * 24 + 5, 4, 2, (64, 128, 100)[seed % 3]
+    g = gen_of(100 + seed)
+    q = normal(g, B, Sq, Hq, D, dt=dt)
+    q[..., 0] = 16.0
+    nb = 25
+    top = 6.0 if dt == "f16" else 118.0
+    reach = (2.0, 30.0, 90.0, 125.0, 240.0, 60.0)[seed]
+    e = torch.rand(B, nb, Hkv, generator=g, device="cuda") * reach
+    vs = torch.exp2((top - e).clamp_min(-126.0))
+    if seed % 2:
+        vs = torch.exp2(torch.floor(torch.log2(vs)))
+    x = torch.randn(2, B, Sk, Hkv, D, generator=g, device="cuda") * 100
+    move = torch.randn(B, nb, Hkv, generator=g, device="cuda") * (0.0, 5.0, 30.0)[seed // 2]
+    x[0, ..., 0] = move.repeat_interleave(64, 1)[:, :Sk] * 8
+    k8, v8 = x.clamp(-448, 448).to(F8)
+    ks = torch.full((B, nb, Hkv), 2.0 ** -6, device="cuda")
+    check_scales(L, q, k8, v8, ks, vs, f"reach {reach}")
+    mask = torch.rand(B, Sk, generator=g, device="cuda") > 0.3
+    mask[0, 64:192] = False
+    kv_len = torch.tensor([Sk, 700], dtype=torch.int32, device="cuda")
+    check_scales(L, q, k8, v8, ks, vs, f"reach {reach} masked", kv_len=kv_len, kv_mask=mask)
