@@ -14,9 +14,10 @@ ProposalBlock runs it forward, for a batch of hypotheses or one at a time, and
 backward.  With image=True its token norms are layer norms, heads turn by a
 patch's row and column, and an image's keys and values can be made once
 (encode, in 16 or 8 bits) for any number of proposals (propose).
-`python -m paper_2210_10108_amd.propose` trains it that way on views of a
-synthetic field, its gradients clipped, and reports how far the hypotheses are
-from the true pose before and after.  The proposals are poses as Field.render_loss_grad takes them;
+`python -m paper_2210_10108_amd.propose` trains it on views of a synthetic field
+and reports how far the hypotheses are from the true pose before and after;
+--image trains it that way, its gradients clipped, and proposes from states in
+8 bits.  The proposals are poses as Field.render_loss_grad takes them;
 the optimisation itself is not run here.
 """
 from __future__ import annotations
@@ -284,15 +285,19 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     ap.add_argument("--steps", type=int, default=300)
     ap.add_argument("--workload", default="tiny_bump", choices=synth.ORDER)
-    ap.add_argument("--max-norm", type=float, default=100.0, help="bound on the gradients' norm (inf: none)")
-    ap.add_argument("--bits", type=int, default=8, choices=(8, 16), help="of the states that the proposals read")
+    ap.add_argument("--image", action="store_true", help="layer norms, and heads turned by a patch's row and column")
+    ap.add_argument("--max-norm", type=float, help="bound on the gradients' norm (default: 100 with --image, else none)")
+    ap.add_argument("--bits", type=int, choices=(8, 16), help="of the states that proposals read (default: 8 with --image, else 16)")
     args = ap.parse_args()
     views = Views(args.workload)
-    block = ProposalBlock(state_dim=views.state_dim, image=True)
-    train(block, views, args.steps, report=max(1, args.steps // 10), max_norm=args.max_norm)
-    poses, states, _, _, _, hyps, gt = views.batch(4, 64, 10 ** 6, block.dtype)
-    q_pos, k_pos = views.patch_positions(4, 64)
-    y = block.propose(poses, block.encode(states, k_pos, bits=args.bits), q_pos)
+    block = ProposalBlock(state_dim=views.state_dim, image=args.image)
+    max_norm = 100.0 if args.image and args.max_norm is None else args.max_norm
+    bits = args.bits or (8 if args.image else 16)
+    train(block, views, args.steps, report=max(1, args.steps // 10), max_norm=max_norm)
+    poses, states, q_pos, k_pos, _, hyps, gt = views.batch(4, 64, 10 ** 6, block.dtype)
+    if args.image:
+        q_pos, k_pos = views.patch_positions(4, 64)
+    y = block.propose(poses, block.encode(states, k_pos, bits=bits), q_pos)
     moved = corrected(hyps, y[..., :6].double().cpu().numpy())
     for name, p in (("hypotheses", hyps), ("proposals", moved)):
         r, t = errors(p, gt[:, None])
