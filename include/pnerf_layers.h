@@ -23,7 +23,8 @@
  * message from pnerf_last_error), `stream` is a hipStream_t (NULL = the default
  * stream), device pointers stay valid until the queued work has finished.
  * Further, for every call here:
- *  - It only enqueues kernels on `stream`: no synchronisation, no allocation, no
+ *  - It only enqueues kernels on `stream`: no synchronisation, no allocation (but for
+ *    host memory that pnerf_clip_gradients takes for its list and gives back), no
  *    state kept between calls, so it can be captured into a HIP graph, and calls
  *    on different streams or threads may overlap.
  *  - The workspace is the caller's: at least the bytes that the operator's
@@ -38,7 +39,7 @@
  *    an input, save where stated.  Any stride and any pointer aligned to its
  *    elements will do; the fast kernels want every row to start on 16 bytes
  *    (pointers and strides), as contiguous tensors with rows of a multiple of 8
- *    16-bit elements do.  (Linear layers copy large operands of other sizes and
+ *    16-bit elements do, and of 16 bytes for 8-bit states.  (Linear layers copy large operands of other sizes and
  *    strides to such rows in the workspace.  The workspace follows from sizes and
  *    strides alone: where those are of whole 16-byte chunks and only a pointer is off 16
  *    bytes nothing is copied, and a large product runs element by element, an order
@@ -194,8 +195,12 @@ pnerf_status pnerf_linear_backward(const pnerf_linear_params* params, const void
  * of equal elements has n = 0 exactly where eps > 0; where eps = 0 its n is NaN.  Where
  * the sum of a row's squared differences passes float32's range (differences of some
  * 10^19 / sqrt(W)) r and n are 0.  An infinity or NaN makes n NaN in all of its row.
- * Any width and alignment takes the fast kernels (a width of whole 16-byte chunks the
- * fastest); the gradient of rows wider than 16384 adds to its sums in memory, row by row.
+ * Squared differences are 32-bit numbers too: with eps = 0, r is as exact as their mean is
+ * where that is below 2^-126, and infinite where they are all below 2^-150.
+ * Rows of up to 16384 elements, 8192 in the gradient, are read once, whatever their width
+ * and alignment (fastest where they start on 16 bytes and have a multiple of 8 elements).
+ * Wider ones are read again for each step, and the gradient of rows wider than 16384 adds
+ * to the weights' sums in memory, row by row.
  *
  * Requires rows >= 0, 1 <= width <= 2^20, rows * width at most 2^40, finite eps >= 0;
  * any dtype. */
@@ -298,7 +303,13 @@ pnerf_status pnerf_quantize_states(const pnerf_states_params* params, const void
  * 2^-118.  Keys, values and masks in places that are not allowed, and the scales of blocks
  * without an allowed key, have no influence.  A query with an infinity or NaN has NaN for
  * o and lse where a key is allowed, 0 and -inf where none is.  No gradient: states are
- * kept in 8 bits for proposals, not for training. */
+ * kept in 8 bits for proposals, not for training.
+ * States in 8 bits take half the memory of those in 16.  With heads of 128 the attention
+ * takes 0.55 to 0.6 of the other one's time at up to 32 rows of a kv head (q_rows q_heads
+ * / kv_heads), 0.8 at 64 and 1 to 1.1 beyond; with heads of 64, whose states are fewer
+ * bytes, 0.8 to 1.25.  The fast kernels want a head_dim of a multiple of 16 and rows of k8
+ * and v8 on 16 bytes; others take 4 to 8 times as long, where the attention to 16-bit
+ * states is fast at multiples of 8. */
 typedef struct {
   pnerf_attention_params attention;
   int64_t k_scale_stride[2], v_scale_stride[2]; /* (batch, block) */

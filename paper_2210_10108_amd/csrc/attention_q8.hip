@@ -249,6 +249,9 @@ struct ScaledRows : Rows<T, DP> {
       }
     this->l = fmaf(sum, __builtin_amdgcn_exp2f(-sh), this->l);
   }
+  // (Rounding them to the data type, as the matrix instructions take them, leaves an error
+  // against 64 bits of 1.8e-3 in bfloat16 and 2.1e-4 in float16, where the result's own
+  // rounding makes 1.6e-3 and 2.1e-4.)
   __device__ __forceinline__ void add(const uint4* sv, int lane) {
     weights();
 #pragma unroll
@@ -384,8 +387,8 @@ struct ByteTile {
 // next in registers on its way there.  One barrier a tile.  KS = 2: as in k_attn_fwd.
 // Matrix products, exponentials and LDS reads bound it, as with 16-bit states, and the
 // widening on top: 13 vector instructions for each product of 32 cycles (2 x 4096 rows, 8192
-// keys, 32 heads of 128 over 8, bf16: 1255 us or 0.88 PFLOP/s where 16-bit states take 1116; 5%
-// of the keys masked costs 20% more).  Tried and slower: the next tile widened beside the
+// keys, 32 heads of 128 over 8, bf16: 1202 us or 0.91 PFLOP/s where 16-bit states take 1112; 5%
+// of the keys masked: 1245 and 1240).  Tried and slower: the next tile widened beside the
 // scores' products (spills), or by one group after them, and sums of unmasked tiles that
 // start from the instruction's own zero.
 template <class T, int DP, int KS>
@@ -489,8 +492,8 @@ struct ByteRows {
 // and values in LDS, as bytes, and no barrier; keys are loaded again as soon as the
 // scores are there, values as soon as they have been used.  The bytes are widened on
 // the way from LDS to the products: each is read once.  (One token over 131109 rows, 32
-// heads of 128 over 8: 60 us or 4.5 TB/s and the join's 5; 64 ragged entries of up to 2500
-// rows, 16 heads over 4: 27 us, 42 with four wavefronts and tiles widened through registers.)
+// heads of 128 over 8: 59 us or 4.6 TB/s and the join's 5; 64 ragged entries of up to 2500
+// rows, 16 heads over 4: 26.7 us, 42 with four wavefronts and tiles widened through registers.)
 template <class T, int DP>
 __global__ __launch_bounds__(512) void k_attn_q8_few(const AttnArgs a, const Order order) {
   constexpr int kWaves = 8, kTile = kBN * DP;

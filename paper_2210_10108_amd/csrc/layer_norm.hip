@@ -3,8 +3,8 @@
 // with g = dy w, n = (x - mean) r, r = 1 / sqrt(var + eps).
 //
 // A stream, bound by memory: x in and y out, x, dy (and dres) in and dx out (16384 x 1024
-// bf16: 13.8 us or 4.9 TB/s forward, 25 us or 4.0 TB/s backward with its sums; 8192 x 3000
-// f32: 5.2 and 6.2 TB/s; a copy reaches 5.2).
+// bf16: 13.9 us or 4.8 TB/s forward, 24.7 us or 4.1 TB/s backward with its sums; 8192 x 3000
+// f32: 5.1 and 5.1 TB/s; a copy reaches 5.2).
 //
 // Sums are float32.  A row's mean is taken in two steps, m = x_0 + mean(x - x_0) and then
 // c = mean(x - m), and var = mean (x - m)^2 - c^2: rows whose mean is large beside their

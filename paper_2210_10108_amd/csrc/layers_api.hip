@@ -1,5 +1,6 @@
 // C ABI of the layer operators (include/pnerf_layers.h): argument checks and the
-// kernels' arguments.  Nothing here allocates or synchronises.
+// kernels' arguments.  Nothing here synchronises or allocates device memory; clipping has
+// its list in host memory for the length of the call.
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>

@@ -100,7 +100,9 @@ class ProposalBlock:
 
     def encode(self, states, k_pos, kv_len=None, kv_mask=None, bits=16):
         """An image's keys and values for propose: (k, v) of states [B, T, state_dim],
-        or with bits=8 (k8, v8, k_scale, v_scale)."""
+        or with bits=8 (k8, v8, k_scale, v_scale), which take half the memory.  (Not less
+        time, with these heads of 64: 64 hypotheses over 300 patches, attention 10.4 us
+        where 16 bits take 8.5; over one set of 131109 states a single one 17 and 21.)"""
         B, T, _ = states.shape
         kv = L.linear(states.reshape(B * T, -1), self.p["w_kv"]).view(B * T, 2, self.kv_heads, self.D)
         if self.image:
