@@ -72,3 +72,35 @@ def test_rows_of_equal_elements(L, W, dt):
     R.check(dx, *ref["dx"], "dx")
     assert bool((dw == 0).all())
     R.check(db, *ref["db"], "db")
+
+
+@pytest.mark.parametrize("shape", [(300001, 24), (70001, 250), (40001, 1000), (9001, 2048), (9001, 2999), (5001, 8192),
+                                   (4301, 12288), (700, 20001)], ids=str)
+def test_such_rows_among_many(L, shape):
+    # rows of equal elements and rows past the range beside ordinary ones, in every step of
+    # the kernels' walks; then rows without numbers, which take no other row with them
+    g = gen_of(3)
+    rows, W = shape
+    x, dy, dres = (normal(g, rows, W, dt="bf16") for _ in range(3))
+    w, b = normal(g, W, dt="bf16"), normal(g, W, dt="bf16")
+    i = torch.arange(rows, device="cuda")
+    far, equal = i % 7 == 3, i % 11 == 5
+    equal &= ~far
+    x[far] *= 1e30
+    x[equal] = x[equal][:, :1] * 1e9
+    say("rows among many", shape)
+    ref = M.layer_norm_ref(torch.where((far | equal)[:, None], torch.zeros_like(x), x), w, b, 1e-5, dy, dres)
+    y = L.layer_norm(x, w, b)
+    dx, dw, db = L.layer_norm_backward(dy, x, w, residual_grad=dres)
+    assert bool((y[far | equal] == b).all()) and torch.equal(dx[far], dres[far])
+    R.check(y[~far], ref["y"][0][~far], ref["y"][1][~far], "y")
+    R.check(dx[~far], ref["dx"][0][~far], ref["dx"][1][~far], "dx")
+    R.check(dw, *ref["dw"], "dw")
+    R.check(db, *ref["db"], "db")
+    none = i % 5 == 1
+    x[none, (i[none] * 31) % W] = math.nan
+    x[i % 35 == 11, W - 1] = math.inf
+    z = L.layer_norm(x, w, b)
+    dz = L.layer_norm_backward(dy, x, w, residual_grad=dres)[0]
+    assert bool(z[none].isnan().all()) and bool(dz[none].isnan().all())
+    assert torch.equal(z[~none], y[~none]) and torch.equal(dz[~none], dx[~none])

@@ -131,3 +131,30 @@ def test_scales_of_every_size(L, seed, Sq, dt):
     mask[0, 64:192] = False
     kv_len = torch.tensor([Sk, 700], dtype=torch.int32, device="cuda")
     check_scales(L, q, k8, v8, ks, vs, f"reach {reach} masked", kv_len=kv_len, kv_mask=mask)
+
+
+@pytest.mark.parametrize("Sq,Sk", [(1, 40003), (7, 9000), (600, 3000)])
+@pytest.mark.parametrize("D", [64, 128, 33])
+def test_values_near_the_largest_number_over_many_keys(L, D, Sq, Sk):
+    # their weighted sums pass float32's range, the results do not: by parts of the key axis,
+    # by wavefronts and by groups of them
+    g = gen_of(5)
+    B, Hq, Hkv = 1, 4, 2
+    q, k = normal(g, B, Sq, Hq, D, dt="bf16", std=0.1), normal(g, B, Sk, Hkv, D, dt="bf16")
+    v = (1 + torch.rand(B, Sk, Hkv, D, generator=g, device="cuda")) * 1.4e38
+    block = (torch.arange(Sk, device="cuda") // 64 % 5)[None, :, None, None]
+    for name, x in (("all", v), ("of both signs", v * torch.sign(torch.randn(v.shape, generator=g, device="cuda"))),
+                    ("one block in five", torch.where(block == 3, v, v * 1e-30)), ("four in five", torch.where(block == 3, v * 1e-60, v))):
+        check_scales(L, q, *L.quantize_states(k, x.bfloat16()), name)
+    # a query that is no number, its sums joined too
+    bad = q.clone()
+    bad[0, Sq - 1, 1, 0] = math.inf
+    packed = L.quantize_states(k, v.bfloat16())
+    want, got = (L.cross_attention_q8(t, *packed, return_lse=True) for t in (q, bad))
+    assert bool(got[0][0, Sq - 1, 1].isnan().all()) and bool(got[1][0, 1, Sq - 1].isnan())
+    rest = torch.ones(Sq, Hq, dtype=torch.bool, device="cuda")
+    rest[Sq - 1, 1] = False
+    assert torch.equal(got[0][0][rest], want[0][0][rest])
+    none = torch.zeros(B, Sk, dtype=torch.bool, device="cuda")
+    o, lse = L.cross_attention_q8(bad, *packed, kv_mask=none, return_lse=True)
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all())
