@@ -22,7 +22,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_fwd(const NormArgs a, int block
   const NormSide& x = second ? a.side[1] : a.side[0];
   const int blk = second ? blockIdx.x - blocks0 : blockIdx.x, blocks = second ? blocks1 : blocks0;
   const int d = 8 * (threadIdx.x % LR);
-  const bool col = d < a.D;
+  // what lies past the rotated part passes as it is (see rotate_axes.hip)
+  const bool col = d < a.D, turned = P == kHalf || d < a.R;
   float w[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) w[i] = 1.0f;
@@ -53,8 +54,9 @@ __global__ __launch_bounds__(kBlock) void k_norm_fwd(const NormArgs a, int block
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= r * w[j];
     partners<P, LR>(a, d, v, p);
+    if (turned)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * c[j] + p[j] * s[j];
+      for (int j = 0; j < 8; ++j) v[j] = v[j] * c[j] + p[j] * s[j];
     if (here) Elem<E>::store(y, v);
   }
 }
@@ -68,7 +70,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(const NormArgs a, int block
   const NormSide& x = second ? a.side[1] : a.side[0];
   const int blk = second ? blockIdx.x - blocks0 : blockIdx.x, blocks = second ? blocks1 : blocks0;
   const int grp = threadIdx.x / LR, d = 8 * (threadIdx.x % LR);
-  const bool col = d < a.D;
+  const bool col = d < a.D, turned = P == kHalf || d < a.R;
   float w[8], dw[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) w[i] = 1.0f, dw[i] = 0.0f;
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(const NormArgs a, int block
     float q = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      g[j] = here ? g[j] * c[j] - p[j] * s[j] : 0.0f;  // turned back
+      g[j] = !here ? 0.0f : turned ? g[j] * c[j] - p[j] * s[j] : g[j];  // turned back
       v[j] = here ? v[j] : 0.0f;
       q += v[j] * v[j];
       dot += g[j] * w[j] * v[j];

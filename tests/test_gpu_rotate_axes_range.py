@@ -99,3 +99,30 @@ def test_axes_of_pairs_as_bytes_or_numbers(L):
     for bad in (16, np.int64(16), torch.tensor(16)):
         with pytest.raises(TypeError):
             L.rotate_axes(q, None, table, pos, None, bad)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("D,rotated", [(64, 0), (64, 32), (128, 64), (256, 16)])
+def test_norm_rotate_of_heads_that_hold_no_numbers(L, D, rotated, inter, dt):
+    # the same of the operator with one position a row
+    g = gen_of(4)
+    T, H = 19, 3
+    x, dy, w = normal(g, T, H, D, dt=dt), normal(g, T, H, D, dt=dt), normal(g, D, dt=dt)
+    table = table_of(40, rotated // 2) if rotated else None
+    pos = torch.randint(0, 40, (T,), generator=g, device="cuda", dtype=torch.int32) if rotated else None
+    at = rotated + 5
+    others = torch.ones(D, dtype=torch.bool, device="cuda")
+    others[at] = False
+    heads = torch.ones(T, H, dtype=torch.bool, device="cuda")
+    heads[4, 1] = False
+    for make in (lambda t: t, odd_rows):
+        wdx, _, wdw, _ = L.norm_rotate_backward(make(dy), None, make(x), None, w, None, table, pos, None, interleaved=inter)
+        bad = x.clone()
+        bad[4, 1, at] = math.inf
+        y = L.norm_rotate(make(bad), None, w, None, table, pos, None, interleaved=inter)[0]
+        assert bool(y[4, 1, at].isnan()) and bool((y[4, 1, others] == 0).all())
+        bad = dy.clone()
+        bad[4, 1, at] = math.inf
+        dx, _, dw, _ = L.norm_rotate_backward(make(bad), None, make(x), None, w, None, table, pos, None, interleaved=inter)
+        assert not bool(torch.isfinite(dw[at])) and torch.equal(dw[others], wdw[others]) and torch.equal(dx[heads], wdx[heads])
